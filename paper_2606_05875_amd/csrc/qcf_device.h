@@ -83,21 +83,18 @@ inline RopeFreq<kBig> rope_freq(double theta, int d) {
   return r;
 }
 
-// The (cos, sin) of pos * omega_j, formed in float64 and rounded to float32.  The angle is reduced
-// by multiples of pi/2 (two-part constant, one fused multiply-add each: exact to float64 rounding
+// The (cos, sin) of the angle x, formed in float64 and rounded to float32 (kMag: multiplied by mag
+// first).  The angle is reduced by multiples of pi/2 (two-part constant, one fused multiply-add each: exact to float64 rounding
 // for angles below 2^52; kernels of their own send larger ones through the library, whose code in
 // every kernel cost assembly 0.5%) and both functions come from their Taylor series on [-pi/4, pi/4] (first omitted terms below 1e-16).  With the
 // library's pow and sincos a block's start took longer: assembling a 32K-token request 58.7 ->
 // 56.1 us, a layer recompute of 10 x 512 tokens ~1 us less in each of its two rotations.
-template <bool kBig>
-__device__ __forceinline__ float2 rope_cs(double pos, int j, const RopeFreq<kBig>& fr) {
-  double x = pos;
-#pragma unroll
-  for (int i = 0; i < 6; ++i) x = (j >> i) & 1 ? x * fr.f[i] : x;
+template <bool kBig, bool kMag = false>
+__device__ __forceinline__ float2 angle_cs(double x, double mag = 1.0) {
   if (kBig && !(fabs(x) < 0x1p52)) {  // (infinity, NaN: NaN)
     double s, c;
     sincos(x, &s, &c);
-    return make_float2((float)c, (float)s);
+    return kMag ? make_float2((float)(c * mag), (float)(s * mag)) : make_float2((float)c, (float)s);
   }
   const double k = rint(x * 0x1.45f306dc9c883p-1);  // 2 / pi
   double r = fma(-k, 0x1.921fb54442d18p+0, x);
@@ -122,9 +119,22 @@ __device__ __forceinline__ float2 rope_cs(double pos, int j, const RopeFreq<kBig
   c = fma(c, z, 1.0);
   const double kq = k * 0.25;
   const int q = (int)((kq - floor(kq)) * 4.0);  // quadrant
+  if (kMag) {
+    s *= mag;
+    c *= mag;
+  }
   const float sf = (float)s, cf = (float)c;
   const float co = q & 1 ? sf : cf, si = q & 1 ? cf : sf;
   return make_float2((q + 1) & 2 ? -co : co, q & 2 ? -si : si);
+}
+
+// The (cos, sin) of pos * omega_j.
+template <bool kBig>
+__device__ __forceinline__ float2 rope_cs(double pos, int j, const RopeFreq<kBig>& fr) {
+  double x = pos;
+#pragma unroll
+  for (int i = 0; i < 6; ++i) x = (j >> i) & 1 ? x * fr.f[i] : x;
+  return angle_cs<kBig>(x);
 }
 
 // One rotate-half pair (x1, x2) turned by the angle whose (cos, sin) is cs:

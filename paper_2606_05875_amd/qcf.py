@@ -22,6 +22,8 @@ __all__ = [
     "qcf_select_topk", "qcf_probe_scores_select", "qcf_probe_scores_select_noalloc",
     "qcf_sparse_prefill_attn", "qcf_sparse_prefill_attn_rope", "rope_position_table", "qcf_sparse_prefill_attn_workspace_size",
     "qcf_mfma_loop",
+    "qcf_page_plan", "qcf_rope_frequencies", "rope_frequencies", "qcf_rope_store", "qcf_tree_attn_workspace_size",
+    "qcf_tree_attn", "qcf_verify_drafts_workspace_size", "qcf_verify_drafts",
     "EXPORTS", "Prepared", "prepare",
 ]
 
@@ -33,8 +35,10 @@ _P = ctypes.c_void_p
 _I64 = ctypes.c_int64
 _I = ctypes.c_int
 _SZ = ctypes.c_size_t
+_D = ctypes.c_double
+_F = ctypes.c_float
 
-# name -> (restype, argtypes); mirrors include/qcf.h
+# name -> (restype, argtypes); mirrors include/qcf.h and include/qcf_decode.h
 EXPORTS = {
     "qcf_version": (_I, []),
     "qcf_status_string": (ctypes.c_char_p, [_I]),
@@ -67,6 +71,17 @@ EXPORTS = {
     "qcf_sparse_prefill_attn": (_I, [_P, _P, _P, _P, _I64, _P, _P, _P, _I64, _I64, _P, _P, _I, _I,
                                      _I, _I, _I, _I, _I, ctypes.c_float, _P, _SZ, _P]),
     "qcf_mfma_loop": (_I, [_P, _I64, _P, _I64, _P, _I, _I, _P]),
+    "qcf_page_plan": (_I, [_P, _I64, _I, _I, _P, _P, _P, _P, _I64, _P, _I64, _I, _I, _P, _P, _I, _P, _P, _I64,
+                           _P, _P, _P, _P, _P]),
+    "qcf_rope_frequencies": (_I, [_P, _I, _D, _I, _D, _D, _D, _D]),
+    "qcf_rope_store": (_I, [_P, _P, _I64, _I64, _P, _P, _P, _I64, _P, _I64, _I64, _P, _I, _I64, _P, _P, _P, _I,
+                            _I, _F, _I, _I, _I, _P]),
+    "qcf_tree_attn_workspace_size": (_SZ, [_I, _I, _I, _I, _I, _I, _I]),
+    "qcf_tree_attn": (_I, [_P, _P, _P, _I64, _P, _P, _P, _I64, _I64, _P, _I64, _I, _I, _P, _P, _I, _I, _I, _I,
+                           _I, _I, _I, _I, _F, _P, _SZ, _P]),
+    "qcf_verify_drafts_workspace_size": (_SZ, [_I, _I]),
+    "qcf_verify_drafts": (_I, [_P, _P, _P, _P, _P, _I64, _I, _I64, _I, _P, _P, _I, _P, _I, _P, _P, _P, _P, _P,
+                               _P, _SZ, _P]),
 }
 
 
@@ -608,3 +623,221 @@ def qcf_mfma_loop(operands, sink, clocks, blocks, iters):
         raise QcfError("clocks needs 32 entries, sink blocks * 256, operands a dense buffer")
     _invoke("qcf_mfma_loop", _ptr(operands), operands.numel(), _ptr(sink), sink.numel(), _ptr(clocks),
             int(blocks), int(iters))
+
+
+# -- answering from the fused cache (include/qcf_decode.h) ----------------------
+def _here(name, **tensors):
+    """All tensors on the current device, whose stream the call takes."""
+    for n, t in tensors.items():
+        _dev(t, n)
+    devices = {t.device.index for t in tensors.values() if t is not None}
+    if len(devices) > 1 or (devices and devices != {torch.cuda.current_device()}):
+        raise QcfError(f"{name}: every tensor must be on the current device")
+
+
+def _table(t):
+    _dev(t, "block_table", torch.int32)
+    if t.dim() != 2 or (t.numel() and t.stride(1) != 1):
+        raise QcfError("block_table must be [batch, pages] with dense rows")
+    return max(t.stride(0), t.shape[1]) if t.shape[0] <= 1 else t.stride(0)
+
+
+def _one_or_none(t, name, n):
+    _i32(t, name)
+    if t is not None and t.numel() != n:
+        raise QcfError(f"{name} must have {n} entries")
+
+
+def _row_stride(t, name, width):
+    """Distance of a [rows, heads, d] tensor's rows (a single row may have any)."""
+    return _rows(t, name) if t.shape[0] > 1 else max(_rows(t, name), width)
+
+
+def qcf_page_plan(block_table, kv_len, new_len, free_pages, slots, positions, cu_new, page_size, n_pages, max_new,
+                  pages_held=None, free_head=None, kv_end=None, pages_held_out=None, free_head_out=None,
+                  parents=None, tree_mask=None):
+    """Pages, slots and positions (with parents: by depth, and ancestor masks) of the new rows."""
+    stride = _table(block_table)
+    batch, n = kv_len.numel(), slots.numel()
+    for name, t, size in (("kv_len", kv_len, batch), ("new_len", new_len, batch), ("slots", slots, n),
+                          ("positions", positions, n), ("cu_new", cu_new, batch + 1),
+                          ("pages_held", pages_held, batch), ("free_head", free_head, 1), ("kv_end", kv_end, batch),
+                          ("pages_held_out", pages_held_out, batch), ("free_head_out", free_head_out, 1),
+                          ("parents", parents, n)):
+        _one_or_none(t, name, size)
+    _i32(free_pages, "free_pages")
+    _i32(tree_mask, "tree_mask")
+    if block_table.shape[0] != batch:
+        raise QcfError("block_table needs a row per request")
+    if (parents is None) != (tree_mask is None):
+        raise QcfError("parents and tree_mask go together")
+    if tree_mask is not None and (tree_mask.dim() != 2 or tree_mask.shape[0] != n):
+        raise QcfError("tree_mask must be [rows, words]")
+    _here("qcf_page_plan", block_table=block_table, kv_len=kv_len, new_len=new_len, free_pages=free_pages,
+          slots=slots, positions=positions, cu_new=cu_new, pages_held=pages_held, free_head=free_head, kv_end=kv_end,
+          pages_held_out=pages_held_out, free_head_out=free_head_out, parents=parents, tree_mask=tree_mask)
+    _invoke("qcf_page_plan", _ptr(block_table), stride, block_table.shape[1], batch, _ptr(kv_len), _ptr(new_len),
+            _ptr(pages_held), _ptr(free_pages), free_pages.numel(), _ptr(free_head), int(n_pages), int(page_size),
+            int(max_new), _ptr(parents), _ptr(tree_mask), 0 if tree_mask is None else tree_mask.shape[1], _ptr(slots),
+            _ptr(positions), n, _ptr(cu_new), _ptr(kv_end), _ptr(pages_held_out), _ptr(free_head_out))
+
+
+ROPE_SCALING = {"none": 0, "linear": 1, "by_parts": 2}
+
+
+def qcf_rope_frequencies(freq, rope_theta, scaling="none", factor=1.0, low_turns=1.0, high_turns=4.0,
+                         trained_len=0.0):
+    """freq (float64 CPU tensor [rotary_dim / 2]) <- the angular frequencies of the rotary pairs; host call."""
+    if freq.is_cuda or freq.dtype != torch.float64 or not freq.is_contiguous():
+        raise QcfError("freq must be a dense float64 CPU tensor")
+    if scaling not in ROPE_SCALING:
+        raise QcfError(f"scaling must be one of {tuple(ROPE_SCALING)}, not {scaling!r}")
+    _check(lib().qcf_rope_frequencies(_ptr(freq), 2 * freq.numel(), float(rope_theta), ROPE_SCALING[scaling],
+                                      float(factor), float(low_turns), float(high_turns), float(trained_len)),
+           "qcf_rope_frequencies")
+
+
+def rope_frequencies(rotary_dim, rope_theta, device="cuda", **scaling):
+    """The device array of frequencies that qcf_rope_store reads (a constant of the model)."""
+    if rotary_dim % 2:
+        raise QcfError("rotary_dim must be even")
+    freq = torch.empty(rotary_dim // 2, dtype=torch.float64)
+    qcf_rope_frequencies(freq, rope_theta, **scaling)
+    return freq.to(device)
+
+
+def qcf_rope_store(k_cache, v_cache, k_new, v_new, slots, positions=None, freq=None, interleaved=False,
+                   magnitude=1.0, q_new=None, q_out=None, src_idx=None):
+    """New rows' keys (turned) and values into cache slots, queries turned into q_out; the rotated
+    part of a head is 2 * len(freq) wide.  Without positions nothing is turned; k_cache, v_cache,
+    k_new, v_new and slots may be None together (queries only)."""
+    some = k_cache if k_cache is not None else q_new
+    if some is None:
+        raise QcfError("qcf_rope_store needs keys and values or queries")
+    dt = some.dtype
+    for name, t in (("k_cache", k_cache), ("v_cache", v_cache), ("k_new", k_new), ("v_new", v_new),
+                    ("q_new", q_new), ("q_out", q_out)):
+        _dev(t, name, dt)
+    for name, t in (("slots", slots), ("positions", positions), ("src_idx", src_idx)):
+        _i32(t, name)
+    _dev(freq, "freq", torch.float64)
+    if (positions is None) != (freq is None) or (freq is not None and not freq.is_contiguous()):
+        raise QcfError("positions and freq (dense) go together")
+    if len({x is None for x in (k_cache, v_cache, k_new, v_new, slots)}) > 1:
+        raise QcfError("k_cache, v_cache, k_new, v_new and slots go together")
+    if (q_new is None) != (q_out is None):
+        raise QcfError("q_new and q_out go together")
+    src = k_new if k_new is not None else q_new
+    idx = [x for x in (slots, positions, src_idx) if x is not None]
+    n = idx[0].numel() if idx else src.shape[0]
+    if any(x.numel() != n for x in idx) or (src_idx is None and src.shape[0] < n):
+        raise QcfError("slots, positions and src_idx need one entry per row, and without src_idx the rows exist")
+    hkv = hq = 1
+    n_slots = c_stride = n_stride = q_stride = 0
+    d = src.shape[-1]
+    if src.dim() != 3 or some.dim() != 3:
+        raise QcfError("tensors must be [rows, heads, head_dim]")
+    if k_cache is not None:
+        n_slots, hkv, _ = k_cache.shape
+        hq = hkv
+        c_stride, n_stride = _row_stride(k_cache, "k_cache", hkv * d), _row_stride(k_new, "k_new", hkv * d)
+        if (k_cache.shape[2] != d or v_cache.shape != k_cache.shape or k_new.shape[1:] != (hkv, d)
+                or v_new.shape != k_new.shape or _row_stride(v_cache, "v_cache", hkv * d) != c_stride
+                or _row_stride(v_new, "v_new", hkv * d) != n_stride):
+            raise QcfError("k/v pairs must match each other and the cache in row shape and row stride")
+    if q_new is not None:
+        hq = q_new.shape[1]
+        hkv = hkv if k_cache is not None else hq
+        q_stride = _row_stride(q_new, "q_new", hq * d)
+        if (q_new.dim() != 3 or q_new.shape[2] != d or q_new.shape[0] != src.shape[0] or q_out.shape != (n, hq, d)
+                or not q_out.is_contiguous()):
+            raise QcfError("q_new must be [n_src_rows, H_q, d] and q_out dense [n_rows, H_q, d]")
+    _here("qcf_rope_store", k_cache=k_cache, v_cache=v_cache, k_new=k_new, v_new=v_new, slots=slots,
+          positions=positions, freq=freq, q_new=q_new, q_out=q_out, src_idx=src_idx)
+    _invoke("qcf_rope_store", _ptr(k_cache), _ptr(v_cache), n_slots, c_stride, _ptr(q_out), _ptr(k_new), _ptr(v_new),
+            n_stride, _ptr(q_new), q_stride, src.shape[0], _ptr(src_idx), _dtype(some), n, _ptr(slots),
+            _ptr(positions), _ptr(freq), 0 if freq is None else 2 * freq.numel(), int(bool(interleaved)),
+            float(magnitude), hq, hkv, d)
+
+
+def qcf_tree_attn_workspace_size(batch, max_q, max_kv, n_q_heads, n_kv_heads, head_dim, dtype=torch.bfloat16):
+    return int(lib().qcf_tree_attn_workspace_size(batch, max_q, max_kv, n_q_heads, n_kv_heads, head_dim, _DT[dtype]))
+
+
+def qcf_tree_attn(out, q, cu_q, k_cache, v_cache, block_table, kv_len, page_size, max_q, max_kv, softmax_scale,
+                  tree_mask=None, lse=None, workspace=None):
+    """Attention of each request's new rows over its pages: all of kv_len, then the new rows' own
+    tokens by the tree mask (int32 [rows, words]) or, without one, up to the row's own."""
+    for name, t in (("out", out), ("k_cache", k_cache), ("v_cache", v_cache)):
+        _dev(t, name, q.dtype)
+    _dev(q, "q")
+    _dev(lse, "lse", torch.float32)
+    stride = _table(block_table)
+    batch = kv_len.numel()
+    _one_or_none(kv_len, "kv_len", batch)
+    _one_or_none(cu_q, "cu_q", batch + 1)
+    _i32(tree_mask, "tree_mask")
+    if q.dim() != 3 or k_cache.dim() != 3 or not (q.is_contiguous() and out.is_contiguous()) or out.shape != q.shape:
+        raise QcfError("q and out must be dense [rows, H_q, d] tensors of the same shape")
+    n, hq, d = q.shape
+    n_slots, hkv, d2 = k_cache.shape
+    rs = _row_stride(k_cache, "k_cache", hkv * d)
+    if v_cache.shape != k_cache.shape or _row_stride(v_cache, "v_cache", hkv * d) != rs or d2 != d:
+        raise QcfError("k_cache and v_cache must match each other and q's head_dim")
+    if block_table.shape[0] != batch:
+        raise QcfError("block_table needs a row per request")
+    if tree_mask is not None and (tree_mask.dim() != 2 or tree_mask.shape[0] != n):
+        raise QcfError("tree_mask must be [rows, words]")
+    if lse is not None and (lse.shape != (n, hq) or not lse.is_contiguous()):
+        raise QcfError("lse must be dense [n_rows, H_q]")
+    _here("qcf_tree_attn", out=out, q=q, cu_q=cu_q, k_cache=k_cache, v_cache=v_cache, block_table=block_table,
+          kv_len=kv_len, tree_mask=tree_mask, lse=lse, workspace=workspace)
+    need = qcf_tree_attn_workspace_size(batch, max_q, max_kv, hq, hkv, d, q.dtype)
+    if workspace is None and need > 0:
+        workspace = torch.empty(need, dtype=torch.uint8, device=q.device)
+    _invoke("qcf_tree_attn", _ptr(out), _ptr(lse), _ptr(q), n, _ptr(cu_q), _ptr(k_cache), _ptr(v_cache), n_slots, rs,
+            _ptr(block_table), stride, block_table.shape[1], int(page_size), _ptr(kv_len), _ptr(tree_mask),
+            0 if tree_mask is None else tree_mask.shape[1], _dtype(q), batch, int(max_q), int(max_kv), hq, hkv, d,
+            float(softmax_scale), _ptr(workspace), 0 if workspace is None else workspace.numel(), keep=workspace)
+
+
+def qcf_verify_drafts_workspace_size(batch, vocab):
+    return int(lib().qcf_verify_drafts_workspace_size(int(batch), int(vocab)))
+
+
+def qcf_verify_drafts(n_out, path, out_tokens, target, tokens, cu_rows, u_accept, u_next, draft=None, parents=None,
+                      slots=None, move_src=None, move_dst=None, workspace=None):
+    """Accepted rows and tokens of each request's drafts (path, out_tokens [batch, max_rows]) and the
+    token after them; with slots also where the accepted rows' keys and values move."""
+    batch, n = n_out.numel(), tokens.numel()
+    for name, t, size in (("n_out", n_out, batch), ("tokens", tokens, n), ("cu_rows", cu_rows, batch + 1),
+                          ("parents", parents, n), ("slots", slots, n)):
+        _one_or_none(t, name, size)
+    for name, t in (("path", path), ("out_tokens", out_tokens), ("move_src", move_src), ("move_dst", move_dst)):
+        _i32(t, name)
+        if t is not None and (t.dim() != 2 or t.shape[0] != batch or t.shape != path.shape):
+            raise QcfError(f"{name} must be [batch, max_rows]")
+    _dev(target, "target")
+    _dev(draft, "draft", target.dtype)
+    for name, t, size in (("u_accept", u_accept, n), ("u_next", u_next, batch)):
+        _dev(t, name, torch.float32)
+        if t.numel() != size or not t.is_contiguous():
+            raise QcfError(f"{name} must be dense with {size} entries")
+    if len({x is None for x in (slots, move_src, move_dst)}) > 1:
+        raise QcfError("slots, move_src and move_dst go together")
+    if target.dim() != 2 or target.shape[0] != n:
+        raise QcfError("target must be [rows, vocab]")
+    vocab = target.shape[1]
+    rs = _row_stride(target, "target", vocab)
+    if draft is not None and (draft.shape != target.shape or _row_stride(draft, "draft", vocab) != rs):
+        raise QcfError("draft must match target in shape and row stride")
+    _here("qcf_verify_drafts", n_out=n_out, path=path, out_tokens=out_tokens, target=target, tokens=tokens,
+          cu_rows=cu_rows, u_accept=u_accept, u_next=u_next, draft=draft, parents=parents, slots=slots,
+          move_src=move_src, move_dst=move_dst, workspace=workspace)
+    need = qcf_verify_drafts_workspace_size(batch, vocab)
+    if workspace is None:
+        workspace = torch.empty(max(need, 1), dtype=torch.uint8, device=target.device)
+    _invoke("qcf_verify_drafts", _ptr(n_out), _ptr(path), _ptr(out_tokens), _ptr(target), _ptr(draft), rs,
+            _dtype(target), n, vocab, _ptr(tokens), _ptr(parents), batch, _ptr(cu_rows), path.shape[1],
+            _ptr(u_accept), _ptr(u_next), _ptr(slots), _ptr(move_src), _ptr(move_dst), _ptr(workspace),
+            workspace.numel(), keep=workspace)
