@@ -1,0 +1,184 @@
+// Device code shared by the kernels of qcf_tree_attn: how the work is cut over blocks, and which of a
+// request's own new rows a row sees.
+//
+// A unit is a tile of query vectors (rows times the heads that share a KV head) of one request and KV
+// head; its work is one step per kt tokens of the request.  Where every block takes one unit there is
+// nothing to plan.  Else the steps of all units, laid end to end (request, KV head, tile), are shared
+// evenly over a fixed number of blocks, whatever the requests' lengths: a block takes its share unit by
+// unit, and a unit that is cut between blocks is merged from float32 partial results.  A block has at most
+// two of them, at the start and at the end of its share (slots 2 x and 2 x + 1).
+#pragma once
+#include "qcf_decode_launch.h"
+#include "qcf_device.h"
+
+namespace qcf {
+
+struct TreeCut {
+  int vt;      // query vectors per unit
+  int kt;      // tokens per step
+  int blocks;  // blocks that share the steps, 0: one block per unit
+  int tiles;   // units of the longest request per KV head
+};
+
+// The workspace of a cut call: prefix[b] is the number of steps before request b
+struct TreeWs {
+  int64_t* prefix;   // [batch + 1]
+  float2* ml;        // [2 * blocks][vt] running maximum (log2 units) and sum
+  float* o;          // [2 * blocks][vt][d]
+};
+
+// a value that is the same in every lane, in scalar registers
+__device__ __forceinline__ int uni(int x) { return __builtin_amdgcn_readfirstlane(x); }
+__device__ __forceinline__ int64_t uni(int64_t x) {
+  return (int64_t)((uint64_t)(uint32_t)uni((int)(x >> 32)) << 32 | (uint32_t)uni((int)x));
+}
+
+struct TreeRequest {
+  int64_t r0;   // first packed row
+  int rows;     // new rows
+  int kv, end;  // tokens before them, tokens in all
+};
+
+__device__ __forceinline__ TreeRequest tree_request(const TreeAttn& p, int b) {
+  TreeRequest q;
+  const int r0 = p.cu_q[b], r1 = p.cu_q[b + 1], kv = p.kv_len[b];
+  q.r0 = r0;
+  q.rows = r0 < 0 ? 0 : (int)max(min(min((int64_t)r1, p.n_rows) - r0, (int64_t)p.max_q), (int64_t)0);
+  q.kv = max(kv, 0);
+  q.end = (int)min((int64_t)q.kv + q.rows, (int64_t)p.max_kv);
+  return q;
+}
+
+// the same for a request that is the same in every lane
+__device__ __forceinline__ TreeRequest tree_request_uni(const TreeAttn& p, int b) {
+  TreeRequest q = tree_request(p, b);
+  q.r0 = uni(q.r0);
+  q.rows = uni(q.rows);
+  q.kv = uni(q.kv);
+  q.end = uni(q.end);
+  return q;
+}
+
+__device__ __forceinline__ int tree_tiles(const TreeRequest& q, int lg, int vt) {
+  return (int)((((int64_t)q.rows << lg) + vt - 1) / vt);
+}
+// steps of one unit: at least one, for the rows that see nothing are written too
+__device__ __forceinline__ int tree_steps(const TreeRequest& q, int kt) { return max((q.end + kt - 1) / kt, 1); }
+
+// The first step of block x's share of n
+__device__ __forceinline__ int64_t tree_share(int64_t n, int x, int blocks) { return n * x / blocks; }
+
+// Blocks in an order that gives each of the 8 XCDs (blocks go to them in turn) consecutive shares:
+// tiles of one request and KV head read the same keys.
+__device__ __forceinline__ int tree_block(int blocks) {
+  const int x = blockIdx.x;
+  return blocks % 8 == 0 ? (x & 7) * (blocks >> 3) + (x >> 3) : x;
+}
+
+// Runs `unit(b, request, g, tile, first, n, steps, slot)` for this block's share: steps first .. first+n-1
+// of a unit's `steps`, to be written out whole (slot < 0) or as a partial result.  NT threads.
+template <int NT, typename F>
+__device__ __forceinline__ void tree_walk(const TreeAttn& p, const TreeCut& cut, const TreeWs& ws, int lg,
+                                          F&& unit) {
+  int b;
+  TreeRequest q;
+  int64_t before, c, s, share1;  // steps before request b, its own; the share's next and last
+  int x = 0;
+  if (cut.blocks == 0) {
+    const int g = blockIdx.x % p.hkv, rest = blockIdx.x / p.hkv;
+    const int tile = rest % cut.tiles;
+    b = rest / cut.tiles;
+    q = tree_request_uni(p, b);
+    const int tiles = tree_tiles(q, lg, cut.vt), steps = tree_steps(q, cut.kt);
+    if (tile >= tiles) return;
+    before = 0;
+    c = (int64_t)p.hkv * tiles * steps;
+    s = (int64_t)(g * tiles + tile) * steps;
+    share1 = s + steps;
+  } else {
+    __shared__ int64_t sum_l[NT + 1];  // steps before each thread's requests
+    __shared__ int64_t wave_l[NT / 64];
+    const int tid = threadIdx.x, lane = tid & 63;
+    const int per = (p.batch + NT - 1) / NT;
+    auto cost = [&](const TreeRequest& r) {
+      return (int64_t)p.hkv * tree_tiles(r, lg, cut.vt) * tree_steps(r, cut.kt);
+    };
+    int64_t own = 0;
+    for (int i = tid * per; i < min((tid + 1) * per, p.batch); ++i) own += cost(tree_request(p, i));
+    int64_t sum = own;
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+      const int64_t y = __shfl_up(sum, o, 64);
+      if (lane >= o) sum += y;
+    }
+    if (lane == 63) wave_l[tid >> 6] = sum;
+    __syncthreads();
+    for (int i = 0; i < tid >> 6; ++i) sum += wave_l[i];
+    sum_l[tid] = sum - own;
+    if (tid == NT - 1) sum_l[NT] = sum;
+    if (blockIdx.x == 0) {
+      int64_t at = sum - own;
+      for (int i = tid * per; i < min((tid + 1) * per, p.batch); ++i) {
+        ws.prefix[i] = at;
+        at += cost(tree_request(p, i));
+      }
+      if (tid == NT - 1) ws.prefix[p.batch] = sum;
+    }
+    __syncthreads();
+    const int64_t all = uni(sum_l[NT]);
+    x = tree_block(cut.blocks);
+    s = tree_share(all, x, cut.blocks);
+    share1 = tree_share(all, x + 1, cut.blocks);
+    if (s >= share1) return;
+    int lo = 0, hi = NT;  // the last thread whose requests start at or before s
+    while (hi - lo > 1) {
+      const int mid = (lo + hi) >> 1;
+      if (uni(sum_l[mid]) <= s) lo = mid; else hi = mid;
+    }
+    b = lo * per;
+    before = uni(sum_l[lo]);
+    q = tree_request_uni(p, b);
+    c = cost(q);
+  }
+  const int64_t share0 = s;
+  while (s < share1) {
+    while (before + c <= s) {  // (ends: the requests' costs sum to more than s)
+      before += c;
+      q = tree_request_uni(p, ++b);
+      c = (int64_t)p.hkv * tree_tiles(q, lg, cut.vt) * tree_steps(q, cut.kt);
+    }
+    const int steps = tree_steps(q, cut.kt), tiles = tree_tiles(q, lg, cut.vt);
+    const int64_t u = (s - before) / steps;
+    const int first = (int)(s - before - u * steps);
+    const int n = (int)min((int64_t)(steps - first), share1 - s);
+    const int slot = n == steps ? -1 : 2 * x + (s - first < share0 ? 0 : 1);
+    unit(b, q, (int)(u / tiles), (int)(u % tiles), first, n, steps, slot);
+    s += n;
+  }
+}
+
+// Bits of the W (<= 32) tokens from t0 on that row `row` (index i of its request) sees, as far as the new
+// rows' own tokens go; the tokens before them are all seen.  Tokens at and behind `end` are not.
+template <int W>
+__device__ __forceinline__ uint32_t tree_sees(const TreeAttn& p, const TreeRequest& q, int64_t row, int i, int t0) {
+  constexpr uint32_t kAll = W == 32 ? 0xffffffffu : (1u << W) - 1u;
+  const int left = q.end - t0;  // > 0
+  const uint32_t in = left >= W ? kAll : (1u << left) - 1u;
+  const int j = t0 - q.kv;  // index of the first token among the new rows' own
+  if (j + W <= 0) return in;
+  uint32_t own;
+  if (p.tree_mask) {
+    const uint32_t* m = p.tree_mask + row * p.mask_words;
+    const int w = j >> 5, sh = j & 31;  // (rounds down: w = -1 for -32 <= j < 0)
+    const uint64_t lo = w >= 0 && w < p.mask_words ? m[w] : 0u;
+    const uint64_t hi = w + 1 >= 0 && w + 1 < p.mask_words ? m[w + 1] : 0u;
+    own = (uint32_t)((hi << 32 | lo) >> sh);
+  } else {
+    const int n = i - j + 1;  // tokens j .. i
+    own = n <= 0 ? 0u : n >= 32 ? 0xffffffffu : (1u << n) - 1u;
+  }
+  if (j < 0) own |= (1u << -j) - 1u;  // (-j < W <= 32)
+  return own & in;
+}
+
+}  // namespace qcf

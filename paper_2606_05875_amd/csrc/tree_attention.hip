@@ -1,106 +1,808 @@
-// Attention of each request's new rows over its paged cache (qcf_tree_attn).
+// Attention of each request's new rows over its paged cache (qcf_tree_attn), bf16.
 //
-// One wave per row and query head, 64 tokens at a time: a lane holds one token's logit, then the
-// weights go round the wave and a lane sums its output columns.  The softmax is online (running
-// maximum and sum).
+// With the softmax's running maximum m and sum l per query vector, one pass over the tokens suffices:
+// S = K Q^T, p = exp2(S - m), O = O alpha + V^T p^T.  Products are transposed, as in the other attention
+// kernels of this library: a lane holds tokens' logits of ONE query vector, so its p are the second
+// product's operand as they stand.
+//
+// Keys and values go from the pages into LDS without passing registers (16 bytes per lane); the
+// block table's entries come through the scalar cache, one per 16 tokens, a step ahead.
+//  narrow  up to 32 query vectors per request and KV head (one token, short chains).  Bound: HBM.  Four
+//          waves take 16-token tiles in turn, each on its own (two stages of LDS, no barrier in the loop),
+//          v_mfma_f32_16x16x32/16x16x16_bf16; their results are summed through LDS once per unit.
+//  wide    more vectors (trees).  A wave holds 32 of them (v_mfma_f32_32x32x16_bf16) and the 2 to 8
+//          waves of a block share every 32-token tile (three stages, one barrier per tile).  Bound: HBM
+//          up to about 128 vectors, the matrix units beyond.
 #include <math.h>
 
-#include "qcf_decode_launch.h"
-#include "qcf_device.h"
+#include <algorithm>
+
+#include "qcf_attn.h"
+#include "qcf_tree.h"
 
 namespace qcf {
 namespace {
 
-constexpr int kWaves = 4;
+typedef short v4s __attribute__((ext_vector_type(4)));
+typedef v4s __attribute__((address_space(3))) * lds_v4s;
+typedef const int32_t __attribute__((address_space(4))) * const_i32;
 
-__device__ __forceinline__ float to_f(float x) { return x; }
-__device__ __forceinline__ float to_f(uint16_t x) { return bf2f(x); }
-__device__ __forceinline__ void store_as(float* p, float x) { *p = x; }
-__device__ __forceinline__ void store_as(uint16_t* p, float x) { *p = f2bf(x); }
+// 16 bytes per lane from base + off into LDS at byte address lds + 16 * lane, past the registers and
+// without a wait of the compiler's (the caller counts)
+__device__ __forceinline__ void copy16(const void* base, uint32_t off, uint32_t lds) {
+  const uint32_t la = __builtin_amdgcn_readfirstlane(lds);
+  asm volatile("s_mov_b32 m0, %0\n\tglobal_load_lds_dwordx4 %1, %2" : : "s"(la), "v"(off), "s"(uni((int64_t)base)) : "memory");
+}
+__device__ __forceinline__ void copy16(const void* from, uint32_t lds) {
+  const uint32_t la = __builtin_amdgcn_readfirstlane(lds);
+  asm volatile("s_mov_b32 m0, %0\n\tglobal_load_lds_dwordx4 %1, off" : : "s"(la), "v"(from) : "memory");
+}
 
+// a running maximum as the reference of exponentials: 0 while nothing has been seen
+__device__ __forceinline__ float finite(float m) { return m == -INFINITY ? 0.f : m; }
+
+// exp2(s * scale2 - ref).  The fused form keeps the product exact, but its difference to the rounded
+// maximum reaches 2^-24 of that, too much to be an exponent where maxima pass 2^28 (`big`).
+__device__ __forceinline__ float weight(float s, float scale2, float ref, bool big) {
+#pragma clang fp contract(off)
+  const float x = s * scale2;
+  return __builtin_amdgcn_exp2f(big ? x - ref : fmaf(s, scale2, -ref));
+}
+__device__ __forceinline__ bool is_big(float m) { return __ballot(fabsf(finite(m)) > 0x1p28f) != 0; }
+
+// any of a 16-byte piece's 8 values infinite or NaN
+__device__ __forceinline__ bool not_finite(const uint4& x) {
+  const uint32_t w[4] = {x.x, x.y, x.z, x.w};
+  bool bad = false;
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+    bad = bad || (w[i] & 0x7f80u) == 0x7f80u || (w[i] & 0x7f800000u) == 0x7f800000u;
+  return bad;
+}
+
+// The page of 16 tokens from t0 on (t0 a multiple of 16, pages of 16 rows and more), or -1
+__device__ __forceinline__ int page_of(const TreeAttn& p, const_i32 table, int t0, int end) {
+  const int pg = t0 >> p.page_log2;
+  if (t0 >= end || pg >= p.max_pages) return -1;
+  const int page = uni(table[pg]);
+  return page < p.n_pages ? max(page, -1) : -1;
+}
+
+// Pages of fewer than 16 rows: the slot of a lane's token, or -1
+__device__ __forceinline__ int64_t slot_of(const TreeAttn& p, int b, int t, int end) {
+  const int pg = t >> p.page_log2;
+  if (t >= end || pg >= p.max_pages) return -1;
+  const int page = p.block_table[b * p.table_stride + pg];
+  return page >= 0 && page < p.n_pages ? ((int64_t)page << p.page_log2) + (t & ((1 << p.page_log2) - 1)) : -1;
+}
+
+// ---------------------------------------------------------------------------
+// narrow
+// ---------------------------------------------------------------------------
+constexpr int kNW = 4;   // waves
+constexpr int kNT = 16;  // tokens per wave and step
+
+template <int D, int NV, bool kTiny>
+__global__ __launch_bounds__(kNW * 64, 2) void tree_attn_narrow_kernel(TreeAttn p, TreeCut cut, TreeWs ws, int lg) {
+  constexpr int CH = D / 8;          // 16-byte chunks per row
+  constexpr int RPC = 64 / CH;       // rows per copy
+  constexpr int RB = D * 2;          // bytes per row
+  constexpr int TB = kNT * RB;       // bytes of a tile of K or V
+  constexpr int TC = kNT / RPC;      // copies per tile of K or V
+  constexpr int MB = D / 16, ST = D / 32;
+  constexpr int VT = 16 * NV;
+  __shared__ __attribute__((aligned(1024))) uint8_t ring[kNW * 4 * TB];  // per wave: K, V of two stages
+  __shared__ float2 ml_l[kNW][VT];
+  static_assert(kNW * VT * D * 4 <= (int)sizeof(ring), "the waves' O fit");
+
+  const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int l = threadIdx.x & 63, ln = l & 15, lk = l >> 4;
+  uint8_t* mine = ring + w * 4 * TB;
+  const uint32_t lds0 = lds_addr(mine);
+  const uint32_t row_b = (uint32_t)(p.kv_stride * 2);
+  const float scale2 = p.scale * kLog2e;
+
+  // copy i of a tile fills rows RPC i + l / CH; chunk c of K row r sits at c ^ r (D = 64: r / 2), of V row r
+  // at c ^ 2 (r % 8) (D = 64: 2 (r / 2 % 4)): the fragment reads below are free of conflicts
+  uint32_t koff[TC], voff[TC];
+#pragma unroll
+  for (int i = 0; i < TC; ++i) {
+    const int r = RPC * i + l / CH, c = l % CH;
+    koff[i] = r * row_b + (c ^ (D == 128 ? r : r >> 1)) * 16;
+    voff[i] = r * row_b + (c ^ (D == 128 ? 2 * (r & 7) : 2 * ((r >> 1) & 3))) * 16;
+  }
+  const int krd = ln * RB, ksw = D == 128 ? ln : ln >> 1;
+  const int vr = 4 * lk + ((l >> 2) & 3);  // V row this lane reads for the transposing read
+  const int vrd = vr * RB + 8 * (l & 3), vsw = D == 128 ? vr & 7 : (vr >> 1) & 3;
+
+  tree_walk<kNW * 64>(p, cut, ws, lg, [&](int b, const TreeRequest& rq, int g, int tile, int first, int n,
+                                          int steps, int slot) {
+    const_i32 table = (const_i32)(p.block_table + b * p.table_stride);
+    const uint16_t* kc = static_cast<const uint16_t*>(p.k_cache) + (int64_t)g * D;
+    const uint16_t* vc = static_cast<const uint16_t*>(p.v_cache) + (int64_t)g * D;
+    const int t_first = (first * kNW + w) * kNT;  // this wave's first token; the next ones follow kNW * kNT on
+    constexpr int kHop = kNW * kNT;
+
+    bf16x8 qf[NV][ST];
+    int64_t row[NV];
+    int idx[NV], head[NV];
+    bool valid[NV];
+#pragma unroll
+    for (int c = 0; c < NV; ++c) {
+      const int v = tile * VT + 16 * c + ln;
+      idx[c] = v >> lg;
+      head[c] = (g << lg) + (v & ((1 << lg) - 1));
+      valid[c] = idx[c] < rq.rows;
+      row[c] = rq.r0 + min(idx[c], rq.rows - 1);
+      const uint16_t* q = static_cast<const uint16_t*>(p.q) + (row[c] * p.hq + head[c]) * D + 8 * lk;
+#pragma unroll
+      for (int st = 0; st < ST; ++st) qf[c][st] = as_bf16x8(ld16(q + 32 * st));
+    }
+    // Q has to be there before the loop: a wait for it inside would count the copies in flight
+#pragma unroll
+    for (int c = 0; c < NV; ++c)
+#pragma unroll
+      for (int st = 0; st < ST; ++st) asm volatile("" : "+v"(qf[c][st]));
+
+    f32x4 o[NV][MB];
+    float m[NV], ls[NV];  // running maximum in log2 units, this lane's part of the sum
+    bool big[NV];
+#pragma unroll
+    for (int c = 0; c < NV; ++c) {
+      big[c] = false;
+      m[c] = -INFINITY;
+      ls[c] = 0.f;
+#pragma unroll
+      for (int mb = 0; mb < MB; ++mb) o[c][mb] = f32x4{};
+    }
+
+    // K and V of the tile at t0 into stage s; returns the rows that hold a token, as bits
+    auto copy_tile = [&](int t0, int page, int s) {
+      const uint32_t lk0 = lds0 + s * 2 * TB, lv0 = lk0 + TB;
+      if (!kTiny) {
+        const int64_t base = ((int64_t)max(page, 0) << p.page_log2) + (t0 & ((1 << p.page_log2) - 1));
+        const uint16_t* kb = kc + (page < 0 ? 0 : base) * p.kv_stride;
+        const uint16_t* vb = vc + (page < 0 ? 0 : base) * p.kv_stride;
+#pragma unroll
+        for (int i = 0; i < TC; ++i) copy16(kb, koff[i], lk0 + i * 1024);
+#pragma unroll
+        for (int i = 0; i < TC; ++i) copy16(vb, voff[i], lv0 + i * 1024);
+      } else {
+#pragma unroll
+        for (int i = 0; i < TC; ++i) {
+          const int r = RPC * i + l / CH;
+          const int64_t at = max(slot_of(p, b, t0 + r, rq.end), (int64_t)0) * p.kv_stride;
+          copy16(kc + at + (koff[i] - r * row_b) / 2, lk0 + i * 1024);
+          copy16(vc + at + (voff[i] - r * row_b) / 2, lv0 + i * 1024);
+        }
+      }
+    };
+    auto page_at = [&](int i) { return kTiny || i >= n ? -1 : page_of(p, table, t_first + i * kHop, rq.end); };
+
+    // the rows of a page are there even where a page ends the pool, so a whole tile can be copied; without
+    // a page the pool's first rows stand in and are not seen
+    const bool pool = p.n_pages > 0 && (kTiny || p.page_log2 >= 4);
+    int page = page_at(0), page1 = page_at(1);
+    if (pool) copy_tile(t_first, page, 0);
+    for (int i = 0; i < n && pool; ++i) {
+      const int t0 = t_first + i * kHop;
+      asm volatile("" ::: "memory");
+      __builtin_amdgcn_s_waitcnt(0xc07f);  // the last tile's LDS reads are done (lgkmcnt 0) before it is overwritten
+      if (i + 1 < n) copy_tile(t0 + kHop, page1, (i + 1) & 1);
+      const int page2 = page_at(i + 2);
+      if (i + 1 < n) wait_vm_lgkm0<2 * TC>();
+      else wait_vm_lgkm0<0>();
+      asm volatile("" ::: "memory");
+      uint8_t* kl = mine + (i & 1) * 2 * TB;
+      uint8_t* vl = kl + TB;
+
+      f32x4 s[NV];
+#pragma unroll
+      for (int c = 0; c < NV; ++c) s[c] = f32x4{};
+#pragma unroll
+      for (int st = 0; st < ST; ++st) {
+        const bf16x8 kf = as_bf16x8(ld16(kl + krd + (((4 * st + lk) ^ ksw) * 16)));
+#pragma unroll
+        for (int c = 0; c < NV; ++c)
+          s[c] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, qf[c][st], s[c], 0, 0, 0);
+      }
+      // lane value r of s is token t0 + 4 lk + r
+      uint32_t sees[NV];
+      uint32_t loose = 0;  // tokens whose values are added one by one
+      bool edge = t0 + kNT > min(rq.kv, rq.end) || (!kTiny && page < 0);
+      uint32_t held = 0xffffu;
+      if (kTiny) {
+        held = (uint32_t)__ballot(slot_of(p, b, t0 + ln, rq.end) >= 0) & 0xffffu;
+        edge = edge || held != 0xffffu;
+      }
+      if (edge) {
+        if (t0 >= rq.end || (!kTiny && page < 0)) held = 0;
+        else if (rq.end - t0 < kNT) held &= (1u << (rq.end - t0)) - 1u;
+#pragma unroll
+        for (int c = 0; c < NV; ++c) {
+          sees[c] = held ? tree_sees<16>(p, rq, row[c], idx[c], t0) & held : 0u;
+#pragma unroll
+          for (int r = 0; r < 4; ++r)
+            if (!(sees[c] >> (4 * lk + r) & 1)) s[c][r] = -INFINITY;
+        }
+        // a value that a row does not see must not meet its weight 0 where it is not finite: rows that
+        // hold no token become zeros, and tokens with such values (rare) are taken out and added to the
+        // rows that see them
+#pragma unroll
+        for (int i4 = 0; i4 < TC; ++i4) {
+          const int r = RPC * i4 + l / CH;
+          uint8_t* at = vl + i4 * 1024 + 16 * l;
+          const bool drop = !(held >> r & 1);
+          const uint64_t bad = __ballot(!drop && not_finite(ld16(at)));
+#pragma unroll
+          for (int k = 0; k < RPC; ++k)
+            if (bad >> (k * CH) & (CH == 16 ? 0xffffull : 0xffull)) loose |= 1u << (RPC * i4 + k);
+          if (drop) st16(at, make_uint4(0, 0, 0, 0));
+        }
+        asm volatile("" ::: "memory");
+      }
+      v4s pb[NV];
+      float pw[NV][4];
+#pragma unroll
+      for (int c = 0; c < NV; ++c) {
+        float mt = fmaxf(fmaxf(s[c][0], s[c][1]), fmaxf(s[c][2], s[c][3])) * scale2;
+        // lazy rescale: a stale maximum stays unless the vector's grew by more than 2^8 (by each
+        // vector's own, so that no row's bits hang on another's)
+        if (__ballot(mt > m[c] + 8.f)) {
+          mt = fmaxf(mt, __shfl_xor(mt, 16, 64));
+          mt = fmaxf(mt, __shfl_xor(mt, 32, 64));
+          const float mn = mt > m[c] + 8.f ? mt : m[c];
+          const float alpha = __builtin_amdgcn_exp2f(m[c] - finite(mn));
+          ls[c] *= alpha;
+#pragma unroll
+          for (int mb = 0; mb < MB; ++mb) o[c][mb] *= alpha;
+          m[c] = mn;
+          big[c] = is_big(mn);
+        }
+        const float ref = finite(m[c]);
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          pw[c][r] = weight(s[c][r], scale2, ref, big[c]);
+          pb[c][r] = (short)f2bf(pw[c][r]);
+        }
+        ls[c] += (pw[c][0] + pw[c][1]) + (pw[c][2] + pw[c][3]);
+      }
+      if (loose) {
+        for (uint32_t left = loose; left; left &= left - 1) {
+          const int k = __builtin_ctz(left);
+#pragma unroll
+          for (int c = 0; c < NV; ++c) {
+            const float a = k & 2 ? (k & 1 ? pw[c][3] : pw[c][2]) : (k & 1 ? pw[c][1] : pw[c][0]);
+            const float pk = __shfl(a, (k >> 2) * 16 + ln, 64);
+            if (sees[c] >> k & 1) {
+              const int sw = D == 128 ? k & 7 : (k >> 1) & 3;
+#pragma unroll
+              for (int mb = 0; mb < MB; ++mb) {
+                const uint16_t* v = reinterpret_cast<const uint16_t*>(vl + k * RB + ((mb ^ sw) << 5) + 8 * lk);
+#pragma unroll
+                for (int r = 0; r < 4; ++r) o[c][mb][r] = fmaf(pk, bf2f(v[r]), o[c][mb][r]);
+              }
+            }
+          }
+        }
+        asm volatile("" ::: "memory");
+#pragma unroll
+        for (int i4 = 0; i4 < TC; ++i4)
+          if (loose >> (RPC * i4 + l / CH) & 1) st16(vl + i4 * 1024 + 16 * l, make_uint4(0, 0, 0, 0));
+        asm volatile("" ::: "memory");
+      }
+#pragma unroll
+      for (int mb = 0; mb < MB; ++mb) {
+        const v4s va = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4s)(vl + vrd + ((mb ^ vsw) << 5)));
+#pragma unroll
+        for (int c = 0; c < NV; ++c) o[c][mb] = __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(va, pb[c], o[c][mb], 0, 0, 0);
+      }
+      page = page1;
+      page1 = page2;
+    }
+
+    // the waves' results, summed in their order: vector v's columns 4 i .. + 3 at i ^ (v % 8)
+    __syncthreads();  // every wave has read its tiles
+    float4* o_l = reinterpret_cast<float4*>(ring);
+#pragma unroll
+    for (int c = 0; c < NV; ++c) {
+      ls[c] += __shfl_xor(ls[c], 16, 64);
+      ls[c] += __shfl_xor(ls[c], 32, 64);
+      const int v = 16 * c + ln;
+      if (lk == 0) ml_l[w][v] = make_float2(m[c], ls[c]);
+#pragma unroll
+      for (int mb = 0; mb < MB; ++mb)
+        o_l[(w * VT + v) * (D / 4) + ((4 * mb + lk) ^ (v & 7))] = make_float4(o[c][mb][0], o[c][mb][1], o[c][mb][2], o[c][mb][3]);
+    }
+    __syncthreads();
+    for (int u = threadIdx.x; u < VT * (D / 4); u += kNW * 64) {
+      const int v = u / (D / 4), i4 = u % (D / 4);
+      const int vec = tile * VT + v, i = vec >> lg;
+      if (i >= rq.rows) continue;
+      float2 ml[kNW];
+      float mx = -INFINITY, lt = 0.f;
+#pragma unroll
+      for (int k = 0; k < kNW; ++k) {
+        ml[k] = ml_l[k][v];
+        mx = fmaxf(mx, ml[k].x);
+      }
+      float4 a = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+      for (int k = 0; k < kNW; ++k) {
+        const float f = __builtin_amdgcn_exp2f(ml[k].x - finite(mx));
+        const float4 x = o_l[(k * VT + v) * (D / 4) + (i4 ^ (v & 7))];
+        lt += f * ml[k].y;
+        a.x += f * x.x;
+        a.y += f * x.y;
+        a.z += f * x.z;
+        a.w += f * x.w;
+      }
+      if (slot >= 0) {
+        reinterpret_cast<float4*>(ws.o)[((int64_t)slot * VT + v) * (D / 4) + i4] = a;
+        if (i4 == 0) ws.ml[(int64_t)slot * VT + v] = make_float2(mx, lt);
+      } else {
+        const int64_t at = (rq.r0 + i) * p.hq + (g << lg) + (vec & ((1 << lg) - 1));
+        const bool none = mx == -INFINITY;
+        const float inv = none ? 0.f : 1.f / lt;
+        *reinterpret_cast<uint2*>(static_cast<uint16_t*>(p.out) + at * D + 4 * i4) =
+            make_uint2(pack_bf16x2(a.x * inv, a.y * inv), pack_bf16x2(a.z * inv, a.w * inv));
+        if (p.lse && i4 == 0) p.lse[at] = none ? -INFINITY : (mx + log2f(lt)) * kLn2;
+      }
+    }
+    __syncthreads();  // (the next unit's tiles go over them)
+  });
+}
+
+// ---------------------------------------------------------------------------
+// wide
+// ---------------------------------------------------------------------------
+constexpr int kWT = 32;  // tokens per step
+constexpr int kWStages = 3;
+
+template <int D, int VG, bool kTiny>
+__global__ __launch_bounds__(VG * 64, 2) void tree_attn_wide_kernel(TreeAttn p, TreeCut cut, TreeWs ws, int lg) {
+  constexpr int CH = D / 8;              // 16-byte chunks per row
+  constexpr int RPC = 64 / CH;           // rows per copy
+  constexpr int RB = D * 2;              // bytes per row
+  constexpr int TB = kWT * RB;           // bytes of a tile of K or V
+  constexpr int TC = kWT / RPC;          // copies per tile of K or V
+  constexpr int WC = (TC + VG - 1) / VG;  // per wave (the last ones may be made twice)
+  constexpr int VT = 32 * VG;
+  __shared__ __attribute__((aligned(1024))) uint8_t ring[kWStages * 2 * TB];
+  __shared__ uint32_t loose_l;
+
+  const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int l = threadIdx.x & 63, lq = l & 31, hi = l >> 5;
+  const uint32_t lds0 = lds_addr(ring);
+  const uint32_t row_b = (uint32_t)(p.kv_stride * 2);
+  const float scale2 = p.scale * kLog2e;
+  // Chunk c of K row r sits at c ^ (r % 16) (D = 64: c ^ (r / 2 % 8)), of V row r at c ^ 4 (r % 4)
+  // (D = 64: c ^ 4 (r / 2 % 2)): lane fragments st at krd ^ (st << 5), V column blocks mb at vrd ^ (mb << 6)
+  const int ky = D == 128 ? lq & 15 : (lq >> 1) & 7;
+  const int krd = lq * RB + (hi ^ (ky & 1)) * 16 + (ky >> 1) * 32;
+  const int tg = l >> 4, te = (l >> 2) & 3, tq = l & 3;
+  const int vrd = (4 * (tg >> 1) + te) * RB + (D == 128 ? te : te >> 1) * 64 + 32 * (tg & 1) + 8 * tq;
+  int cp[WC];  // this wave's copies of a tile
+  uint32_t koff[WC], voff[WC];
+#pragma unroll
+  for (int i = 0; i < WC; ++i) {
+    cp[i] = min(w + VG * i, TC - 1);
+    const int r = RPC * cp[i] + l / CH, c = l % CH;
+    koff[i] = (r & 15) * row_b + (c ^ (D == 128 ? r & 15 : (r >> 1) & 7)) * 16;
+    voff[i] = (r & 15) * row_b + (c ^ (4 * (D == 128 ? r & 3 : (r >> 1) & 1))) * 16;
+  }
+
+  tree_walk<VG * 64>(p, cut, ws, lg, [&](int b, const TreeRequest& rq, int g, int tile, int first, int n,
+                                         int steps, int slot) {
+    const_i32 table = (const_i32)(p.block_table + b * p.table_stride);
+    const uint16_t* kc = static_cast<const uint16_t*>(p.k_cache) + (int64_t)g * D;
+    const uint16_t* vc = static_cast<const uint16_t*>(p.v_cache) + (int64_t)g * D;
+    const int v0 = tile * VT + 32 * w;
+    const int idx = (v0 + lq) >> lg;
+    const int head = (g << lg) + ((v0 + lq) & ((1 << lg) - 1));
+    const bool valid = idx < rq.rows;
+    const bool busy = (v0 >> lg) < rq.rows;  // (the wave has a vector)
+    const int64_t row = rq.r0 + min(idx, rq.rows - 1);
+    bf16x8 qreg[D / 16];
+    {
+      const uint16_t* q = static_cast<const uint16_t*>(p.q) + (row * p.hq + head) * D + 8 * hi;
+#pragma unroll
+      for (int st = 0; st < D / 16; ++st) qreg[st] = as_bf16x8(ld16(q + 16 * st));
+    }
+#pragma unroll
+    for (int st = 0; st < D / 16; ++st) asm volatile("" : "+v"(qreg[st]));
+    f32x16 o[D / 32];
+#pragma unroll
+    for (int mb = 0; mb < D / 32; ++mb) o[mb] = f32x16{};
+    float m = -INFINITY, ls = 0.f;
+    bool big = false;
+
+    const bool pool = p.n_pages > 0 && (kTiny || p.page_log2 >= 4);
+    const int t_first = first * kWT;
+    auto page_at = [&](int i, int half) {
+      return kTiny || i >= n ? -1 : page_of(p, table, t_first + i * kWT + 16 * half, rq.end);
+    };
+    auto copy_tile = [&](int t0, int page_a, int page_b, int s) {
+      const uint32_t lk0 = lds0 + s * 2 * TB, lv0 = lk0 + TB;
+#pragma unroll
+      for (int i = 0; i < WC; ++i) {
+        if (!kTiny) {
+          const bool half = RPC * cp[i] >= 16;
+          const int page = half ? page_b : page_a, t = t0 + (half ? 16 : 0);
+          const int64_t at = page < 0 ? 0 : ((int64_t)page << p.page_log2) + (t & ((1 << p.page_log2) - 1));
+          copy16(kc + at * p.kv_stride, koff[i], lk0 + cp[i] * 1024);
+          copy16(vc + at * p.kv_stride, voff[i], lv0 + cp[i] * 1024);
+        } else {
+          const int r = RPC * cp[i] + l / CH;
+          const int64_t at = max(slot_of(p, b, t0 + r, rq.end), (int64_t)0) * p.kv_stride;
+          copy16(kc + at + (koff[i] - (r & 15) * row_b) / 2, lk0 + cp[i] * 1024);
+          copy16(vc + at + (voff[i] - (r & 15) * row_b) / 2, lv0 + cp[i] * 1024);
+        }
+      }
+    };
+    // pages of tile i and the two after it
+    int pa[3], pb_[3];
+#pragma unroll
+    for (int k = 0; k < 3; ++k) {
+      pa[k] = page_at(k, 0);
+      pb_[k] = page_at(k, 1);
+    }
+    if (pool) {
+      copy_tile(t_first, pa[0], pb_[0], 0);
+      if (n > 1) copy_tile(t_first + kWT, pa[1], pb_[1], 1);
+    }
+    int stage = 0;
+    for (int i = 0; i < n && pool; ++i) {
+      const int t0 = t_first + i * kWT;
+      // this wave's copies of tile i are complete, then everyone's, and everyone has read tile i - 1
+      asm volatile("" ::: "memory");
+      if (i + 1 < n) wait_vm_lgkm0<2 * WC>();
+      else wait_vm_lgkm0<0>();
+      __builtin_amdgcn_s_barrier();
+      asm volatile("" ::: "memory");
+      if (i + 2 < n) copy_tile(t0 + 2 * kWT, pa[2], pb_[2], stage == 0 ? 2 : stage - 1);
+      uint8_t* kl = ring + stage * 2 * TB;
+      uint8_t* vl = kl + TB;
+      stage = stage == kWStages - 1 ? 0 : stage + 1;
+      const int page_a = pa[0], page_b = pb_[0];
+      pa[0] = pa[1];
+      pb_[0] = pb_[1];
+      pa[1] = pa[2];
+      pb_[1] = pb_[2];
+      pa[2] = page_at(i + 3, 0);
+      pb_[2] = page_at(i + 3, 1);
+
+      // tokens of the tile that there are, as bits (the same for the whole block)
+      uint32_t held = 0xffffffffu;
+      if (kTiny) held = (uint32_t)__ballot(slot_of(p, b, t0 + lq, rq.end) >= 0);
+      else held = (page_a < 0 ? 0u : 0xffffu) | (page_b < 0 ? 0u : 0xffff0000u);
+      if (rq.end - t0 < kWT) held &= rq.end > t0 ? (1u << (rq.end - t0)) - 1u : 0u;
+      const bool edge = t0 + kWT > rq.kv || held != 0xffffffffu;
+      uint32_t loose = 0;
+      if (edge) {
+        // rows that hold no token become zeros; tokens with a value that is not finite are taken out
+        // and added to the rows that see them (see the narrow kernel)
+        if (threadIdx.x == 0) loose_l = 0;
+        __syncthreads();
+        for (int u = threadIdx.x; u < TC * 64; u += VG * 64) {
+          const int r = u / CH;
+          if (!(held >> r & 1)) st16(vl + 16 * u, make_uint4(0, 0, 0, 0));
+          else if (not_finite(ld16(vl + 16 * u))) atomicOr(&loose_l, 1u << r);
+        }
+        __syncthreads();
+        loose = loose_l;
+      }
+      if (busy || loose) {
+        f32x16 s = f32x16{};
+#pragma unroll
+        for (int st = 0; st < D / 16; ++st)
+          s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(ld16(kl + (krd ^ (st << 5)))), qreg[st], s, 0, 0, 0);
+        // lane value v is token t0 + 8 (v >> 2) + 4 hi + (v & 3)
+        uint32_t sees = 0xffffffffu;
+        if (edge) {
+          sees = rq.end > t0 ? tree_sees<32>(p, rq, row, idx, t0) & held : 0u;
+#pragma unroll
+          for (int v = 0; v < 16; ++v)
+            if (!(sees >> (8 * (v >> 2) + 4 * hi + (v & 3)) & 1)) s[v] = -INFINITY;
+        }
+        float mt = s[0];
+#pragma unroll
+        for (int v = 1; v < 16; ++v) mt = fmaxf(mt, s[v]);
+        mt *= scale2;
+        if (__ballot(mt > m + 8.f)) {
+          mt = fmaxf(mt, __shfl_xor(mt, 32, 64));
+          const float mn = mt > m + 8.f ? mt : m;
+          const float alpha = __builtin_amdgcn_exp2f(m - finite(mn));
+          ls *= alpha;
+#pragma unroll
+          for (int mb = 0; mb < D / 32; ++mb) o[mb] *= alpha;
+          m = mn;
+          big = is_big(mn);
+        }
+        const float ref = finite(m);
+        bf16x8 pv[2];
+        float psum = 0.f, pw[16];
+#pragma unroll
+        for (int v = 0; v < 16; ++v) {
+          pw[v] = weight(s[v], scale2, ref, big);
+          psum += pw[v];
+          pv[v >> 3][v & 7] = (__bf16)pw[v];
+        }
+        ls += psum;
+        if (loose) {
+          for (uint32_t left = loose; left; left &= left - 1) {
+            const int k = __builtin_ctz(left);
+            float a = 0.f;
+#pragma unroll
+            for (int v = 0; v < 16; ++v) a = (k >> 3) * 4 + (k & 3) == v ? pw[v] : a;
+            const float pk = __shfl(a, ((k >> 2) & 1) * 32 + lq, 64);
+            if (sees >> k & 1) {
+              const int sw = D == 128 ? k & 3 : (k >> 1) & 1;
+#pragma unroll
+              for (int mb = 0; mb < D / 32; ++mb)
+#pragma unroll
+                for (int c = 0; c < 4; ++c) {
+                  // columns 32 mb + 8 c + 4 hi .. + 3: half of chunk 4 mb + c
+                  const uint16_t* x = reinterpret_cast<const uint16_t*>(vl + k * RB + (((4 * mb + c) ^ (4 * sw)) * 16) + 8 * hi);
+#pragma unroll
+                  for (int e = 0; e < 4; ++e) o[mb][4 * c + e] = fmaf(pk, bf2f(x[e]), o[mb][4 * c + e]);
+                }
+            }
+          }
+          __syncthreads();  // everyone has read them (loose is the block's)
+          for (int u = threadIdx.x; u < TC * 64; u += VG * 64)
+            if (loose >> (u / CH) & 1) st16(vl + 16 * u, make_uint4(0, 0, 0, 0));
+          __syncthreads();
+        }
+#pragma unroll
+        for (int k2 = 0; k2 < 2; ++k2)
+#pragma unroll
+          for (int mb = 0; mb < D / 32; ++mb) {
+            const uint8_t* at = vl + 16 * k2 * RB + (vrd ^ (mb << 6));
+            const v4s lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4s)(at));
+            const v4s up = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4s)(at + 8 * RB));
+            const bf16x8 va = __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, up, 0, 1, 2, 3, 4, 5, 6, 7));
+            o[mb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(va, pv[k2], o[mb], 0, 0, 0);
+          }
+      }
+    }
+    ls += __shfl_xor(ls, 32, 64);
+    if (valid) {
+      const bool none = m == -INFINITY;
+      if (slot >= 0) {
+        const int64_t at = (int64_t)slot * VT + 32 * w + lq;
+        if (hi == 0) ws.ml[at] = make_float2(m, ls);
+#pragma unroll
+        for (int mb = 0; mb < D / 32; ++mb)
+#pragma unroll
+          for (int c = 0; c < 4; ++c)
+            reinterpret_cast<float4*>(ws.o)[at * (D / 4) + 8 * mb + 2 * c + hi] =
+                make_float4(o[mb][4 * c], o[mb][4 * c + 1], o[mb][4 * c + 2], o[mb][4 * c + 3]);
+      } else {
+        const float inv = none ? 0.f : 1.f / ls;
+        const int64_t at = row * p.hq + head;
+        uint16_t* out = static_cast<uint16_t*>(p.out) + at * D + 4 * hi;
+#pragma unroll
+        for (int mb = 0; mb < D / 32; ++mb)
+#pragma unroll
+          for (int c = 0; c < 4; ++c)
+            *reinterpret_cast<uint2*>(out + 32 * mb + 8 * c) =
+                make_uint2(pack_bf16x2(o[mb][4 * c] * inv, o[mb][4 * c + 1] * inv),
+                           pack_bf16x2(o[mb][4 * c + 2] * inv, o[mb][4 * c + 3] * inv));
+        if (p.lse && hi == 0) p.lse[at] = none ? -INFINITY : (m + log2f(ls)) * kLn2;
+      }
+    }
+    __syncthreads();  // (the next unit's tiles go over these)
+  });
+}
+
+// ---------------------------------------------------------------------------
+// merge
+// ---------------------------------------------------------------------------
+__device__ __forceinline__ void store4(uint16_t* p, const float4& a) {
+  *reinterpret_cast<uint2*>(p) = make_uint2(pack_bf16x2(a.x, a.y), pack_bf16x2(a.z, a.w));
+}
+__device__ __forceinline__ void store4(float* p, const float4& a) { *reinterpret_cast<float4*>(p) = a; }
+
+// The partial results of a unit that is cut between blocks, in the blocks' order.  D / 4 lanes take one
+// row and head; those whose unit one block took whole have nothing to do.
+constexpr int kMergeThreads = 256;
 template <typename T, int D>
-__global__ __launch_bounds__(kWaves * 64) void tree_attn_kernel(TreeAttn p) {
-  constexpr int VEC = Vec16<T>::N, NC = D / 64;
+__global__ __launch_bounds__(kMergeThreads) void tree_attn_merge_kernel(TreeAttn p, TreeCut cut, TreeWs ws, int lg) {
+  constexpr int LPR = D / 4, RPB = kMergeThreads / LPR;
+  const int l = threadIdx.x % LPR;
+  const int64_t item = (int64_t)blockIdx.x * RPB + threadIdx.x / LPR;
+  const int h = (int)(item % p.hq);
+  const int64_t bi = item / p.hq;
+  const int i = (int)(bi % p.max_q);
+  if (bi / p.max_q >= p.batch) return;
+  const int b = (int)(bi / p.max_q);
+  const TreeRequest q = tree_request(p, b);
+  if (i >= q.rows) return;
+  const int g = h >> lg, vec = (i << lg) + (h & ((1 << lg) - 1));
+  const int steps = tree_steps(q, cut.kt);
+  const int64_t all = ws.prefix[p.batch];
+  const int64_t u0 = ws.prefix[b] + (int64_t)(g * tree_tiles(q, lg, cut.vt) + vec / cut.vt) * steps, u1 = u0 + steps;
+  // the block whose share holds step u0
+  int x = (int)(u0 * cut.blocks / all);
+  while (x > 0 && tree_share(all, x, cut.blocks) > u0) --x;
+  while (tree_share(all, x + 1, cut.blocks) <= u0) ++x;
+  if (tree_share(all, x + 1, cut.blocks) >= u1) return;
+  float mx = -INFINITY, lt = 0.f;
+  float4 a = make_float4(0.f, 0.f, 0.f, 0.f);
+  for (; x < cut.blocks; ++x) {
+    const int64_t s0 = tree_share(all, x, cut.blocks), s1 = tree_share(all, x + 1, cut.blocks);
+    if (s0 >= u1) break;
+    if (s0 == s1) continue;
+    const int64_t at = (int64_t)(2 * x + (u0 < s0 ? 0 : 1)) * cut.vt + vec % cut.vt;
+    const float2 ml = ws.ml[at];
+    const float4 o = reinterpret_cast<const float4*>(ws.o)[at * LPR + l];
+    const float mn = fmaxf(mx, ml.x);
+    const float fa = __builtin_amdgcn_exp2f(mx - finite(mn)), fo = __builtin_amdgcn_exp2f(ml.x - finite(mn));
+    a.x = a.x * fa + o.x * fo;
+    a.y = a.y * fa + o.y * fo;
+    a.z = a.z * fa + o.z * fo;
+    a.w = a.w * fa + o.w * fo;
+    lt = lt * fa + ml.y * fo;
+    mx = mn;
+  }
+  const bool none = mx == -INFINITY;
+  const float inv = none ? 0.f : 1.f / lt;
+  const int64_t at = (q.r0 + i) * p.hq + h;
+  store4(static_cast<T*>(p.out) + at * D + 4 * l, make_float4(a.x * inv, a.y * inv, a.z * inv, a.w * inv));
+  if (p.lse && l == 0) p.lse[at] = none ? -INFINITY : (mx + log2f(lt)) * kLn2;
+}
+
+// ---------------------------------------------------------------------------
+// float32: one wave per row and head, 64 tokens at a time
+// ---------------------------------------------------------------------------
+template <int D>
+__global__ __launch_bounds__(256) void tree_attn_f32_kernel(TreeAttn p) {
+  constexpr int NC = D / 64;
   const int l = threadIdx.x & 63;
-  const int h = blockIdx.y * kWaves + (threadIdx.x >> 6);
+  const int h = blockIdx.y * 4 + (threadIdx.x >> 6);
   const int b = blockIdx.x / p.max_q, i = blockIdx.x % p.max_q;
   if (h >= p.hq) return;
-  const int64_t r0 = p.cu_q[b], nr = min((int64_t)p.cu_q[b + 1], p.n_rows) - r0;
-  if (r0 < 0 || i >= nr) return;
-  const int64_t r = r0 + i;
-  const int64_t kv = max(p.kv_len[b], 0);
-  const int64_t end = min(kv + nr, (int64_t)p.max_kv);
+  const TreeRequest rq = tree_request(p, b);
+  if (i >= rq.rows) return;
+  const int64_t r = rq.r0 + i;
   const int g = h / (p.hq / p.hkv);
-  const T* q = static_cast<const T*>(p.q) + (r * p.hq + h) * D;
+  const float* q = static_cast<const float*>(p.q) + (r * p.hq + h) * D;
   float m = -INFINITY, sum = 0.f, o[NC];
 #pragma unroll
   for (int c = 0; c < NC; ++c) o[c] = 0.f;
-  for (int64_t t0 = 0; t0 < end; t0 += 64) {
-    const int64_t t = t0 + l, pg = t >> p.page_log2;
-    bool see = t < end && pg < p.max_pages;
-    if (see && t >= kv) {
-      const int j = (int)(t - kv);
-      see = p.tree_mask ? j < 32 * p.mask_words && (p.tree_mask[r * p.mask_words + (j >> 5)] >> (j & 31) & 1)
-                        : j <= i;
-    }
-    int64_t slot = 0;
-    if (see) {
-      const int64_t page = p.block_table[b * p.table_stride + pg];
-      see = page >= 0 && page < p.n_pages;
-      slot = (page << p.page_log2) + (t & ((1ll << p.page_log2) - 1));
-    }
+  for (int t0 = 0; t0 < rq.end; t0 += 64) {
+    const uint64_t bits = tree_sees<32>(p, rq, r, i, t0) |
+                          (t0 + 32 < rq.end ? (uint64_t)tree_sees<32>(p, rq, r, i, t0 + 32) << 32 : 0);
+    const int64_t slot = max(slot_of(p, b, t0 + l, rq.end), (int64_t)-1);
+    const bool see = (bits >> l & 1) && slot >= 0;
     float x = -INFINITY;
     if (see) {
-      const T* k = static_cast<const T*>(p.k_cache) + slot * p.kv_stride + g * D;
+      const float* k = static_cast<const float*>(p.k_cache) + slot * p.kv_stride + g * D;
       float dot = 0.f;
-      for (int c = 0; c < D; c += VEC) {
-        float a[VEC], y[VEC];
-        Vec16<T>::unpack(ld16(q + c), a);
-        Vec16<T>::unpack(ld16(k + c), y);
-#pragma unroll
-        for (int e = 0; e < VEC; ++e) dot = fmaf(a[e], y[e], dot);
+      for (int c = 0; c < D; c += 4) {
+        const float4 a = *reinterpret_cast<const float4*>(q + c), y = *reinterpret_cast<const float4*>(k + c);
+        dot = fmaf(a.x, y.x, fmaf(a.y, y.y, fmaf(a.z, y.z, fmaf(a.w, y.w, dot))));
       }
       x = dot * p.scale;
     }
     const float mn = fmaxf(m, wave_max(x));
-    const float ref = mn == -INFINITY ? 0.f : mn;
-    const float w = see ? expf(x - ref) : 0.f, alpha = expf(m - ref);
+    const float w = see ? expf(x - finite(mn)) : 0.f, alpha = expf(m - finite(mn));
     sum = sum * alpha + wave_sum(w);
     m = mn;
 #pragma unroll
     for (int c = 0; c < NC; ++c) o[c] *= alpha;
-    uint64_t vis = __ballot(see);
-    while (vis) {
+    for (uint64_t vis = __ballot(see); vis; vis &= vis - 1) {
       const int k = __builtin_ctzll(vis);
-      vis &= vis - 1;
       const float wk = __shfl(w, k, 64);
       const int64_t sk = __shfl(slot, k, 64);
-      const T* v = static_cast<const T*>(p.v_cache) + sk * p.kv_stride + g * D;
+      const float* v = static_cast<const float*>(p.v_cache) + sk * p.kv_stride + g * D;
 #pragma unroll
-      for (int c = 0; c < NC; ++c) o[c] = fmaf(wk, to_f(v[c * 64 + l]), o[c]);
+      for (int c = 0; c < NC; ++c) o[c] = fmaf(wk, v[c * 64 + l], o[c]);
     }
   }
-  T* out = static_cast<T*>(p.out) + (r * p.hq + h) * D;
+  float* out = static_cast<float*>(p.out) + (r * p.hq + h) * D;
+  const bool none = m == -INFINITY;
 #pragma unroll
-  for (int c = 0; c < NC; ++c) store_as(out + c * 64 + l, m == -INFINITY ? 0.f : o[c] / sum);
-  if (p.lse && l == 0) p.lse[r * p.hq + h] = m == -INFINITY ? -INFINITY : m + logf(sum);
+  for (int c = 0; c < NC; ++c) out[c * 64 + l] = none ? 0.f : o[c] / sum;
+  if (p.lse && l == 0) p.lse[r * p.hq + h] = none ? -INFINITY : m + logf(sum);
+}
+
+int log2_of(int x) { return __builtin_ctz((unsigned)x); }
+
+// How a bf16 call is cut, from its bounds (lengths are on the device)
+TreeCut tree_cut(int batch, int max_q, int max_kv, int hq, int hkv) {
+  const int64_t vectors = (int64_t)max_q * (hq / hkv);
+  TreeCut c;
+  if (vectors <= 32) {
+    c.vt = vectors <= 16 ? 16 : 32;
+    c.kt = kNW * kNT;
+    c.tiles = 1;
+  } else {
+    const int64_t groups = (vectors + 31) / 32;
+    const int64_t tiles = (groups + 7) / 8;
+    int vg = (int)((groups + tiles - 1) / tiles);
+    if (vg == 7) vg = 8;
+    c.vt = 32 * vg;
+    c.kt = kWT;
+    c.tiles = (int)((vectors + c.vt - 1) / c.vt);
+  }
+  const int64_t steps = ((int64_t)max_kv + c.kt - 1) / c.kt;
+  const int64_t all = (int64_t)batch * hkv * c.tiles * steps;
+  // short units are taken whole; else as many blocks as run at once, with 4 steps each at least
+  c.blocks = 0;
+  if (steps > 8) c.blocks = (int)std::max<int64_t>(std::min<int64_t>(c.vt > 128 ? 256 : 512, all / 4), 1);
+  return c;
+}
+
+struct WsLayout {
+  size_t ml, o, total;
+};
+WsLayout ws_layout(const TreeCut& c, int batch, int d) {
+  const auto up = [](size_t x) { return (x + 255) / 256 * 256; };
+  WsLayout w{};
+  if (c.blocks == 0) return w;
+  w.ml = up(((size_t)batch + 1) * 8);
+  w.o = w.ml + up((size_t)2 * c.blocks * c.vt * 8);
+  w.total = w.o + up((size_t)2 * c.blocks * c.vt * d * 4);
+  return w;
+}
+
+template <int D>
+hipError_t launch_bf16(const TreeAttn& p, void* workspace, hipStream_t stream) {
+  const int lg = log2_of(p.hq / p.hkv);
+  const TreeCut c = tree_cut(p.batch, p.max_q, p.max_kv, p.hq, p.hkv);
+  const WsLayout wl = ws_layout(c, p.batch, D);
+  char* base = static_cast<char*>(workspace);
+  const TreeWs ws{reinterpret_cast<int64_t*>(base), reinterpret_cast<float2*>(base + wl.ml),
+                  reinterpret_cast<float*>(base + wl.o)};
+  const int64_t blocks = c.blocks ? c.blocks : (int64_t)p.batch * p.hkv * c.tiles;
+  if (blocks > 0x7fffffff) return hipErrorInvalidConfiguration;
+  const dim3 grid((unsigned)blocks);
+  const bool tiny = p.page_log2 < 4;
+#define QCF_NARROW(NV)                                                                          \
+  do {                                                                                          \
+    if (tiny) tree_attn_narrow_kernel<D, NV, true><<<grid, kNW * 64, 0, stream>>>(p, c, ws, lg); \
+    else tree_attn_narrow_kernel<D, NV, false><<<grid, kNW * 64, 0, stream>>>(p, c, ws, lg);     \
+  } while (0)
+#define QCF_WIDE(VG)                                                                            \
+  case VG:                                                                                      \
+    if (tiny) tree_attn_wide_kernel<D, VG, true><<<grid, VG * 64, 0, stream>>>(p, c, ws, lg);   \
+    else tree_attn_wide_kernel<D, VG, false><<<grid, VG * 64, 0, stream>>>(p, c, ws, lg);       \
+    break
+  if (c.vt == 16 && c.kt == kNW * kNT) QCF_NARROW(1);
+  else if (c.kt == kNW * kNT) QCF_NARROW(2);
+  else switch (c.vt / 32) {
+    QCF_WIDE(2);
+    QCF_WIDE(3);
+    QCF_WIDE(4);
+    QCF_WIDE(5);
+    QCF_WIDE(6);
+    QCF_WIDE(8);
+  }
+#undef QCF_WIDE
+#undef QCF_NARROW
+  if (c.blocks) {
+    const int64_t rows = (int64_t)p.batch * p.max_q * p.hq;
+    const int rpb = kMergeThreads / (D / 4);
+    tree_attn_merge_kernel<uint16_t, D><<<dim3((unsigned)((rows + rpb - 1) / rpb)), kMergeThreads, 0, stream>>>(p, c, ws, lg);
+  }
+  return hipGetLastError();
 }
 
 }  // namespace
 
-size_t tree_attn_workspace(int, int, int, int, int, int, bool) { return 0; }
+size_t tree_attn_workspace(int batch, int max_q, int max_kv, int hq, int hkv, int head_dim, bool bf16) {
+  if (!bf16) return 0;
+  return ws_layout(tree_cut(batch, max_q, max_kv, hq, hkv), batch, head_dim).total;
+}
 
-hipError_t launch_tree_attn(const TreeAttn& p, bool bf16, int head_dim, void*, hipStream_t stream) {
-  const int64_t blocks = (int64_t)p.batch * p.max_q;
-  if (blocks > 0x7fffffff) return hipErrorInvalidConfiguration;
-  const dim3 grid((unsigned)blocks, (unsigned)((p.hq + kWaves - 1) / kWaves));
-  if (bf16) {
-    if (head_dim == 64) tree_attn_kernel<uint16_t, 64><<<grid, kWaves * 64, 0, stream>>>(p);
-    else tree_attn_kernel<uint16_t, 128><<<grid, kWaves * 64, 0, stream>>>(p);
-  } else {
-    if (head_dim == 64) tree_attn_kernel<float, 64><<<grid, kWaves * 64, 0, stream>>>(p);
-    else tree_attn_kernel<float, 128><<<grid, kWaves * 64, 0, stream>>>(p);
-  }
+hipError_t launch_tree_attn(const TreeAttn& p, bool bf16, int head_dim, void* ws, hipStream_t stream) {
+  if ((int64_t)p.batch * p.max_q * p.hq > 0x7fffffff) return hipErrorInvalidConfiguration;
+  if (bf16) return head_dim == 64 ? launch_bf16<64>(p, ws, stream) : launch_bf16<128>(p, ws, stream);
+  const dim3 grid((unsigned)(p.batch * p.max_q), (unsigned)((p.hq + 3) / 4));
+  if (head_dim == 64) tree_attn_f32_kernel<64><<<grid, 256, 0, stream>>>(p);
+  else tree_attn_f32_kernel<128><<<grid, 256, 0, stream>>>(p);
   return hipGetLastError();
 }
 
