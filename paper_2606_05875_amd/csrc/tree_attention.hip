@@ -10,12 +10,14 @@
 //  narrow  up to 32 query vectors per request and KV head (one token, short chains).  Bound: HBM.  Four
 //          waves take 16-token tiles in turn, each on its own (two stages of LDS, no barrier in the loop),
 //          v_mfma_f32_16x16x32/16x16x16_bf16; their results are summed through LDS once per unit.
-//  wide    more vectors (trees).  A wave holds 32 of them (v_mfma_f32_32x32x16_bf16) and the 2 to 8
-//          waves of a block share every 32-token tile (three stages, one barrier per tile).  Bound: HBM
+//  wide    more vectors (trees).  A wave holds 32 of them (v_mfma_f32_32x32x16_bf16) and the 2, 4 or 8
+//          waves of a block share every 64-token tile (a ring of stages, one barrier per tile); the
+//          products of the next tile's S run beside this tile's exponentials.  Bound: HBM
 //          up to about 128 vectors, the matrix units beyond.
 #include <math.h>
 
 #include <algorithm>
+#include <type_traits>
 
 #include "qcf_attn.h"
 #include "qcf_tree.h"
@@ -41,13 +43,9 @@ __device__ __forceinline__ void copy16(const void* from, uint32_t lds) {
 // a running maximum as the reference of exponentials: 0 while nothing has been seen
 __device__ __forceinline__ float finite(float m) { return m == -INFINITY ? 0.f : m; }
 
-// exp2(s * scale2 - ref).  The fused form keeps the product exact, but its difference to the rounded
-// maximum reaches 2^-24 of that, too much to be an exponent where maxima pass 2^28 (`big`).
-__device__ __forceinline__ float weight(float s, float scale2, float ref, bool big) {
-#pragma clang fp contract(off)
-  const float x = s * scale2;
-  return __builtin_amdgcn_exp2f(big ? x - ref : fmaf(s, scale2, -ref));
-}
+// Weights are exp2(s * scale2 - ref) with a fused multiply-add, which keeps the product exact; its
+// difference to the rounded maximum reaches 2^-24 of that, too much to be an exponent where maxima
+// pass 2^28.  Such logits are scaled (and rounded) first.
 __device__ __forceinline__ bool is_big(float m) { return __ballot(fabsf(finite(m)) > 0x1p28f) != 0; }
 
 // any of a 16-byte piece's 8 values infinite or NaN
@@ -260,9 +258,11 @@ __global__ __launch_bounds__(kNW * 64, 2) void tree_attn_narrow_kernel(TreeAttn 
           big[c] = is_big(mn);
         }
         const float ref = finite(m[c]);
+        if (big[c]) s[c] *= scale2;
+        const float sc = big[c] ? 1.f : scale2;
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
-          pw[c][r] = weight(s[c][r], scale2, ref, big[c]);
+          pw[c][r] = __builtin_amdgcn_exp2f(fmaf(s[c][r], sc, -ref));
           pb[c][r] = (short)f2bf(pw[c][r]);
         }
         ls[c] += (pw[c][0] + pw[c][1]) + (pw[c][2] + pw[c][3]);
@@ -356,47 +356,119 @@ __global__ __launch_bounds__(kNW * 64, 2) void tree_attn_narrow_kernel(TreeAttn 
 // ---------------------------------------------------------------------------
 // wide
 // ---------------------------------------------------------------------------
-constexpr int kWT = 32;  // tokens per step
-constexpr int kWStages = 3;
+constexpr int kWT = 64;  // tokens per step
+// Stages of the K and V rings.  A block of 8 waves is alone on its CU and takes most of its LDS, smaller
+// ones run two at a time.
+constexpr int wide_stages(int d, int vg) { return (vg == 8 ? 4 : 2) * (d == 64 ? 2 : 1); }
 
 template <int D, int VG, bool kTiny>
-__global__ __launch_bounds__(VG * 64, 2) void tree_attn_wide_kernel(TreeAttn p, TreeCut cut, TreeWs ws, int lg) {
-  constexpr int CH = D / 8;              // 16-byte chunks per row
-  constexpr int RPC = 64 / CH;           // rows per copy
-  constexpr int RB = D * 2;              // bytes per row
-  constexpr int TB = kWT * RB;           // bytes of a tile of K or V
-  constexpr int TC = kWT / RPC;          // copies per tile of K or V
-  constexpr int WC = (TC + VG - 1) / VG;  // per wave (the last ones may be made twice)
+__global__ __launch_bounds__(VG * 64, VG == 2 ? 1 : 2) void tree_attn_wide_kernel(TreeAttn p, TreeCut cut, TreeWs ws, int lg) {
+  constexpr int CH = D / 8;        // 16-byte chunks per row
+  constexpr int RPC = 64 / CH;     // rows per copy
+  constexpr int RB = D * 2;        // bytes per row
+  constexpr int TB = kWT * RB;     // bytes of a tile of K or V
   constexpr int VT = 32 * VG;
-  __shared__ __attribute__((aligned(1024))) uint8_t ring[kWStages * 2 * TB];
-  __shared__ uint32_t loose_l;
+  constexpr int NB = wide_stages(D, VG);
+  // Copies go by groups of 16 rows, which lie in one page: wave w takes groups w, w + VG, .. of the
+  // tile's four, or (8 waves) half of group w / 2
+  constexpr int CPG = 16 / RPC;
+  constexpr int WG = VG >= 4 ? 1 : 4 / VG;      // groups per wave
+  constexpr int WC = VG == 8 ? CPG / 2 : CPG;   // copies of a group per wave, K or V
+  constexpr int WI = WG * WC;
+  static_assert(VG == 2 || VG == 4 || VG == 8, "groups are shared evenly");
+  __shared__ __attribute__((aligned(1024))) uint8_t k_ring[NB * TB];
+  __shared__ __attribute__((aligned(1024))) uint8_t v_ring[NB * TB];
+  __shared__ uint32_t loose_l[2];
 
   const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int l = threadIdx.x & 63, lq = l & 31, hi = l >> 5;
-  const uint32_t lds0 = lds_addr(ring);
+  const uint32_t k_lds = lds_addr(k_ring), v_lds = lds_addr(v_ring);
   const uint32_t row_b = (uint32_t)(p.kv_stride * 2);
   const float scale2 = p.scale * kLog2e;
   // Chunk c of K row r sits at c ^ (r % 16) (D = 64: c ^ (r / 2 % 8)), of V row r at c ^ 4 (r % 4)
   // (D = 64: c ^ 4 (r / 2 % 2)): lane fragments st at krd ^ (st << 5), V column blocks mb at vrd ^ (mb << 6)
   const int ky = D == 128 ? lq & 15 : (lq >> 1) & 7;
-  const int krd = lq * RB + (hi ^ (ky & 1)) * 16 + (ky >> 1) * 32;
+  int krd = lq * RB + (hi ^ (ky & 1)) * 16 + (ky >> 1) * 32;
   const int tg = l >> 4, te = (l >> 2) & 3, tq = l & 3;
   const int vrd = (4 * (tg >> 1) + te) * RB + (D == 128 ? te : te >> 1) * 64 + 32 * (tg & 1) + 8 * tq;
-  int cp[WC];  // this wave's copies of a tile
-  uint32_t koff[WC], voff[WC];
-#pragma unroll
-  for (int i = 0; i < WC; ++i) {
-    cp[i] = min(w + VG * i, TC - 1);
-    const int r = RPC * cp[i] + l / CH, c = l % CH;
-    koff[i] = (r & 15) * row_b + (c ^ (D == 128 ? r & 15 : (r >> 1) & 7)) * 16;
-    voff[i] = (r & 15) * row_b + (c ^ (4 * (D == 128 ? r & 3 : (r >> 1) & 1))) * 16;
-  }
+  const int c0 = VG == 8 ? (w & 1) * WC : 0;  // this wave's first copy in a group
+  // copy i of a group fills rows RPC i + l / CH: the row within the copy and the chunk of K, V before i's
+  // part of the exchange (which i's bits give by themselves)
+  const int cr = l / CH, cc = l % CH;
+  uint32_t coff = cr * row_b, kx = (cc ^ (D == 128 ? cr : cr >> 1)) * 16;
+  const uint32_t vx = (cc ^ (4 * (D == 128 ? cr : (cr >> 1) & 1))) * 16;
 
   tree_walk<VG * 64>(p, cut, ws, lg, [&](int b, const TreeRequest& rq, int g, int tile, int first, int n,
                                          int steps, int slot) {
     const_i32 table = (const_i32)(p.block_table + b * p.table_stride);
     const uint16_t* kc = static_cast<const uint16_t*>(p.k_cache) + (int64_t)g * D;
     const uint16_t* vc = static_cast<const uint16_t*>(p.v_cache) + (int64_t)g * D;
+    const bool pool = p.n_pages > 0 && (kTiny || p.page_log2 >= 4);
+    const int t_first = first * kWT;
+    auto group = [&](int k) { return VG >= 4 ? w * 4 / VG : w + VG * k; };
+    auto page_at = [&](int t, int k) {
+      return kTiny || t >= n ? -1 : page_of(p, table, t_first + t * kWT + 16 * group(k), rq.end);
+    };
+    // K (V) of this wave's groups of tile t into its stage; without a page the pool's first rows stand in
+    // and are not seen
+    auto copy = [&](auto is_k, uint32_t lds, int t, const int (&page)[WG]) {
+      constexpr bool kK = decltype(is_k)::value;
+      const uint16_t* from = kK ? kc : vc;
+      const uint32_t to = lds + (t & (NB - 1)) * TB;
+      asm volatile("" : "+v"(coff), "+v"(kx));  // (formed anew: every copy's offset kept is a register each)
+#pragma unroll
+      for (int k = 0; k < WG; ++k) {
+        const int t0 = t_first + t * kWT + 16 * group(k);
+        const int64_t at = page[k] < 0 ? 0 : ((int64_t)page[k] << p.page_log2) + (t0 & ((1 << p.page_log2) - 1));
+#pragma unroll
+        for (int i = 0; i < WC; ++i) {
+          const int ci = c0 + i;
+          const uint32_t dst = to + (group(k) * CPG + ci) * 1024;
+          const uint32_t chunk = kK ? kx ^ (ci * 64) : vx;
+          if (!kTiny)
+            copy16(from + (at + RPC * ci) * p.kv_stride, coff + chunk, dst);
+          else
+            copy16(from + max(slot_of(p, b, t0 + RPC * ci + cr, rq.end), (int64_t)0) * p.kv_stride + chunk / 2, dst);
+        }
+      }
+    };
+    const std::true_type K{};
+    const std::false_type V{};
+    // K(0); then K(t + 1), V(t), in this order to the end
+    int page[WG], pagev[WG];  // of the next K to be copied, of the next V
+    if (pool) {
+#pragma unroll
+      for (int k = 0; k < WG; ++k) page[k] = page_at(0, k);
+      copy(K, k_lds, 0, page);
+#pragma unroll
+      for (int t = 1; t < NB; ++t) {
+#pragma unroll
+        for (int k = 0; k < WG; ++k) {
+          pagev[k] = page[k];
+          page[k] = page_at(t, k);
+        }
+        if (t < n) copy(K, k_lds, t, page);
+        if (t <= n) copy(V, v_lds, t - 1, pagev);
+      }
+#pragma unroll
+      for (int k = 0; k < WG; ++k) {
+        pagev[k] = page[k];
+        page[k] = page_at(NB, k);
+      }
+    }
+    // pages that are not there are rare: looked for once, then tile by tile
+    bool holes = kTiny;
+    if (!kTiny && pool) {
+      const int lp = p.page_log2, p0 = t_first >> lp;
+      const int p1 = min((min(t_first + n * kWT, rq.end) + (1 << lp) - 1) >> lp, (int)INT32_MAX);
+      bool bad = false;
+      for (int i = p0 + (int)threadIdx.x; i < p1; i += VG * 64) {
+        const int x = i < p.max_pages ? p.block_table[b * p.table_stride + i] : -1;
+        bad = bad || x < 0 || x >= p.n_pages;
+      }
+      holes = __syncthreads_or(bad);
+    }
+
     const int v0 = tile * VT + 32 * w;
     const int idx = (v0 + lq) >> lg;
     const int head = (g << lg) + ((v0 + lq) & ((1 << lg) - 1));
@@ -409,161 +481,248 @@ __global__ __launch_bounds__(VG * 64, 2) void tree_attn_wide_kernel(TreeAttn p, 
 #pragma unroll
       for (int st = 0; st < D / 16; ++st) qreg[st] = as_bf16x8(ld16(q + 16 * st));
     }
+    // Q has to be there before the loop: a wait for it inside would count the copies in flight
 #pragma unroll
     for (int st = 0; st < D / 16; ++st) asm volatile("" : "+v"(qreg[st]));
     f32x16 o[D / 32];
 #pragma unroll
     for (int mb = 0; mb < D / 32; ++mb) o[mb] = f32x16{};
-    float m = -INFINITY, ls = 0.f;
+    float m = -INFINITY, ls = 0.f;  // running maximum in log2 units, this lane's part of the sum
     bool big = false;
 
-    const bool pool = p.n_pages > 0 && (kTiny || p.page_log2 >= 4);
-    const int t_first = first * kWT;
-    auto page_at = [&](int i, int half) {
-      return kTiny || i >= n ? -1 : page_of(p, table, t_first + i * kWT + 16 * half, rq.end);
-    };
-    auto copy_tile = [&](int t0, int page_a, int page_b, int s) {
-      const uint32_t lk0 = lds0 + s * 2 * TB, lv0 = lk0 + TB;
-#pragma unroll
-      for (int i = 0; i < WC; ++i) {
-        if (!kTiny) {
-          const bool half = RPC * cp[i] >= 16;
-          const int page = half ? page_b : page_a, t = t0 + (half ? 16 : 0);
-          const int64_t at = page < 0 ? 0 : ((int64_t)page << p.page_log2) + (t & ((1 << p.page_log2) - 1));
-          copy16(kc + at * p.kv_stride, koff[i], lk0 + cp[i] * 1024);
-          copy16(vc + at * p.kv_stride, voff[i], lv0 + cp[i] * 1024);
-        } else {
-          const int r = RPC * cp[i] + l / CH;
-          const int64_t at = max(slot_of(p, b, t0 + r, rq.end), (int64_t)0) * p.kv_stride;
-          copy16(kc + at + (koff[i] - (r & 15) * row_b) / 2, lk0 + cp[i] * 1024);
-          copy16(vc + at + (voff[i] - (r & 15) * row_b) / 2, lv0 + cp[i] * 1024);
-        }
-      }
-    };
-    // pages of tile i and the two after it
-    int pa[3], pb_[3];
-#pragma unroll
-    for (int k = 0; k < 3; ++k) {
-      pa[k] = page_at(k, 0);
-      pb_[k] = page_at(k, 1);
-    }
-    if (pool) {
-      copy_tile(t_first, pa[0], pb_[0], 0);
-      if (n > 1) copy_tile(t_first + kWT, pa[1], pb_[1], 1);
-    }
-    int stage = 0;
-    for (int i = 0; i < n && pool; ++i) {
-      const int t0 = t_first + i * kWT;
-      // this wave's copies of tile i are complete, then everyone's, and everyone has read tile i - 1
+    // this wave's copies but the last `pairs` (K, V) are there, then the block's
+    auto meet = [&](int pairs) {
       asm volatile("" ::: "memory");
-      if (i + 1 < n) wait_vm_lgkm0<2 * WC>();
+      if (NB > 2 && pairs == NB - 2) wait_vm_lgkm0<(NB - 2) * 2 * WI>();
+      else if (pairs == NB - 1) wait_vm_lgkm0<(NB - 1) * 2 * WI>();
       else wait_vm_lgkm0<0>();
       __builtin_amdgcn_s_barrier();
       asm volatile("" ::: "memory");
-      if (i + 2 < n) copy_tile(t0 + 2 * kWT, pa[2], pb_[2], stage == 0 ? 2 : stage - 1);
-      uint8_t* kl = ring + stage * 2 * TB;
-      uint8_t* vl = kl + TB;
-      stage = stage == kWStages - 1 ? 0 : stage + 1;
-      const int page_a = pa[0], page_b = pb_[0];
-      pa[0] = pa[1];
-      pb_[0] = pb_[1];
-      pa[1] = pa[2];
-      pb_[1] = pb_[2];
-      pa[2] = page_at(i + 3, 0);
-      pb_[2] = page_at(i + 3, 1);
-
-      // tokens of the tile that there are, as bits (the same for the whole block)
-      uint32_t held = 0xffffffffu;
-      if (kTiny) held = (uint32_t)__ballot(slot_of(p, b, t0 + lq, rq.end) >= 0);
-      else held = (page_a < 0 ? 0u : 0xffffu) | (page_b < 0 ? 0u : 0xffff0000u);
-      if (rq.end - t0 < kWT) held &= rq.end > t0 ? (1u << (rq.end - t0)) - 1u : 0u;
-      const bool edge = t0 + kWT > rq.kv || held != 0xffffffffu;
-      uint32_t loose = 0;
-      if (edge) {
-        // rows that hold no token become zeros; tokens with a value that is not finite are taken out
-        // and added to the rows that see them (see the narrow kernel)
-        if (threadIdx.x == 0) loose_l = 0;
-        __syncthreads();
-        for (int u = threadIdx.x; u < TC * 64; u += VG * 64) {
-          const int r = u / CH;
-          if (!(held >> r & 1)) st16(vl + 16 * u, make_uint4(0, 0, 0, 0));
-          else if (not_finite(ld16(vl + 16 * u))) atomicOr(&loose_l, 1u << r);
-        }
-        __syncthreads();
-        loose = loose_l;
-      }
-      if (busy || loose) {
-        f32x16 s = f32x16{};
+    };
+    constexpr int NS = D / 16;  // products per 32 tokens of S
+    auto k_frag = [&](const uint8_t* kl, int i) {
+      return as_bf16x8(ld16(kl + (i / NS) * 32 * RB + (krd ^ ((i % NS) << 5))));
+    };
+    auto products = [&](const uint8_t* kl, f32x16 (&s)[2]) {
 #pragma unroll
-        for (int st = 0; st < D / 16; ++st)
-          s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(ld16(kl + (krd ^ (st << 5)))), qreg[st], s, 0, 0, 0);
-        // lane value v is token t0 + 8 (v >> 2) + 4 hi + (v & 3)
-        uint32_t sees = 0xffffffffu;
-        if (edge) {
-          sees = rq.end > t0 ? tree_sees<32>(p, rq, row, idx, t0) & held : 0u;
+      for (int hb = 0; hb < 2; ++hb) {
+        __builtin_amdgcn_sched_barrier(0);
+        s[hb] = f32x16{};
+#pragma unroll
+        for (int st = 0; st < NS; ++st)
+          s[hb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k_frag(kl, hb * NS + st), qreg[st], s[hb], 0, 0, 0);
+      }
+    };
+    // the running maximum of the tile's logits, and what the exponentials are taken of
+    auto maximum = [&](f32x16 (&s)[2]) {
+      float mt = s[0][0];
+#pragma unroll
+      for (int e = 1; e < 32; ++e) mt = fmaxf(mt, s[e >> 4][e & 15]);
+      mt *= scale2;
+      // lazily and by each vector's own growth (see the narrow kernel)
+      if (__ballot(mt > m + 8.f)) {
+        mt = fmaxf(mt, __shfl_xor(mt, 32, 64));
+        const float mn = mt > m + 8.f ? mt : m;
+        const float alpha = __builtin_amdgcn_exp2f(m - finite(mn));
+        ls *= alpha;
+#pragma unroll
+        for (int mb = 0; mb < D / 32; ++mb) o[mb] *= alpha;
+        m = mn;
+        big = is_big(mn);
+      }
+      if (big) {
+        s[0] *= scale2;
+        s[1] *= scale2;
+      }
+    };
+    typedef float f32x2_t __attribute__((ext_vector_type(2)));
+    typedef __bf16 bf16x2_t __attribute__((ext_vector_type(2)));
+    // P of the tile; with kNext S of the next one beside it: one product per fenced group with its K fragment
+    // read four groups ahead, a group's arguments, exponentials and sums in three groups in turn
+    auto weights = [&](auto next, const uint8_t* kn, f32x16 (&sn)[2], f32x16 (&s)[2], bf16x8 (&pb)[2][2]) {
+      constexpr bool kNext = decltype(next)::value;
+      constexpr int NM = 2 * NS, EG = 32 / NM, PF = 4;
+      const float nm = -finite(m), sc = big ? 1.f : scale2;
+      float psum = 0.f, x[32], pw[32];
+      bf16x8 kf[NM];
+      auto arg = [&](int i) {
+#pragma unroll
+        for (int e = EG * i; e < EG * (i + 1); ++e) x[e] = fmaf(s[e >> 4][e & 15], sc, nm);
+      };
+      auto sum_pack = [&](int i) {
+#pragma unroll
+        for (int e = EG * i; e < EG * (i + 1); e += 2) {
+          psum += pw[e];
+          psum += pw[e + 1];
+          const bf16x2_t pk = __builtin_convertvector((f32x2_t){pw[e], pw[e + 1]}, bf16x2_t);
+          pb[e >> 4][(e >> 3) & 1][e & 7] = pk[0];
+          pb[e >> 4][(e >> 3) & 1][(e & 7) + 1] = pk[1];
+        }
+      };
+      if (kNext) {
+#pragma unroll
+        for (int i = 0; i < PF; ++i) kf[i] = k_frag(kn, i);
+      }
+      arg(0);
+#pragma unroll
+      for (int i = 0; i < NM; ++i) {
+        __builtin_amdgcn_sched_barrier(0);
+        if (kNext) {
+          if (i + PF < NM) kf[i + PF] = k_frag(kn, i + PF);
+          sn[i / NS] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[i], qreg[i % NS], i % NS == 0 ? f32x16{} : sn[i / NS], 0, 0, 0);
+        }
+        if (i + 1 < NM) arg(i + 1);
+#pragma unroll
+        for (int e = EG * i; e < EG * (i + 1); ++e) pw[e] = __builtin_amdgcn_exp2f(x[e]);
+        if (i > 0) sum_pack(i - 1);
+      }
+      __builtin_amdgcn_sched_barrier(0);
+      sum_pack(NM - 1);
+      ls += psum;
+    };
+    // O += V^T P^T, one product per fenced group with its V fragment read four groups ahead
+    auto products_o = [&](const uint8_t* vl, bf16x8 (&pb)[2][2]) {
+      constexpr int MB = D / 32, NM = 4 * MB, PF = 4;
+      auto v_frag = [&](int j) {
+        const uint8_t* at = vl + (j / MB) * 16 * RB + (vrd ^ ((j % MB) << 6));
+        const v4s lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4s)(at));
+        const v4s up = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4s)(at + 8 * RB));
+        return __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, up, 0, 1, 2, 3, 4, 5, 6, 7));
+      };
+      bf16x8 vf[NM];
+#pragma unroll
+      for (int j = 0; j < PF; ++j) vf[j] = v_frag(j);
+#pragma unroll
+      for (int j = 0; j < NM; ++j) {
+        __builtin_amdgcn_sched_barrier(0);
+        if (j + PF < NM) vf[j + PF] = v_frag(j + PF);
+        o[j % MB] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[j], pb[j / (2 * MB)][(j / MB) & 1], o[j % MB], 0, 0, 0);
+      }
+      __builtin_amdgcn_sched_barrier(0);
+    };
+
+    // K(t + 1) and V(t) are there, and everyone has read K(t) and V(t - 1), whose stages are filled next
+    auto begin = [&](int t) {
+      meet(t + NB - 1 < n ? NB - 2 : 0);
+      if (t + NB < n) copy(K, k_lds, t + NB, page);
+      if (t + NB - 1 < n) copy(V, v_lds, t + NB - 1, pagev);
+#pragma unroll
+      for (int k = 0; k < WG; ++k) {
+        pagev[k] = page[k];
+        page[k] = page_at(t + NB + 1, k);
+      }
+    };
+    // element e of s is token t0 + 32 (e / 16) + 8 (e / 4 % 4) + 4 hi + e % 4
+    // the tiles before the first that is the last one or has tokens that are not there or not seen by all
+    const int plain = holes ? 0 : min(n - 1, (min(rq.kv, rq.end) - t_first) / kWT) & ~1;
+    auto plain_step = [&](int t, f32x16 (&s)[2], f32x16 (&sn)[2]) {
+      begin(t);
+      bf16x8 pb[2][2];
+      maximum(s);
+      __builtin_amdgcn_s_setprio(1);
+      weights(std::true_type{}, k_ring + ((t + 1) & (NB - 1)) * TB, sn, s, pb);
+      __builtin_amdgcn_s_setprio(0);
+      products_o(v_ring + (t & (NB - 1)) * TB, pb);
+    };
+    // Tiles with tokens that are not there or that some row does not see.  held: those that are there, as
+    // bits; true if there is something to do (for the whole block).
+    auto is_edge = [&](int t, uint64_t& held) {
+      const int t0 = t_first + t * kWT;
+      held = ~0ull;
+      if (holes) held = __ballot(slot_of(p, b, t0 + l, rq.end) >= 0);
+      else if (rq.end - t0 < kWT) held = rq.end > t0 ? (1ull << (rq.end - t0)) - 1ull : 0ull;
+      return t0 + kWT > rq.kv || held != ~0ull;
+    };
+    // rows of V that hold no token become zeros; the result is the tokens with a value that is not
+    // finite, which are added to the rows that see them one by one (see the narrow kernel) ..
+    auto clean = [&](int t, uint64_t held) {
+      uint8_t* vl = v_ring + (t & (NB - 1)) * TB;
+      if (threadIdx.x < 2) loose_l[threadIdx.x] = 0;
+      __syncthreads();
+      for (int u = threadIdx.x; u < kWT * CH; u += VG * 64) {
+        const int r = u / CH;
+        if (!(held >> r & 1)) st16(vl + 16 * u, make_uint4(0, 0, 0, 0));
+        else if (not_finite(ld16(vl + 16 * u))) atomicOr(&loose_l[r >> 5], 1u << (r & 31));
+      }
+      __syncthreads();
+      return (uint64_t)(uint32_t)uni((int)loose_l[1]) << 32 | (uint32_t)uni((int)loose_l[0]);
+    };
+    // .. and taken out once everyone has done so
+    auto take_out = [&](int t, uint64_t loose) {
+      uint8_t* vl = v_ring + (t & (NB - 1)) * TB;
+      __syncthreads();
+      for (int u = threadIdx.x; u < kWT * CH; u += VG * 64)
+        if (loose >> (u / CH) & 1) st16(vl + 16 * u, make_uint4(0, 0, 0, 0));
+      __syncthreads();
+    };
+    // any step, its next S (into s) after it
+    auto other_step = [&](int t, f32x16 (&s)[2]) {
+      const int t0 = t_first + t * kWT;
+      begin(t);
+      const uint8_t* kn = k_ring + ((t + 1) & (NB - 1)) * TB;
+      const uint8_t* vl = v_ring + (t & (NB - 1)) * TB;
+      bf16x8 pb[2][2];
+      uint64_t held, loose = 0;
+      uint32_t sees[2] = {0, 0};
+      if (is_edge(t, held)) {
+        loose = clean(t, held);
+#pragma unroll
+        for (int hb = 0; hb < 2; ++hb) {
+          const uint32_t h = (uint32_t)(held >> (32 * hb));
+          sees[hb] = h ? tree_sees<32>(p, rq, row, idx, t0 + 32 * hb) & h : 0u;
 #pragma unroll
           for (int v = 0; v < 16; ++v)
-            if (!(sees >> (8 * (v >> 2) + 4 * hi + (v & 3)) & 1)) s[v] = -INFINITY;
+            if (!(sees[hb] >> (8 * (v >> 2) + 4 * hi + (v & 3)) & 1)) s[hb][v] = -INFINITY;
         }
-        float mt = s[0];
+      }
+      maximum(s);
+      weights(std::false_type{}, kn, s, s, pb);
+      if (loose) {
+        for (uint64_t left = loose; left; left &= left - 1) {
+          const int k = __builtin_ctzll(left);
+          float a = 0.f;
 #pragma unroll
-        for (int v = 1; v < 16; ++v) mt = fmaxf(mt, s[v]);
-        mt *= scale2;
-        if (__ballot(mt > m + 8.f)) {
-          mt = fmaxf(mt, __shfl_xor(mt, 32, 64));
-          const float mn = mt > m + 8.f ? mt : m;
-          const float alpha = __builtin_amdgcn_exp2f(m - finite(mn));
-          ls *= alpha;
+          for (int e = 0; e < 32; ++e) a = (k >> 3) * 4 + (k & 3) == e ? s[e >> 4][e & 15] : a;
+          a = __builtin_amdgcn_exp2f(fmaf(a, big ? 1.f : scale2, -finite(m)));
+          const float pk = __shfl(a, ((k >> 2) & 1) * 32 + lq, 64);
+          if ((k < 32 ? sees[0] : sees[1]) >> (k & 31) & 1) {
+            const int sw = D == 128 ? k & 3 : (k >> 1) & 1;
 #pragma unroll
-          for (int mb = 0; mb < D / 32; ++mb) o[mb] *= alpha;
-          m = mn;
-          big = is_big(mn);
-        }
-        const float ref = finite(m);
-        bf16x8 pv[2];
-        float psum = 0.f, pw[16];
+            for (int mb = 0; mb < D / 32; ++mb)
 #pragma unroll
-        for (int v = 0; v < 16; ++v) {
-          pw[v] = weight(s[v], scale2, ref, big);
-          psum += pw[v];
-          pv[v >> 3][v & 7] = (__bf16)pw[v];
-        }
-        ls += psum;
-        if (loose) {
-          for (uint32_t left = loose; left; left &= left - 1) {
-            const int k = __builtin_ctz(left);
-            float a = 0.f;
+              for (int c = 0; c < 4; ++c) {
+                // columns 32 mb + 8 c + 4 hi .. + 3: half of chunk 4 mb + c
+                const uint16_t* x = reinterpret_cast<const uint16_t*>(vl + k * RB + (((4 * mb + c) ^ (4 * sw)) * 16) + 8 * hi);
 #pragma unroll
-            for (int v = 0; v < 16; ++v) a = (k >> 3) * 4 + (k & 3) == v ? pw[v] : a;
-            const float pk = __shfl(a, ((k >> 2) & 1) * 32 + lq, 64);
-            if (sees >> k & 1) {
-              const int sw = D == 128 ? k & 3 : (k >> 1) & 1;
-#pragma unroll
-              for (int mb = 0; mb < D / 32; ++mb)
-#pragma unroll
-                for (int c = 0; c < 4; ++c) {
-                  // columns 32 mb + 8 c + 4 hi .. + 3: half of chunk 4 mb + c
-                  const uint16_t* x = reinterpret_cast<const uint16_t*>(vl + k * RB + (((4 * mb + c) ^ (4 * sw)) * 16) + 8 * hi);
-#pragma unroll
-                  for (int e = 0; e < 4; ++e) o[mb][4 * c + e] = fmaf(pk, bf2f(x[e]), o[mb][4 * c + e]);
-                }
-            }
+                for (int e = 0; e < 4; ++e) o[mb][4 * c + e] = fmaf(pk, bf2f(x[e]), o[mb][4 * c + e]);
+              }
           }
-          __syncthreads();  // everyone has read them (loose is the block's)
-          for (int u = threadIdx.x; u < TC * 64; u += VG * 64)
-            if (loose >> (u / CH) & 1) st16(vl + 16 * u, make_uint4(0, 0, 0, 0));
-          __syncthreads();
         }
-#pragma unroll
-        for (int k2 = 0; k2 < 2; ++k2)
-#pragma unroll
-          for (int mb = 0; mb < D / 32; ++mb) {
-            const uint8_t* at = vl + 16 * k2 * RB + (vrd ^ (mb << 6));
-            const v4s lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4s)(at));
-            const v4s up = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4s)(at + 8 * RB));
-            const bf16x8 va = __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, up, 0, 1, 2, 3, 4, 5, 6, 7));
-            o[mb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(va, pv[k2], o[mb], 0, 0, 0);
-          }
+        take_out(t, loose);
+      }
+      products_o(vl, pb);
+      if (t + 1 < n) products(kn, s);
+    };
+
+    if (pool) meet(n >= NB ? NB - 1 : 0);
+    if (pool && busy) {
+      f32x16 sa[2];
+      products(k_ring, sa);
+      int t = 0;
+      for (; t < plain; t += 2) {
+        f32x16 sb[2];
+        plain_step(t, sa, sb);
+        plain_step(t + 1, sb, sa);
+      }
+      for (; t < n; ++t) other_step(t, sa);
+    } else if (pool) {
+      // a wave without vectors takes part in the copies and the block's meetings
+      for (int t = 0; t < n; ++t) {
+        uint64_t held;
+        begin(t);
+        if (!is_edge(t, held)) continue;
+        const uint64_t loose = clean(t, held);
+        if (loose) take_out(t, loose);
       }
     }
     ls += __shfl_xor(ls, 32, 64);
@@ -719,11 +878,7 @@ TreeCut tree_cut(int batch, int max_q, int max_kv, int hq, int hkv) {
     c.kt = kNW * kNT;
     c.tiles = 1;
   } else {
-    const int64_t groups = (vectors + 31) / 32;
-    const int64_t tiles = (groups + 7) / 8;
-    int vg = (int)((groups + tiles - 1) / tiles);
-    if (vg == 7) vg = 8;
-    c.vt = 32 * vg;
+    c.vt = vectors <= 64 ? 64 : vectors <= 128 ? 128 : 256;
     c.kt = kWT;
     c.tiles = (int)((vectors + c.vt - 1) / c.vt);
   }
@@ -731,7 +886,7 @@ TreeCut tree_cut(int batch, int max_q, int max_kv, int hq, int hkv) {
   const int64_t all = (int64_t)batch * hkv * c.tiles * steps;
   // short units are taken whole; else as many blocks as run at once, with 4 steps each at least
   c.blocks = 0;
-  if (steps > 8) c.blocks = (int)std::max<int64_t>(std::min<int64_t>(c.vt > 128 ? 256 : 512, all / 4), 1);
+  if (steps > 8) c.blocks = (int)std::max<int64_t>(std::min<int64_t>(c.vt == 256 ? 256 : 512, all / 4), 1);
   return c;
 }
 
@@ -770,14 +925,11 @@ hipError_t launch_bf16(const TreeAttn& p, void* workspace, hipStream_t stream) {
     if (tiny) tree_attn_wide_kernel<D, VG, true><<<grid, VG * 64, 0, stream>>>(p, c, ws, lg);   \
     else tree_attn_wide_kernel<D, VG, false><<<grid, VG * 64, 0, stream>>>(p, c, ws, lg);       \
     break
-  if (c.vt == 16 && c.kt == kNW * kNT) QCF_NARROW(1);
-  else if (c.kt == kNW * kNT) QCF_NARROW(2);
+  if (c.vt == 16) QCF_NARROW(1);
+  else if (c.vt == 32) QCF_NARROW(2);
   else switch (c.vt / 32) {
     QCF_WIDE(2);
-    QCF_WIDE(3);
     QCF_WIDE(4);
-    QCF_WIDE(5);
-    QCF_WIDE(6);
     QCF_WIDE(8);
   }
 #undef QCF_WIDE
