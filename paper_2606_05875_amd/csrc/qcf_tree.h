@@ -2,7 +2,7 @@
 // request's own new rows a row sees.
 //
 // A unit is a tile of query vectors (rows times the heads that share a KV head) of one request and KV
-// head; its work is one step per kt tokens of the request.  Where every block takes one unit there is
+// head; its work is one step per 64 tokens of the request.  Where every block takes one unit there is
 // nothing to plan.  Else the steps of all units, laid end to end (request, KV head, tile), are shared
 // evenly over a fixed number of blocks, whatever the requests' lengths: a block takes its share unit by
 // unit, and a unit that is cut between blocks is merged from float32 partial results.  A block has at most
@@ -13,9 +13,10 @@
 
 namespace qcf {
 
+constexpr int kTreeStep = 64;  // tokens per step
+
 struct TreeCut {
-  int vt;      // query vectors per unit
-  int kt;      // tokens per step
+  int vt_log2; // query vectors per unit
   int blocks;  // blocks that share the steps, 0: one block per unit
   int tiles;   // units of the longest request per KV head
 };
@@ -59,14 +60,34 @@ __device__ __forceinline__ TreeRequest tree_request_uni(const TreeAttn& p, int b
   return q;
 }
 
-__device__ __forceinline__ int tree_tiles(const TreeRequest& q, int lg, int vt) {
-  return (int)((((int64_t)q.rows << lg) + vt - 1) / vt);
+__device__ __forceinline__ int tree_tiles(const TreeRequest& q, int lg, const TreeCut& cut) {
+  return (int)((((int64_t)q.rows << lg) + (1 << cut.vt_log2) - 1) >> cut.vt_log2);
 }
 // steps of one unit: at least one, for the rows that see nothing are written too
-__device__ __forceinline__ int tree_steps(const TreeRequest& q, int kt) { return max((q.end + kt - 1) / kt, 1); }
+__device__ __forceinline__ int tree_steps(const TreeRequest& q) {
+  return (int)max(((int64_t)q.end + kTreeStep - 1) / kTreeStep, (int64_t)1);
+}
 
-// The first step of block x's share of n
-__device__ __forceinline__ int64_t tree_share(int64_t n, int x, int blocks) { return n * x / blocks; }
+// n / d for n >= 0, d > 0, by the short division where it does
+__device__ __forceinline__ int64_t quotient(int64_t n, int d) {
+  return (uint64_t)n >> 32 ? n / d : (int64_t)((uint32_t)n / (uint32_t)d);
+}
+
+// How `all` steps are shared: the first `more` blocks take size + 1, the others size
+struct TreeShares {
+  int64_t size;
+  int more;
+  __device__ __forceinline__ TreeShares(int64_t all, int blocks) {
+    size = quotient(all, blocks);
+    more = (int)(all - size * blocks);
+  }
+  __device__ __forceinline__ int64_t first(int x) const { return size * x + min(x, more); }
+  // the block whose share holds step s
+  __device__ __forceinline__ int holder(int64_t s) const {
+    const int64_t cut = (size + 1) * more;  // (size + 1 <= 2^31: a unit has fewer than 2^31 steps)
+    return s < cut ? (int)quotient(s, (int)(size + 1)) : more + (int)quotient(s - cut, (int)size);
+  }
+};
 
 // Blocks in an order that gives each of the 8 XCDs (blocks go to them in turn) consecutive shares:
 // tiles of one request and KV head read the same keys.
@@ -89,7 +110,7 @@ __device__ __forceinline__ void tree_walk(const TreeAttn& p, const TreeCut& cut,
     const int tile = rest % cut.tiles;
     b = rest / cut.tiles;
     q = tree_request_uni(p, b);
-    const int tiles = tree_tiles(q, lg, cut.vt), steps = tree_steps(q, cut.kt);
+    const int tiles = tree_tiles(q, lg, cut), steps = tree_steps(q);
     if (tile >= tiles) return;
     before = 0;
     c = (int64_t)p.hkv * tiles * steps;
@@ -98,13 +119,18 @@ __device__ __forceinline__ void tree_walk(const TreeAttn& p, const TreeCut& cut,
   } else {
     __shared__ int64_t sum_l[NT + 1];  // steps before each thread's requests
     __shared__ int64_t wave_l[NT / 64];
+    __shared__ int4 req_l[NT];         // its first request
     const int tid = threadIdx.x, lane = tid & 63;
     const int per = (p.batch + NT - 1) / NT;
     auto cost = [&](const TreeRequest& r) {
-      return (int64_t)p.hkv * tree_tiles(r, lg, cut.vt) * tree_steps(r, cut.kt);
+      return (int64_t)p.hkv * tree_tiles(r, lg, cut) * tree_steps(r);
     };
     int64_t own = 0;
-    for (int i = tid * per; i < min((tid + 1) * per, p.batch); ++i) own += cost(tree_request(p, i));
+    for (int i = tid * per; i < min((tid + 1) * per, p.batch); ++i) {
+      const TreeRequest r = tree_request(p, i);
+      own += cost(r);
+      if (i == tid * per) req_l[tid] = make_int4((int)r.r0, r.rows, r.kv, r.end);
+    }
     int64_t sum = own;
 #pragma unroll
     for (int o = 1; o < 64; o <<= 1) {
@@ -120,24 +146,28 @@ __device__ __forceinline__ void tree_walk(const TreeAttn& p, const TreeCut& cut,
       int64_t at = sum - own;
       for (int i = tid * per; i < min((tid + 1) * per, p.batch); ++i) {
         ws.prefix[i] = at;
-        at += cost(tree_request(p, i));
+        if (per > 1) at += cost(tree_request(p, i));
       }
       if (tid == NT - 1) ws.prefix[p.batch] = sum;
     }
     __syncthreads();
-    const int64_t all = uni(sum_l[NT]);
+    const TreeShares shares(uni(sum_l[NT]), cut.blocks);
     x = tree_block(cut.blocks);
-    s = tree_share(all, x, cut.blocks);
-    share1 = tree_share(all, x + 1, cut.blocks);
+    s = shares.first(x);
+    share1 = shares.first(x + 1);
     if (s >= share1) return;
-    int lo = 0, hi = NT;  // the last thread whose requests start at or before s
-    while (hi - lo > 1) {
-      const int mid = (lo + hi) >> 1;
-      if (uni(sum_l[mid]) <= s) lo = mid; else hi = mid;
-    }
+    // the last thread whose requests start at or before s: each lane looks at one of a wave's
+    int lo = 0;
+#pragma unroll
+    for (int i = 0; i < NT; i += 64) lo += __builtin_popcountll(__ballot(sum_l[i + lane] <= s));
+    lo = max(lo - 1, 0);
     b = lo * per;
     before = uni(sum_l[lo]);
-    q = tree_request_uni(p, b);
+    const int4 r = req_l[lo];
+    q.r0 = uni(r.x);
+    q.rows = uni(r.y);
+    q.kv = uni(r.z);
+    q.end = uni(r.w);
     c = cost(q);
   }
   const int64_t share0 = s;
@@ -145,14 +175,15 @@ __device__ __forceinline__ void tree_walk(const TreeAttn& p, const TreeCut& cut,
     while (before + c <= s) {  // (ends: the requests' costs sum to more than s)
       before += c;
       q = tree_request_uni(p, ++b);
-      c = (int64_t)p.hkv * tree_tiles(q, lg, cut.vt) * tree_steps(q, cut.kt);
+      c = (int64_t)p.hkv * tree_tiles(q, lg, cut) * tree_steps(q);
     }
-    const int steps = tree_steps(q, cut.kt), tiles = tree_tiles(q, lg, cut.vt);
-    const int64_t u = (s - before) / steps;
+    const int steps = tree_steps(q), tiles = tree_tiles(q, lg, cut);
+    const int64_t u = quotient(s - before, steps);
     const int first = (int)(s - before - u * steps);
     const int n = (int)min((int64_t)(steps - first), share1 - s);
     const int slot = n == steps ? -1 : 2 * x + (s - first < share0 ? 0 : 1);
-    unit(b, q, (int)(u / tiles), (int)(u % tiles), first, n, steps, slot);
+    const int g = (int)quotient(u, tiles);
+    unit(b, q, g, (int)(u - (int64_t)g * tiles), first, n, steps, slot);
     s += n;
   }
 }

@@ -79,6 +79,7 @@ __device__ __forceinline__ int64_t slot_of(const TreeAttn& p, int b, int t, int 
 // ---------------------------------------------------------------------------
 constexpr int kNW = 4;   // waves
 constexpr int kNT = 16;  // tokens per wave and step
+static_assert(kNW * kNT == kTreeStep, "a block's waves take a step's tokens");
 
 template <int D, int NV, bool kTiny>
 __global__ __launch_bounds__(kNW * 64, 2) void tree_attn_narrow_kernel(TreeAttn p, TreeCut cut, TreeWs ws, int lg) {
@@ -136,12 +137,6 @@ __global__ __launch_bounds__(kNW * 64, 2) void tree_attn_narrow_kernel(TreeAttn 
 #pragma unroll
       for (int st = 0; st < ST; ++st) qf[c][st] = as_bf16x8(ld16(q + 32 * st));
     }
-    // Q has to be there before the loop: a wait for it inside would count the copies in flight
-#pragma unroll
-    for (int c = 0; c < NV; ++c)
-#pragma unroll
-      for (int st = 0; st < ST; ++st) asm volatile("" : "+v"(qf[c][st]));
-
     f32x4 o[NV][MB];
     float m[NV], ls[NV];  // running maximum in log2 units, this lane's part of the sum
     bool big[NV];
@@ -182,6 +177,12 @@ __global__ __launch_bounds__(kNW * 64, 2) void tree_attn_narrow_kernel(TreeAttn 
     const bool pool = p.n_pages > 0 && (kTiny || p.page_log2 >= 4);
     int page = page_at(0), page1 = page_at(1);
     if (pool) copy_tile(t_first, page, 0);
+    // Q has to be there before the loop (and comes with the first tile): a wait for it inside would
+    // count the copies in flight
+#pragma unroll
+    for (int c = 0; c < NV; ++c)
+#pragma unroll
+      for (int st = 0; st < ST; ++st) asm volatile("" : "+v"(qf[c][st]));
     for (int i = 0; i < n && pool; ++i) {
       const int t0 = t_first + i * kHop;
       asm volatile("" ::: "memory");
@@ -272,7 +273,9 @@ __global__ __launch_bounds__(kNW * 64, 2) void tree_attn_narrow_kernel(TreeAttn 
           const int k = __builtin_ctz(left);
 #pragma unroll
           for (int c = 0; c < NV; ++c) {
-            const float a = k & 2 ? (k & 1 ? pw[c][3] : pw[c][2]) : (k & 1 ? pw[c][1] : pw[c][0]);
+            float a = 0.f;
+#pragma unroll
+            for (int r = 0; r < 4; ++r) a = (k & 3) == r ? pw[c][r] : a;
             const float pk = __shfl(a, (k >> 2) * 16 + ln, 64);
             if (sees[c] >> k & 1) {
               const int sw = D == 128 ? k & 7 : (k >> 1) & 3;
@@ -356,7 +359,7 @@ __global__ __launch_bounds__(kNW * 64, 2) void tree_attn_narrow_kernel(TreeAttn 
 // ---------------------------------------------------------------------------
 // wide
 // ---------------------------------------------------------------------------
-constexpr int kWT = 64;  // tokens per step
+constexpr int kWT = kTreeStep;
 // Stages of the K and V rings.  A block of 8 waves is alone on its CU and takes most of its LDS, smaller
 // ones run two at a time.
 constexpr int wide_stages(int d, int vg) { return (vg == 8 ? 4 : 2) * (d == 64 ? 2 : 1); }
@@ -434,6 +437,28 @@ __global__ __launch_bounds__(VG * 64, VG == 2 ? 1 : 2) void tree_attn_wide_kerne
     };
     const std::true_type K{};
     const std::false_type V{};
+    const int v0 = tile * VT + 32 * w;
+    const int idx = (v0 + lq) >> lg;
+    const int head = (g << lg) + ((v0 + lq) & ((1 << lg) - 1));
+    const bool valid = idx < rq.rows;
+    const bool busy = (v0 >> lg) < rq.rows;  // (the wave has a vector)
+    const int64_t row = rq.r0 + min(idx, rq.rows - 1);
+    bf16x8 qreg[D / 16];
+    {
+      const uint16_t* q = static_cast<const uint16_t*>(p.q) + (row * p.hq + head) * D + 8 * hi;
+#pragma unroll
+      for (int st = 0; st < D / 16; ++st) qreg[st] = as_bf16x8(ld16(q + 16 * st));
+    }
+    // pages that are not there are rare: looked for once (by every wave), then tile by tile
+    bool bad = kTiny;
+    if (!kTiny && pool) {
+      const int lp = p.page_log2;
+      const int p1 = (int)(((int64_t)min(t_first + n * kWT, rq.end) + (1 << lp) - 1) >> lp);
+      for (int i = (t_first >> lp) + l; i < p1; i += 64) {
+        const int x = i < p.max_pages ? p.block_table[b * p.table_stride + i] : -1;
+        bad = bad || x < 0 || x >= p.n_pages;
+      }
+    }
     // K(0); then K(t + 1), V(t), in this order to the end
     int page[WG], pagev[WG];  // of the next K to be copied, of the next V
     if (pool) {
@@ -456,31 +481,7 @@ __global__ __launch_bounds__(VG * 64, VG == 2 ? 1 : 2) void tree_attn_wide_kerne
         page[k] = page_at(NB, k);
       }
     }
-    // pages that are not there are rare: looked for once, then tile by tile
-    bool holes = kTiny;
-    if (!kTiny && pool) {
-      const int lp = p.page_log2, p0 = t_first >> lp;
-      const int p1 = min((min(t_first + n * kWT, rq.end) + (1 << lp) - 1) >> lp, (int)INT32_MAX);
-      bool bad = false;
-      for (int i = p0 + (int)threadIdx.x; i < p1; i += VG * 64) {
-        const int x = i < p.max_pages ? p.block_table[b * p.table_stride + i] : -1;
-        bad = bad || x < 0 || x >= p.n_pages;
-      }
-      holes = __syncthreads_or(bad);
-    }
-
-    const int v0 = tile * VT + 32 * w;
-    const int idx = (v0 + lq) >> lg;
-    const int head = (g << lg) + ((v0 + lq) & ((1 << lg) - 1));
-    const bool valid = idx < rq.rows;
-    const bool busy = (v0 >> lg) < rq.rows;  // (the wave has a vector)
-    const int64_t row = rq.r0 + min(idx, rq.rows - 1);
-    bf16x8 qreg[D / 16];
-    {
-      const uint16_t* q = static_cast<const uint16_t*>(p.q) + (row * p.hq + head) * D + 8 * hi;
-#pragma unroll
-      for (int st = 0; st < D / 16; ++st) qreg[st] = as_bf16x8(ld16(q + 16 * st));
-    }
+    const bool holes = __ballot(bad) != 0;
     // Q has to be there before the loop: a wait for it inside would count the copies in flight
 #pragma unroll
     for (int st = 0; st < D / 16; ++st) asm volatile("" : "+v"(qreg[st]));
@@ -763,52 +764,76 @@ __device__ __forceinline__ void store4(uint16_t* p, const float4& a) {
 }
 __device__ __forceinline__ void store4(float* p, const float4& a) { *reinterpret_cast<float4*>(p) = a; }
 
-// The partial results of a unit that is cut between blocks, in the blocks' order.  D / 4 lanes take one
-// row and head; those whose unit one block took whole have nothing to do.
-constexpr int kMergeThreads = 256;
+// The partial results of a unit that is cut between blocks, in the blocks' order: one wave per row and
+// head (those whose unit one block took whole have nothing to do).  Lane j first takes the maximum and sum of
+// partial j, then 64 / (D / 4) partials at a time are read and summed, whose sums meet at the end.
+// Bound: latency (three loads that wait for each other), or the partials' bytes.
+constexpr int kMergeWaves = 4;
 template <typename T, int D>
-__global__ __launch_bounds__(kMergeThreads) void tree_attn_merge_kernel(TreeAttn p, TreeCut cut, TreeWs ws, int lg) {
-  constexpr int LPR = D / 4, RPB = kMergeThreads / LPR;
-  const int l = threadIdx.x % LPR;
-  const int64_t item = (int64_t)blockIdx.x * RPB + threadIdx.x / LPR;
-  const int h = (int)(item % p.hq);
-  const int64_t bi = item / p.hq;
-  const int i = (int)(bi % p.max_q);
-  if (bi / p.max_q >= p.batch) return;
-  const int b = (int)(bi / p.max_q);
+__global__ __launch_bounds__(kMergeWaves * 64) void tree_attn_merge_kernel(TreeAttn p, TreeCut cut, TreeWs ws, int lg) {
+  constexpr int LPR = D / 4, RPW = 64 / LPR, U = 8;
+  const int l = threadIdx.x & 63, lc = l % LPR, lr = l / LPR;
+  const int64_t item = (int64_t)blockIdx.x * kMergeWaves + uni((int)threadIdx.x >> 6);
+  const int64_t bi = quotient(item, p.hq);
+  const int h = (int)(item - bi * p.hq);
+  const int b = (int)quotient(bi, p.max_q), i = (int)(bi - (int64_t)b * p.max_q);
+  if (b >= p.batch) return;
+  const int64_t all = ws.prefix[p.batch], start = ws.prefix[b];
   const TreeRequest q = tree_request(p, b);
   if (i >= q.rows) return;
   const int g = h >> lg, vec = (i << lg) + (h & ((1 << lg) - 1));
-  const int steps = tree_steps(q, cut.kt);
-  const int64_t all = ws.prefix[p.batch];
-  const int64_t u0 = ws.prefix[b] + (int64_t)(g * tree_tiles(q, lg, cut.vt) + vec / cut.vt) * steps, u1 = u0 + steps;
-  // the block whose share holds step u0
-  int x = (int)(u0 * cut.blocks / all);
-  while (x > 0 && tree_share(all, x, cut.blocks) > u0) --x;
-  while (tree_share(all, x + 1, cut.blocks) <= u0) ++x;
-  if (tree_share(all, x + 1, cut.blocks) >= u1) return;
+  const int tile = vec >> cut.vt_log2, v = vec - (tile << cut.vt_log2);
+  const int steps = tree_steps(q);
+  const int64_t u0 = start + (int64_t)(g * tree_tiles(q, lg, cut) + tile) * steps, u1 = u0 + steps;
+  const TreeShares shares(all, cut.blocks);
+  const int x0 = uni(shares.holder(u0)), x1 = uni(shares.holder(u1 - 1));
+  if (x0 == x1) return;
+  // (blocks between the two have a share: one that is empty has the ones behind it empty too)
+  auto slot = [&](int x) {
+    return ((int64_t)(2 * x + (x == x0 && shares.first(x) <= u0 ? 1 : 0)) << cut.vt_log2) + v;
+  };
+  const float4* part = reinterpret_cast<const float4*>(ws.o);
   float mx = -INFINITY, lt = 0.f;
   float4 a = make_float4(0.f, 0.f, 0.f, 0.f);
-  for (; x < cut.blocks; ++x) {
-    const int64_t s0 = tree_share(all, x, cut.blocks), s1 = tree_share(all, x + 1, cut.blocks);
-    if (s0 >= u1) break;
-    if (s0 == s1) continue;
-    const int64_t at = (int64_t)(2 * x + (u0 < s0 ? 0 : 1)) * cut.vt + vec % cut.vt;
-    const float2 ml = ws.ml[at];
-    const float4 o = reinterpret_cast<const float4*>(ws.o)[at * LPR + l];
-    const float mn = fmaxf(mx, ml.x);
-    const float fa = __builtin_amdgcn_exp2f(mx - finite(mn)), fo = __builtin_amdgcn_exp2f(ml.x - finite(mn));
-    a.x = a.x * fa + o.x * fo;
-    a.y = a.y * fa + o.y * fo;
-    a.z = a.z * fa + o.z * fo;
-    a.w = a.w * fa + o.w * fo;
-    lt = lt * fa + ml.y * fo;
+  for (int xb = x0; xb <= x1; xb += 64) {
+    const int n = min(64, x1 - xb + 1);
+    const float2 ml = l < n ? ws.ml[slot(xb + l)] : make_float2(-INFINITY, 0.f);
+    const float mn = fmaxf(mx, wave_max(ml.x));
+    const float f = __builtin_amdgcn_exp2f(ml.x - finite(mn)), fa = __builtin_amdgcn_exp2f(mx - finite(mn));
+    lt = lt * fa + wave_sum(ml.y * f);
     mx = mn;
+    a.x *= fa;
+    a.y *= fa;
+    a.z *= fa;
+    a.w *= fa;
+    for (int j0 = 0; j0 < n; j0 += U * RPW) {
+      float4 o[U];
+#pragma unroll
+      for (int k = 0; k < U; ++k) o[k] = part[slot(xb + min(j0 + k * RPW + lr, n - 1)) * LPR + lc];
+#pragma unroll
+      for (int k = 0; k < U; ++k) {
+        const int j = j0 + k * RPW + lr;
+        const float fo = __shfl(f, min(j, 63), 64);
+        if (j >= n) continue;
+        a.x = fmaf(o[k].x, fo, a.x);
+        a.y = fmaf(o[k].y, fo, a.y);
+        a.z = fmaf(o[k].z, fo, a.z);
+        a.w = fmaf(o[k].w, fo, a.w);
+      }
+    }
+  }
+#pragma unroll
+  for (int m = LPR; m < 64; m <<= 1) {
+    a.x += __shfl_xor(a.x, m, 64);
+    a.y += __shfl_xor(a.y, m, 64);
+    a.z += __shfl_xor(a.z, m, 64);
+    a.w += __shfl_xor(a.w, m, 64);
   }
   const bool none = mx == -INFINITY;
   const float inv = none ? 0.f : 1.f / lt;
   const int64_t at = (q.r0 + i) * p.hq + h;
-  store4(static_cast<T*>(p.out) + at * D + 4 * l, make_float4(a.x * inv, a.y * inv, a.z * inv, a.w * inv));
+  if (lr == 0)
+    store4(static_cast<T*>(p.out) + at * D + 4 * lc, make_float4(a.x * inv, a.y * inv, a.z * inv, a.w * inv));
   if (p.lse && l == 0) p.lse[at] = none ? -INFINITY : (mx + log2f(lt)) * kLn2;
 }
 
@@ -872,21 +897,15 @@ int log2_of(int x) { return __builtin_ctz((unsigned)x); }
 // How a bf16 call is cut, from its bounds (lengths are on the device)
 TreeCut tree_cut(int batch, int max_q, int max_kv, int hq, int hkv) {
   const int64_t vectors = (int64_t)max_q * (hq / hkv);
+  const int vt = vectors <= 16 ? 16 : vectors <= 32 ? 32 : vectors <= 64 ? 64 : vectors <= 128 ? 128 : 256;
   TreeCut c;
-  if (vectors <= 32) {
-    c.vt = vectors <= 16 ? 16 : 32;
-    c.kt = kNW * kNT;
-    c.tiles = 1;
-  } else {
-    c.vt = vectors <= 64 ? 64 : vectors <= 128 ? 128 : 256;
-    c.kt = kWT;
-    c.tiles = (int)((vectors + c.vt - 1) / c.vt);
-  }
-  const int64_t steps = ((int64_t)max_kv + c.kt - 1) / c.kt;
+  c.vt_log2 = log2_of(vt);
+  c.tiles = (int)((vectors + vt - 1) / vt);
+  const int64_t steps = ((int64_t)max_kv + kTreeStep - 1) / kTreeStep;
   const int64_t all = (int64_t)batch * hkv * c.tiles * steps;
   // short units are taken whole; else as many blocks as run at once, with 4 steps each at least
   c.blocks = 0;
-  if (steps > 8) c.blocks = (int)std::max<int64_t>(std::min<int64_t>(c.vt == 256 ? 256 : 512, all / 4), 1);
+  if (steps > 8) c.blocks = (int)std::max<int64_t>(std::min<int64_t>(vt == 256 ? 256 : 512, all / 4), 1);
   return c;
 }
 
@@ -898,8 +917,8 @@ WsLayout ws_layout(const TreeCut& c, int batch, int d) {
   WsLayout w{};
   if (c.blocks == 0) return w;
   w.ml = up(((size_t)batch + 1) * 8);
-  w.o = w.ml + up((size_t)2 * c.blocks * c.vt * 8);
-  w.total = w.o + up((size_t)2 * c.blocks * c.vt * d * 4);
+  w.o = w.ml + up(((size_t)2 * c.blocks << c.vt_log2) * 8);
+  w.total = w.o + up(((size_t)2 * c.blocks << c.vt_log2) * d * 4);
   return w;
 }
 
@@ -925,9 +944,9 @@ hipError_t launch_bf16(const TreeAttn& p, void* workspace, hipStream_t stream) {
     if (tiny) tree_attn_wide_kernel<D, VG, true><<<grid, VG * 64, 0, stream>>>(p, c, ws, lg);   \
     else tree_attn_wide_kernel<D, VG, false><<<grid, VG * 64, 0, stream>>>(p, c, ws, lg);       \
     break
-  if (c.vt == 16) QCF_NARROW(1);
-  else if (c.vt == 32) QCF_NARROW(2);
-  else switch (c.vt / 32) {
+  if (c.vt_log2 == 4) QCF_NARROW(1);
+  else if (c.vt_log2 == 5) QCF_NARROW(2);
+  else switch (1 << (c.vt_log2 - 5)) {
     QCF_WIDE(2);
     QCF_WIDE(4);
     QCF_WIDE(8);
@@ -936,8 +955,8 @@ hipError_t launch_bf16(const TreeAttn& p, void* workspace, hipStream_t stream) {
 #undef QCF_NARROW
   if (c.blocks) {
     const int64_t rows = (int64_t)p.batch * p.max_q * p.hq;
-    const int rpb = kMergeThreads / (D / 4);
-    tree_attn_merge_kernel<uint16_t, D><<<dim3((unsigned)((rows + rpb - 1) / rpb)), kMergeThreads, 0, stream>>>(p, c, ws, lg);
+    tree_attn_merge_kernel<uint16_t, D>
+        <<<dim3((unsigned)((rows + kMergeWaves - 1) / kMergeWaves)), kMergeWaves * 64, 0, stream>>>(p, c, ws, lg);
   }
   return hipGetLastError();
 }
