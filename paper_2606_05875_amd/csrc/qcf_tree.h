@@ -73,19 +73,18 @@ __device__ __forceinline__ int64_t quotient(int64_t n, int d) {
   return (uint64_t)n >> 32 ? n / d : (int64_t)((uint32_t)n / (uint32_t)d);
 }
 
-// How `all` steps are shared: the first `more` blocks take size + 1, the others size
+// How `all` steps are shared: block x begins at floor(all x / blocks), so that equal units that fill a
+// whole number of blocks each are not cut elsewhere
 struct TreeShares {
-  int64_t size;
-  int more;
-  __device__ __forceinline__ TreeShares(int64_t all, int blocks) {
-    size = quotient(all, blocks);
-    more = (int)(all - size * blocks);
-  }
-  __device__ __forceinline__ int64_t first(int x) const { return size * x + min(x, more); }
-  // the block whose share holds step s
+  int64_t all;
+  int blocks;
+  __device__ __forceinline__ int64_t first(int x) const { return quotient(all * x, blocks); }
+  // the block whose share holds step s < all
   __device__ __forceinline__ int holder(int64_t s) const {
-    const int64_t cut = (size + 1) * more;  // (size + 1 <= 2^31: a unit has fewer than 2^31 steps)
-    return s < cut ? (int)quotient(s, (int)(size + 1)) : more + (int)quotient(s - cut, (int)size);
+    int x = all >> 31 ? (int)(s * blocks / all) : (int)quotient(s * blocks, (int)all);
+    while (x > 0 && first(x) > s) --x;
+    while (first(x + 1) <= s) ++x;
+    return x;
   }
 };
 
@@ -151,7 +150,7 @@ __device__ __forceinline__ void tree_walk(const TreeAttn& p, const TreeCut& cut,
       if (tid == NT - 1) ws.prefix[p.batch] = sum;
     }
     __syncthreads();
-    const TreeShares shares(uni(sum_l[NT]), cut.blocks);
+    const TreeShares shares{uni(sum_l[NT]), cut.blocks};
     x = tree_block(cut.blocks);
     s = shares.first(x);
     share1 = shares.first(x + 1);

@@ -352,7 +352,9 @@ __global__ __launch_bounds__(kNW * 64, 2) void tree_attn_narrow_kernel(TreeAttn 
         if (p.lse && i4 == 0) p.lse[at] = none ? -INFINITY : (mx + log2f(lt)) * kLn2;
       }
     }
-    __syncthreads();  // (the next unit's tiles go over them)
+    // everyone has read the results, which the next unit's tiles go over (stores need not be waited for)
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    __builtin_amdgcn_s_barrier();
   });
 }
 
@@ -449,6 +451,11 @@ __global__ __launch_bounds__(VG * 64, VG == 2 ? 1 : 2) void tree_attn_wide_kerne
 #pragma unroll
       for (int st = 0; st < D / 16; ++st) qreg[st] = as_bf16x8(ld16(q + 16 * st));
     }
+    int pages[NB][WG];
+#pragma unroll
+    for (int t = 0; t < NB; ++t)
+#pragma unroll
+      for (int k = 0; k < WG; ++k) pages[t][k] = page_at(t, k);
     // pages that are not there are rare: looked for once (by every wave), then tile by tile
     bool bad = kTiny;
     if (!kTiny && pool) {
@@ -459,32 +466,25 @@ __global__ __launch_bounds__(VG * 64, VG == 2 ? 1 : 2) void tree_attn_wide_kerne
         bad = bad || x < 0 || x >= p.n_pages;
       }
     }
+    const bool holes = __ballot(bad) != 0;
+    // Q has to be there before the copies: a wait for it later would count those in flight
+#pragma unroll
+    for (int st = 0; st < D / 16; ++st) asm volatile("" : "+v"(qreg[st]));
     // K(0); then K(t + 1), V(t), in this order to the end
     int page[WG], pagev[WG];  // of the next K to be copied, of the next V
     if (pool) {
-#pragma unroll
-      for (int k = 0; k < WG; ++k) page[k] = page_at(0, k);
-      copy(K, k_lds, 0, page);
+      copy(K, k_lds, 0, pages[0]);
 #pragma unroll
       for (int t = 1; t < NB; ++t) {
-#pragma unroll
-        for (int k = 0; k < WG; ++k) {
-          pagev[k] = page[k];
-          page[k] = page_at(t, k);
-        }
-        if (t < n) copy(K, k_lds, t, page);
-        if (t <= n) copy(V, v_lds, t - 1, pagev);
+        if (t < n) copy(K, k_lds, t, pages[t]);
+        if (t <= n) copy(V, v_lds, t - 1, pages[t - 1]);
       }
 #pragma unroll
       for (int k = 0; k < WG; ++k) {
-        pagev[k] = page[k];
+        pagev[k] = pages[NB - 1][k];
         page[k] = page_at(NB, k);
       }
     }
-    const bool holes = __ballot(bad) != 0;
-    // Q has to be there before the loop: a wait for it inside would count the copies in flight
-#pragma unroll
-    for (int st = 0; st < D / 16; ++st) asm volatile("" : "+v"(qreg[st]));
     f32x16 o[D / 32];
 #pragma unroll
     for (int mb = 0; mb < D / 32; ++mb) o[mb] = f32x16{};
@@ -617,7 +617,6 @@ __global__ __launch_bounds__(VG * 64, VG == 2 ? 1 : 2) void tree_attn_wide_kerne
     // the tiles before the first that is the last one or has tokens that are not there or not seen by all
     const int plain = holes ? 0 : min(n - 1, (min(rq.kv, rq.end) - t_first) / kWT) & ~1;
     auto plain_step = [&](int t, f32x16 (&s)[2], f32x16 (&sn)[2]) {
-      begin(t);
       bf16x8 pb[2][2];
       maximum(s);
       __builtin_amdgcn_s_setprio(1);
@@ -659,7 +658,6 @@ __global__ __launch_bounds__(VG * 64, VG == 2 ? 1 : 2) void tree_attn_wide_kerne
     // any step, its next S (into s) after it
     auto other_step = [&](int t, f32x16 (&s)[2]) {
       const int t0 = t_first + t * kWT;
-      begin(t);
       const uint8_t* kn = k_ring + ((t + 1) & (NB - 1)) * TB;
       const uint8_t* vl = v_ring + (t & (NB - 1)) * TB;
       bf16x8 pb[2][2];
@@ -712,10 +710,15 @@ __global__ __launch_bounds__(VG * 64, VG == 2 ? 1 : 2) void tree_attn_wide_kerne
       int t = 0;
       for (; t < plain; t += 2) {
         f32x16 sb[2];
+        begin(t);
         plain_step(t, sa, sb);
+        begin(t + 1);
         plain_step(t + 1, sb, sa);
       }
-      for (; t < n; ++t) other_step(t, sa);
+      for (; t < n; ++t) {
+        begin(t);
+        other_step(t, sa);
+      }
     } else if (pool) {
       // a wave without vectors takes part in the copies and the block's meetings
       for (int t = 0; t < n; ++t) {
@@ -752,7 +755,9 @@ __global__ __launch_bounds__(VG * 64, VG == 2 ? 1 : 2) void tree_attn_wide_kerne
         if (p.lse && hi == 0) p.lse[at] = none ? -INFINITY : (m + log2f(ls)) * kLn2;
       }
     }
-    __syncthreads();  // (the next unit's tiles go over these)
+    // everyone has read its tiles, which the next unit's go over (stores need not be waited for)
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    __builtin_amdgcn_s_barrier();
   });
 }
 
@@ -785,19 +790,19 @@ __global__ __launch_bounds__(kMergeWaves * 64) void tree_attn_merge_kernel(TreeA
   const int tile = vec >> cut.vt_log2, v = vec - (tile << cut.vt_log2);
   const int steps = tree_steps(q);
   const int64_t u0 = start + (int64_t)(g * tree_tiles(q, lg, cut) + tile) * steps, u1 = u0 + steps;
-  const TreeShares shares(all, cut.blocks);
+  const TreeShares shares{all, cut.blocks};
   const int x0 = uni(shares.holder(u0)), x1 = uni(shares.holder(u1 - 1));
   if (x0 == x1) return;
-  // (blocks between the two have a share: one that is empty has the ones behind it empty too)
-  auto slot = [&](int x) {
-    return ((int64_t)(2 * x + (x == x0 && shares.first(x) <= u0 ? 1 : 0)) << cut.vt_log2) + v;
-  };
+  auto slot = [&](int x) { return ((int64_t)(2 * x + (x == x0 ? 1 : 0)) << cut.vt_log2) + v; };
   const float4* part = reinterpret_cast<const float4*>(ws.o);
   float mx = -INFINITY, lt = 0.f;
   float4 a = make_float4(0.f, 0.f, 0.f, 0.f);
   for (int xb = x0; xb <= x1; xb += 64) {
     const int n = min(64, x1 - xb + 1);
-    const float2 ml = l < n ? ws.ml[slot(xb + l)] : make_float2(-INFINITY, 0.f);
+    // (blocks between the two can have no share where there are fewer steps than blocks)
+    const bool live = l < n && (all >= cut.blocks || shares.first(xb + l) < shares.first(xb + l + 1));
+    const uint64_t lives = __ballot(live);
+    const float2 ml = live ? ws.ml[slot(xb + l)] : make_float2(-INFINITY, 0.f);
     const float mn = fmaxf(mx, wave_max(ml.x));
     const float f = __builtin_amdgcn_exp2f(ml.x - finite(mn)), fa = __builtin_amdgcn_exp2f(mx - finite(mn));
     lt = lt * fa + wave_sum(ml.y * f);
@@ -814,7 +819,7 @@ __global__ __launch_bounds__(kMergeWaves * 64) void tree_attn_merge_kernel(TreeA
       for (int k = 0; k < U; ++k) {
         const int j = j0 + k * RPW + lr;
         const float fo = __shfl(f, min(j, 63), 64);
-        if (j >= n) continue;
+        if (j >= n || !(lives >> j & 1)) continue;
         a.x = fmaf(o[k].x, fo, a.x);
         a.y = fmaf(o[k].y, fo, a.y);
         a.z = fmaf(o[k].z, fo, a.z);
