@@ -5,8 +5,10 @@
 // head; its work is one step per 64 tokens of the request.  Where every block takes one unit there is
 // nothing to plan.  Else the steps of all units, laid end to end (request, KV head, tile), are shared
 // evenly over a fixed number of blocks, whatever the requests' lengths: a block takes its share unit by
-// unit, and a unit that is cut between blocks is merged from float32 partial results.  A block has at most
-// two of them, at the start and at the end of its share (slots 2 x and 2 x + 1).
+// unit, and a unit that is cut between blocks is merged from float32 partial results.  Beginning and
+// ending a unit costs a block about as much as `start` steps, which stand before each unit's own in the
+// shares.  A block has at most two partial results: of a unit that others began (slot 2 x) and of one
+// that it begins (slot 2 x + 1).
 #pragma once
 #include "qcf_decode_launch.h"
 #include "qcf_device.h"
@@ -18,12 +20,13 @@ constexpr int kTreeStep = 64;  // tokens per step
 struct TreeCut {
   int vt_log2; // query vectors per unit
   int blocks;  // blocks that share the steps, 0: one block per unit
+  int start;   // what beginning a unit counts as, in steps
   int tiles;   // units of the longest request per KV head
 };
 
-// The workspace of a cut call: prefix[b] is the number of steps before request b
+// The workspace of a cut call
 struct TreeWs {
-  int64_t* prefix;   // [batch + 1]
+  int2* held;        // [batch][hkv][tiles]: the blocks that hold a unit's first and last step
   float2* ml;        // [2 * blocks][vt] running maximum (log2 units) and sum
   float* o;          // [2 * blocks][vt][d]
 };
@@ -74,10 +77,14 @@ __device__ __forceinline__ int64_t quotient(int64_t n, int d) {
 }
 
 // How `all` steps are shared: block x begins at floor(all x / blocks), so that equal units that fill a
-// whole number of blocks each are not cut elsewhere
+// whole number of blocks each are not cut elsewhere.  A share is four steps or more.
 struct TreeShares {
   int64_t all;
   int blocks;
+  __device__ __forceinline__ TreeShares(int64_t steps, int most) : all(steps) {
+    const int n = (int)min((int64_t)most, steps >> 2);
+    blocks = max(n >= 64 ? n & ~7 : n, 1);
+  }
   __device__ __forceinline__ int64_t first(int x) const { return quotient(all * x, blocks); }
   // the block whose share holds step s < all
   __device__ __forceinline__ int holder(int64_t s) const {
@@ -86,14 +93,12 @@ struct TreeShares {
     while (first(x + 1) <= s) ++x;
     return x;
   }
+  // The block at place i of the grid, in an order that gives each of the 8 XCDs (blocks go to them in
+  // turn) consecutive shares: tiles of one request and KV head read the same keys.
+  __device__ __forceinline__ int block(int i) const {
+    return blocks % 8 == 0 ? (i & 7) * (blocks >> 3) + (i >> 3) : i;
+  }
 };
-
-// Blocks in an order that gives each of the 8 XCDs (blocks go to them in turn) consecutive shares:
-// tiles of one request and KV head read the same keys.
-__device__ __forceinline__ int tree_block(int blocks) {
-  const int x = blockIdx.x;
-  return blocks % 8 == 0 ? (x & 7) * (blocks >> 3) + (x >> 3) : x;
-}
 
 // Runs `unit(b, request, g, tile, first, n, steps, slot)` for this block's share: steps first .. first+n-1
 // of a unit's `steps`, to be written out whole (slot < 0) or as a partial result.  NT threads.
@@ -102,7 +107,7 @@ __device__ __forceinline__ void tree_walk(const TreeAttn& p, const TreeCut& cut,
                                           F&& unit) {
   int b;
   TreeRequest q;
-  int64_t before, c, s, share1;  // steps before request b, its own; the share's next and last
+  int64_t before, s, share1, all = 0;  // steps before request b; the share's next and end; of all requests
   int x = 0;
   if (cut.blocks == 0) {
     const int g = blockIdx.x % p.hkv, rest = blockIdx.x / p.hkv;
@@ -112,7 +117,6 @@ __device__ __forceinline__ void tree_walk(const TreeAttn& p, const TreeCut& cut,
     const int tiles = tree_tiles(q, lg, cut), steps = tree_steps(q);
     if (tile >= tiles) return;
     before = 0;
-    c = (int64_t)p.hkv * tiles * steps;
     s = (int64_t)(g * tiles + tile) * steps;
     share1 = s + steps;
   } else {
@@ -122,7 +126,7 @@ __device__ __forceinline__ void tree_walk(const TreeAttn& p, const TreeCut& cut,
     const int tid = threadIdx.x, lane = tid & 63;
     const int per = (p.batch + NT - 1) / NT;
     auto cost = [&](const TreeRequest& r) {
-      return (int64_t)p.hkv * tree_tiles(r, lg, cut) * tree_steps(r);
+      return (int64_t)p.hkv * tree_tiles(r, lg, cut) * (tree_steps(r) + cut.start);
     };
     int64_t own = 0;
     for (int i = tid * per; i < min((tid + 1) * per, p.batch); ++i) {
@@ -141,20 +145,12 @@ __device__ __forceinline__ void tree_walk(const TreeAttn& p, const TreeCut& cut,
     for (int i = 0; i < tid >> 6; ++i) sum += wave_l[i];
     sum_l[tid] = sum - own;
     if (tid == NT - 1) sum_l[NT] = sum;
-    if (blockIdx.x == 0) {
-      int64_t at = sum - own;
-      for (int i = tid * per; i < min((tid + 1) * per, p.batch); ++i) {
-        ws.prefix[i] = at;
-        if (per > 1) at += cost(tree_request(p, i));
-      }
-      if (tid == NT - 1) ws.prefix[p.batch] = sum;
-    }
     __syncthreads();
-    const TreeShares shares{uni(sum_l[NT]), cut.blocks};
-    x = tree_block(cut.blocks);
+    const TreeShares shares(uni(sum_l[NT]), cut.blocks);
+    if ((int)blockIdx.x >= shares.blocks || shares.all == 0) return;
+    x = shares.block(blockIdx.x);
     s = shares.first(x);
     share1 = shares.first(x + 1);
-    if (s >= share1) return;
     // the last thread whose requests start at or before s: each lane looks at one of a wave's
     int lo = 0;
 #pragma unroll
@@ -167,23 +163,30 @@ __device__ __forceinline__ void tree_walk(const TreeAttn& p, const TreeCut& cut,
     q.rows = uni(r.y);
     q.kv = uni(r.z);
     q.end = uni(r.w);
-    c = cost(q);
+    all = shares.all;
   }
-  const int64_t share0 = s;
+  const int start = cut.blocks ? cut.start : 0;
   while (s < share1) {
-    while (before + c <= s) {  // (ends: the requests' costs sum to more than s)
-      before += c;
-      q = tree_request_uni(p, ++b);
-      c = (int64_t)p.hkv * tree_tiles(q, lg, cut) * tree_steps(q);
-    }
     const int steps = tree_steps(q), tiles = tree_tiles(q, lg, cut);
-    const int64_t u = quotient(s - before, steps);
-    const int first = (int)(s - before - u * steps);
-    const int n = (int)min((int64_t)(steps - first), share1 - s);
-    const int slot = n == steps ? -1 : 2 * x + (s - first < share0 ? 0 : 1);
-    const int g = (int)quotient(u, tiles);
-    unit(b, q, g, (int)(u - (int64_t)g * tiles), first, n, steps, slot);
-    s += n;
+    const int64_t cq = (int64_t)p.hkv * tiles * (steps + start);
+    if (before + cq <= s) {  // (ends: the requests' costs sum to more than s)
+      before += cq;
+      q = tree_request_uni(p, ++b);
+      continue;
+    }
+    const int64_t u = quotient(s - before, steps + start), u0 = before + u * (steps + start);
+    const int64_t to = min(u0 + start + steps, share1);
+    const int first = (int)max(s - u0 - start, (int64_t)0), n = (int)(to - u0 - start) - first;
+    if (n > 0) {
+      const int g = (int)quotient(u, tiles), tile = (int)(u - (int64_t)g * tiles);
+      if (cut.blocks && first == 0 && threadIdx.x == 0) {
+        const TreeShares shares(all, cut.blocks);
+        ws.held[((int64_t)b * p.hkv + g) * cut.tiles + tile] =
+            make_int2(x, n == steps ? x : shares.holder(u0 + start + steps - 1));
+      }
+      unit(b, q, g, tile, first, n, steps, n == steps ? -1 : 2 * x + (first > 0 ? 0 : 1));
+    }
+    s = to;
   }
 }
 

@@ -10,7 +10,7 @@
 //  narrow  up to 32 query vectors per request and KV head (one token, short chains).  Bound: HBM.  Four
 //          waves take 16-token tiles in turn, each on its own (two stages of LDS, no barrier in the loop),
 //          v_mfma_f32_16x16x32/16x16x16_bf16; their results are summed through LDS once per unit.
-//  wide    more vectors (trees).  A wave holds 32 of them (v_mfma_f32_32x32x16_bf16) and the 2, 4 or 8
+//  wide    more vectors (trees).  A wave holds 32 of them (v_mfma_f32_32x32x16_bf16) and the 2 or 4
 //          waves of a block share every 64-token tile (a ring of stages, one barrier per tile); the
 //          products of the next tile's S run beside this tile's exponentials.  Bound: HBM
 //          up to about 128 vectors, the matrix units beyond.
@@ -362,9 +362,10 @@ __global__ __launch_bounds__(kNW * 64, 2) void tree_attn_narrow_kernel(TreeAttn 
 // wide
 // ---------------------------------------------------------------------------
 constexpr int kWT = kTreeStep;
-// Stages of the K and V rings.  A block of 8 waves is alone on its CU and takes most of its LDS, smaller
-// ones run two at a time.
-constexpr int wide_stages(int d, int vg) { return (vg == 8 ? 4 : 2) * (d == 64 ? 2 : 1); }
+// Stages of the K and V rings (64 KB, so that a CU holds two blocks, which run beside each other's starts,
+// ends and exponentials: blocks of 8 waves, one per CU, took 106 us against 102 for 64 rows over 32896
+// tokens with 64/8 heads, and 174 against 147 for trees of 8 to 40 rows over 2000 to 12700 tokens)
+constexpr int wide_stages(int d) { return d == 64 ? 4 : 2; }
 
 template <int D, int VG, bool kTiny>
 __global__ __launch_bounds__(VG * 64, VG == 2 ? 1 : 2) void tree_attn_wide_kernel(TreeAttn p, TreeCut cut, TreeWs ws, int lg) {
@@ -373,14 +374,13 @@ __global__ __launch_bounds__(VG * 64, VG == 2 ? 1 : 2) void tree_attn_wide_kerne
   constexpr int RB = D * 2;        // bytes per row
   constexpr int TB = kWT * RB;     // bytes of a tile of K or V
   constexpr int VT = 32 * VG;
-  constexpr int NB = wide_stages(D, VG);
+  constexpr int NB = wide_stages(D);
   // Copies go by groups of 16 rows, which lie in one page: wave w takes groups w, w + VG, .. of the
-  // tile's four, or (8 waves) half of group w / 2
-  constexpr int CPG = 16 / RPC;
-  constexpr int WG = VG >= 4 ? 1 : 4 / VG;      // groups per wave
-  constexpr int WC = VG == 8 ? CPG / 2 : CPG;   // copies of a group per wave, K or V
+  // tile's four
+  constexpr int WC = 16 / RPC;   // copies per group, K or V
+  constexpr int WG = 4 / VG;     // groups per wave
   constexpr int WI = WG * WC;
-  static_assert(VG == 2 || VG == 4 || VG == 8, "groups are shared evenly");
+  static_assert(VG == 2 || VG == 4, "groups are shared evenly");
   __shared__ __attribute__((aligned(1024))) uint8_t k_ring[NB * TB];
   __shared__ __attribute__((aligned(1024))) uint8_t v_ring[NB * TB];
   __shared__ uint32_t loose_l[2];
@@ -396,7 +396,6 @@ __global__ __launch_bounds__(VG * 64, VG == 2 ? 1 : 2) void tree_attn_wide_kerne
   int krd = lq * RB + (hi ^ (ky & 1)) * 16 + (ky >> 1) * 32;
   const int tg = l >> 4, te = (l >> 2) & 3, tq = l & 3;
   const int vrd = (4 * (tg >> 1) + te) * RB + (D == 128 ? te : te >> 1) * 64 + 32 * (tg & 1) + 8 * tq;
-  const int c0 = VG == 8 ? (w & 1) * WC : 0;  // this wave's first copy in a group
   // copy i of a group fills rows RPC i + l / CH: the row within the copy and the chunk of K, V before i's
   // part of the exchange (which i's bits give by themselves)
   const int cr = l / CH, cc = l % CH;
@@ -410,7 +409,7 @@ __global__ __launch_bounds__(VG * 64, VG == 2 ? 1 : 2) void tree_attn_wide_kerne
     const uint16_t* vc = static_cast<const uint16_t*>(p.v_cache) + (int64_t)g * D;
     const bool pool = p.n_pages > 0 && (kTiny || p.page_log2 >= 4);
     const int t_first = first * kWT;
-    auto group = [&](int k) { return VG >= 4 ? w * 4 / VG : w + VG * k; };
+    auto group = [&](int k) { return w + VG * k; };
     auto page_at = [&](int t, int k) {
       return kTiny || t >= n ? -1 : page_of(p, table, t_first + t * kWT + 16 * group(k), rq.end);
     };
@@ -427,13 +426,12 @@ __global__ __launch_bounds__(VG * 64, VG == 2 ? 1 : 2) void tree_attn_wide_kerne
         const int64_t at = page[k] < 0 ? 0 : ((int64_t)page[k] << p.page_log2) + (t0 & ((1 << p.page_log2) - 1));
 #pragma unroll
         for (int i = 0; i < WC; ++i) {
-          const int ci = c0 + i;
-          const uint32_t dst = to + (group(k) * CPG + ci) * 1024;
-          const uint32_t chunk = kK ? kx ^ (ci * 64) : vx;
+          const uint32_t dst = to + (group(k) * WC + i) * 1024;
+          const uint32_t chunk = kK ? kx ^ (i * 64) : vx;
           if (!kTiny)
-            copy16(from + (at + RPC * ci) * p.kv_stride, coff + chunk, dst);
+            copy16(from + (at + RPC * i) * p.kv_stride, coff + chunk, dst);
           else
-            copy16(from + max(slot_of(p, b, t0 + RPC * ci + cr, rq.end), (int64_t)0) * p.kv_stride + chunk / 2, dst);
+            copy16(from + max(slot_of(p, b, t0 + RPC * i + cr, rq.end), (int64_t)0) * p.kv_stride + chunk / 2, dst);
         }
       }
     };
@@ -783,15 +781,12 @@ __global__ __launch_bounds__(kMergeWaves * 64) void tree_attn_merge_kernel(TreeA
   const int h = (int)(item - bi * p.hq);
   const int b = (int)quotient(bi, p.max_q), i = (int)(bi - (int64_t)b * p.max_q);
   if (b >= p.batch) return;
-  const int64_t all = ws.prefix[p.batch], start = ws.prefix[b];
-  const TreeRequest q = tree_request(p, b);
-  if (i >= q.rows) return;
   const int g = h >> lg, vec = (i << lg) + (h & ((1 << lg) - 1));
   const int tile = vec >> cut.vt_log2, v = vec - (tile << cut.vt_log2);
-  const int steps = tree_steps(q);
-  const int64_t u0 = start + (int64_t)(g * tree_tiles(q, lg, cut) + tile) * steps, u1 = u0 + steps;
-  const TreeShares shares{all, cut.blocks};
-  const int x0 = uni(shares.holder(u0)), x1 = uni(shares.holder(u1 - 1));
+  const int2 held = ws.held[((int64_t)b * p.hkv + g) * cut.tiles + tile];
+  const TreeRequest q = tree_request(p, b);
+  if (i >= q.rows) return;
+  const int x0 = uni(held.x), x1 = uni(held.y);
   if (x0 == x1) return;
   auto slot = [&](int x) { return ((int64_t)(2 * x + (x == x0 ? 1 : 0)) << cut.vt_log2) + v; };
   const float4* part = reinterpret_cast<const float4*>(ws.o);
@@ -799,10 +794,7 @@ __global__ __launch_bounds__(kMergeWaves * 64) void tree_attn_merge_kernel(TreeA
   float4 a = make_float4(0.f, 0.f, 0.f, 0.f);
   for (int xb = x0; xb <= x1; xb += 64) {
     const int n = min(64, x1 - xb + 1);
-    // (blocks between the two can have no share where there are fewer steps than blocks)
-    const bool live = l < n && (all >= cut.blocks || shares.first(xb + l) < shares.first(xb + l + 1));
-    const uint64_t lives = __ballot(live);
-    const float2 ml = live ? ws.ml[slot(xb + l)] : make_float2(-INFINITY, 0.f);
+    const float2 ml = l < n ? ws.ml[slot(xb + l)] : make_float2(-INFINITY, 0.f);
     const float mn = fmaxf(mx, wave_max(ml.x));
     const float f = __builtin_amdgcn_exp2f(ml.x - finite(mn)), fa = __builtin_amdgcn_exp2f(mx - finite(mn));
     lt = lt * fa + wave_sum(ml.y * f);
@@ -819,7 +811,7 @@ __global__ __launch_bounds__(kMergeWaves * 64) void tree_attn_merge_kernel(TreeA
       for (int k = 0; k < U; ++k) {
         const int j = j0 + k * RPW + lr;
         const float fo = __shfl(f, min(j, 63), 64);
-        if (j >= n || !(lives >> j & 1)) continue;
+        if (j >= n) continue;
         a.x = fmaf(o[k].x, fo, a.x);
         a.y = fmaf(o[k].y, fo, a.y);
         a.z = fmaf(o[k].z, fo, a.z);
@@ -899,10 +891,12 @@ __global__ __launch_bounds__(256) void tree_attn_f32_kernel(TreeAttn p) {
 
 int log2_of(int x) { return __builtin_ctz((unsigned)x); }
 
+constexpr int kBlocks = 512;  // two per CU
+
 // How a bf16 call is cut, from its bounds (lengths are on the device)
 TreeCut tree_cut(int batch, int max_q, int max_kv, int hq, int hkv) {
   const int64_t vectors = (int64_t)max_q * (hq / hkv);
-  const int vt = vectors <= 16 ? 16 : vectors <= 32 ? 32 : vectors <= 64 ? 64 : vectors <= 128 ? 128 : 256;
+  const int vt = vectors <= 16 ? 16 : vectors <= 32 ? 32 : vectors <= 64 ? 64 : 128;
   TreeCut c;
   c.vt_log2 = log2_of(vt);
   c.tiles = (int)((vectors + vt - 1) / vt);
@@ -910,18 +904,19 @@ TreeCut tree_cut(int batch, int max_q, int max_kv, int hq, int hkv) {
   const int64_t all = (int64_t)batch * hkv * c.tiles * steps;
   // short units are taken whole; else as many blocks as run at once, with 4 steps each at least
   c.blocks = 0;
-  if (steps > 8) c.blocks = (int)std::max<int64_t>(std::min<int64_t>(vt == 256 ? 256 : 512, all / 4), 1);
+  c.start = 4;
+  if (steps > 8) c.blocks = (int)std::max<int64_t>(std::min<int64_t>(kBlocks, all / 4), 1);
   return c;
 }
 
 struct WsLayout {
   size_t ml, o, total;
 };
-WsLayout ws_layout(const TreeCut& c, int batch, int d) {
+WsLayout ws_layout(const TreeCut& c, int batch, int hkv, int d) {
   const auto up = [](size_t x) { return (x + 255) / 256 * 256; };
   WsLayout w{};
   if (c.blocks == 0) return w;
-  w.ml = up(((size_t)batch + 1) * 8);
+  w.ml = up((size_t)batch * hkv * c.tiles * sizeof(int2));
   w.o = w.ml + up(((size_t)2 * c.blocks << c.vt_log2) * 8);
   w.total = w.o + up(((size_t)2 * c.blocks << c.vt_log2) * d * 4);
   return w;
@@ -931,9 +926,9 @@ template <int D>
 hipError_t launch_bf16(const TreeAttn& p, void* workspace, hipStream_t stream) {
   const int lg = log2_of(p.hq / p.hkv);
   const TreeCut c = tree_cut(p.batch, p.max_q, p.max_kv, p.hq, p.hkv);
-  const WsLayout wl = ws_layout(c, p.batch, D);
+  const WsLayout wl = ws_layout(c, p.batch, p.hkv, D);
   char* base = static_cast<char*>(workspace);
-  const TreeWs ws{reinterpret_cast<int64_t*>(base), reinterpret_cast<float2*>(base + wl.ml),
+  const TreeWs ws{reinterpret_cast<int2*>(base), reinterpret_cast<float2*>(base + wl.ml),
                   reinterpret_cast<float*>(base + wl.o)};
   const int64_t blocks = c.blocks ? c.blocks : (int64_t)p.batch * p.hkv * c.tiles;
   if (blocks > 0x7fffffff) return hipErrorInvalidConfiguration;
@@ -954,7 +949,6 @@ hipError_t launch_bf16(const TreeAttn& p, void* workspace, hipStream_t stream) {
   else switch (1 << (c.vt_log2 - 5)) {
     QCF_WIDE(2);
     QCF_WIDE(4);
-    QCF_WIDE(8);
   }
 #undef QCF_WIDE
 #undef QCF_NARROW
@@ -970,7 +964,7 @@ hipError_t launch_bf16(const TreeAttn& p, void* workspace, hipStream_t stream) {
 
 size_t tree_attn_workspace(int batch, int max_q, int max_kv, int hq, int hkv, int head_dim, bool bf16) {
   if (!bf16) return 0;
-  return ws_layout(tree_cut(batch, max_q, max_kv, hq, hkv), batch, head_dim).total;
+  return ws_layout(tree_cut(batch, max_q, max_kv, hq, hkv), batch, hkv, head_dim).total;
 }
 
 hipError_t launch_tree_attn(const TreeAttn& p, bool bf16, int head_dim, void* ws, hipStream_t stream) {
