@@ -62,6 +62,7 @@ struct TreeAttn {
   float scale;
 };
 size_t tree_attn_workspace(int batch, int max_q, int max_kv, int hq, int hkv, int head_dim, bool bf16);
+hipError_t launch_tree_attn_f32(const TreeAttn& p, int head_dim, void* ws, hipStream_t stream);
 hipError_t launch_tree_attn(const TreeAttn& p, bool bf16, int head_dim, void* ws, hipStream_t stream);
 
 struct VerifyDrafts {

@@ -10,6 +10,10 @@
 // shares.  A block has at most two partial results: of a unit that others began (slot 2 x) and of one
 // that it begins (slot 2 x + 1).
 #pragma once
+#include <math.h>
+
+#include <algorithm>
+
 #include "qcf_decode_launch.h"
 #include "qcf_device.h"
 
@@ -213,5 +217,149 @@ __device__ __forceinline__ uint32_t tree_sees(const TreeAttn& p, const TreeReque
   if (j < 0) own |= (1u << -j) - 1u;  // (-j < W <= 32)
   return own & in;
 }
+
+// a running maximum as the reference of exponentials: 0 while nothing has been seen
+__device__ __forceinline__ float finite(float m) { return m == -INFINITY ? 0.f : m; }
+
+typedef const int32_t __attribute__((address_space(4))) * const_i32;
+
+// The page of 16 tokens from t0 on (t0 a multiple of 16, pages of 16 rows and more), or -1
+__device__ __forceinline__ int page_of(const TreeAttn& p, const_i32 table, int t0, int end) {
+  const int pg = t0 >> p.page_log2;
+  if (t0 >= end || pg >= p.max_pages) return -1;
+  const int page = uni(table[pg]);
+  return page < p.n_pages ? max(page, -1) : -1;
+}
+
+// Pages of fewer than 16 rows: the slot of a lane's token, or -1
+__device__ __forceinline__ int64_t slot_of(const TreeAttn& p, int b, int t, int end) {
+  const int pg = t >> p.page_log2;
+  if (t >= end || pg >= p.max_pages) return -1;
+  const int page = p.block_table[b * p.table_stride + pg];
+  return page >= 0 && page < p.n_pages ? ((int64_t)page << p.page_log2) + (t & ((1 << p.page_log2) - 1)) : -1;
+}
+
+namespace {
+
+__device__ __forceinline__ void store4(uint16_t* p, const float4& a) {
+  *reinterpret_cast<uint2*>(p) = make_uint2(pack_bf16x2(a.x, a.y), pack_bf16x2(a.z, a.w));
+}
+__device__ __forceinline__ void store4(float* p, const float4& a) { *reinterpret_cast<float4*>(p) = a; }
+
+// The partial results of a unit that is cut between blocks, in the blocks' order: one wave per row and
+// head (those whose unit one block took whole have nothing to do).  Lane j first takes the maximum and sum of
+// partial j, then 64 / (D / 4) partials at a time are read and summed, whose sums meet at the end.
+// Bound: latency (three loads that wait for each other), or the partials' bytes.
+constexpr int kMergeWaves = 4;
+template <typename T, int D>
+__global__ __launch_bounds__(kMergeWaves * 64) void tree_attn_merge_kernel(TreeAttn p, TreeCut cut, TreeWs ws, int lg) {
+  constexpr int LPR = D / 4, RPW = 64 / LPR, U = 8;
+  const int l = threadIdx.x & 63, lc = l % LPR, lr = l / LPR;
+  const int64_t item = (int64_t)blockIdx.x * kMergeWaves + uni((int)threadIdx.x >> 6);
+  const int64_t bi = quotient(item, p.hq);
+  const int h = (int)(item - bi * p.hq);
+  const int b = (int)quotient(bi, p.max_q), i = (int)(bi - (int64_t)b * p.max_q);
+  if (b >= p.batch) return;
+  const int g = h >> lg, vec = (i << lg) + (h & ((1 << lg) - 1));
+  const int tile = vec >> cut.vt_log2, v = vec - (tile << cut.vt_log2);
+  const int2 held = ws.held[((int64_t)b * p.hkv + g) * cut.tiles + tile];
+  const TreeRequest q = tree_request(p, b);
+  if (i >= q.rows) return;
+  const int x0 = uni(held.x), x1 = uni(held.y);
+  if (x0 == x1) return;
+  auto slot = [&](int x) { return ((int64_t)(2 * x + (x == x0 ? 1 : 0)) << cut.vt_log2) + v; };
+  const float4* part = reinterpret_cast<const float4*>(ws.o);
+  float mx = -INFINITY, lt = 0.f;
+  float4 a = make_float4(0.f, 0.f, 0.f, 0.f);
+  for (int xb = x0; xb <= x1; xb += 64) {
+    const int n = min(64, x1 - xb + 1);
+    const float2 ml = l < n ? ws.ml[slot(xb + l)] : make_float2(-INFINITY, 0.f);
+    const float mn = fmaxf(mx, wave_max(ml.x));
+    const float f = __builtin_amdgcn_exp2f(ml.x - finite(mn)), fa = __builtin_amdgcn_exp2f(mx - finite(mn));
+    lt = lt * fa + wave_sum(ml.y * f);
+    mx = mn;
+    a.x *= fa;
+    a.y *= fa;
+    a.z *= fa;
+    a.w *= fa;
+    for (int j0 = 0; j0 < n; j0 += U * RPW) {
+      float4 o[U];
+#pragma unroll
+      for (int k = 0; k < U; ++k) o[k] = part[slot(xb + min(j0 + k * RPW + lr, n - 1)) * LPR + lc];
+#pragma unroll
+      for (int k = 0; k < U; ++k) {
+        const int j = j0 + k * RPW + lr;
+        const float fo = __shfl(f, min(j, 63), 64);
+        if (j >= n) continue;
+        a.x = fmaf(o[k].x, fo, a.x);
+        a.y = fmaf(o[k].y, fo, a.y);
+        a.z = fmaf(o[k].z, fo, a.z);
+        a.w = fmaf(o[k].w, fo, a.w);
+      }
+    }
+  }
+#pragma unroll
+  for (int m = LPR; m < 64; m <<= 1) {
+    a.x += __shfl_xor(a.x, m, 64);
+    a.y += __shfl_xor(a.y, m, 64);
+    a.z += __shfl_xor(a.z, m, 64);
+    a.w += __shfl_xor(a.w, m, 64);
+  }
+  const bool none = mx == -INFINITY;
+  const float inv = none ? 0.f : 1.f / lt;
+  const int64_t at = (q.r0 + i) * p.hq + h;
+  if (lr == 0)
+    store4(static_cast<T*>(p.out) + at * D + 4 * lc, make_float4(a.x * inv, a.y * inv, a.z * inv, a.w * inv));
+  if (p.lse && l == 0) p.lse[at] = none ? -INFINITY : (mx + log2f(lt)) * kLn2;
+}
+
+inline int log2_of(int x) { return __builtin_ctz((unsigned)x); }
+
+constexpr int kTreeBlocks = 512;  // two per CU
+
+// How a call is cut, from its bounds (lengths are on the device).  float32 blocks hold 16 vectors.
+inline TreeCut tree_cut(int batch, int max_q, int max_kv, int hq, int hkv, bool bf16) {
+  const int64_t vectors = (int64_t)max_q * (hq / hkv);
+  const int vt = vectors <= 16 || !bf16 ? 16 : vectors <= 32 ? 32 : vectors <= 64 ? 64 : 128;
+  TreeCut c;
+  c.vt_log2 = log2_of(vt);
+  c.tiles = (int)((vectors + vt - 1) / vt);
+  const int64_t steps = ((int64_t)max_kv + kTreeStep - 1) / kTreeStep;
+  const int64_t all = (int64_t)batch * hkv * c.tiles * steps;
+  // short units are taken whole; else as many blocks as run at once, with 4 steps each at least
+  c.blocks = 0;
+  c.start = 4;
+  if (steps > 8) c.blocks = (int)std::max<int64_t>(std::min<int64_t>(kTreeBlocks, all / 4), 1);
+  return c;
+}
+
+struct TreeWsLayout {
+  size_t ml, o, total;
+};
+inline TreeWsLayout tree_ws_layout(const TreeCut& c, int batch, int hkv, int d) {
+  const auto up = [](size_t x) { return (x + 255) / 256 * 256; };
+  TreeWsLayout w{};
+  if (c.blocks == 0) return w;
+  w.ml = up((size_t)batch * hkv * c.tiles * sizeof(int2));
+  w.o = w.ml + up(((size_t)2 * c.blocks << c.vt_log2) * 8);
+  w.total = w.o + up(((size_t)2 * c.blocks << c.vt_log2) * d * 4);
+  return w;
+}
+
+inline TreeWs tree_ws(const TreeCut& c, int batch, int hkv, int d, void* workspace) {
+  const TreeWsLayout w = tree_ws_layout(c, batch, hkv, d);
+  char* base = static_cast<char*>(workspace);
+  return TreeWs{reinterpret_cast<int2*>(base), reinterpret_cast<float2*>(base + w.ml),
+                reinterpret_cast<float*>(base + w.o)};
+}
+
+template <typename T, int D>
+inline void launch_tree_merge(const TreeAttn& p, const TreeCut& c, const TreeWs& ws, int lg, hipStream_t stream) {
+  const int64_t rows = (int64_t)p.batch * p.max_q * p.hq;
+  tree_attn_merge_kernel<T, D>
+      <<<dim3((unsigned)((rows + kMergeWaves - 1) / kMergeWaves)), kMergeWaves * 64, 0, stream>>>(p, c, ws, lg);
+}
+
+}  // namespace
 
 }  // namespace qcf

@@ -16,7 +16,6 @@
 //          up to about 128 vectors, the matrix units beyond.
 #include <math.h>
 
-#include <algorithm>
 #include <type_traits>
 
 #include "qcf_attn.h"
@@ -27,7 +26,6 @@ namespace {
 
 typedef short v4s __attribute__((ext_vector_type(4)));
 typedef v4s __attribute__((address_space(3))) * lds_v4s;
-typedef const int32_t __attribute__((address_space(4))) * const_i32;
 
 // 16 bytes per lane from base + off into LDS at byte address lds + 16 * lane, past the registers and
 // without a wait of the compiler's (the caller counts)
@@ -39,9 +37,6 @@ __device__ __forceinline__ void copy16(const void* from, uint32_t lds) {
   const uint32_t la = __builtin_amdgcn_readfirstlane(lds);
   asm volatile("s_mov_b32 m0, %0\n\tglobal_load_lds_dwordx4 %1, off" : : "s"(la), "v"(from) : "memory");
 }
-
-// a running maximum as the reference of exponentials: 0 while nothing has been seen
-__device__ __forceinline__ float finite(float m) { return m == -INFINITY ? 0.f : m; }
 
 // Weights are exp2(s * scale2 - ref) with a fused multiply-add, which keeps the product exact; its
 // difference to the rounded maximum reaches 2^-24 of that, too much to be an exponent where maxima
@@ -56,22 +51,6 @@ __device__ __forceinline__ bool not_finite(const uint4& x) {
   for (int i = 0; i < 4; ++i)
     bad = bad || (w[i] & 0x7f80u) == 0x7f80u || (w[i] & 0x7f800000u) == 0x7f800000u;
   return bad;
-}
-
-// The page of 16 tokens from t0 on (t0 a multiple of 16, pages of 16 rows and more), or -1
-__device__ __forceinline__ int page_of(const TreeAttn& p, const_i32 table, int t0, int end) {
-  const int pg = t0 >> p.page_log2;
-  if (t0 >= end || pg >= p.max_pages) return -1;
-  const int page = uni(table[pg]);
-  return page < p.n_pages ? max(page, -1) : -1;
-}
-
-// Pages of fewer than 16 rows: the slot of a lane's token, or -1
-__device__ __forceinline__ int64_t slot_of(const TreeAttn& p, int b, int t, int end) {
-  const int pg = t >> p.page_log2;
-  if (t >= end || pg >= p.max_pages) return -1;
-  const int page = p.block_table[b * p.table_stride + pg];
-  return page >= 0 && page < p.n_pages ? ((int64_t)page << p.page_log2) + (t & ((1 << p.page_log2) - 1)) : -1;
 }
 
 // ---------------------------------------------------------------------------
@@ -759,177 +738,11 @@ __global__ __launch_bounds__(VG * 64, VG == 2 ? 1 : 2) void tree_attn_wide_kerne
   });
 }
 
-// ---------------------------------------------------------------------------
-// merge
-// ---------------------------------------------------------------------------
-__device__ __forceinline__ void store4(uint16_t* p, const float4& a) {
-  *reinterpret_cast<uint2*>(p) = make_uint2(pack_bf16x2(a.x, a.y), pack_bf16x2(a.z, a.w));
-}
-__device__ __forceinline__ void store4(float* p, const float4& a) { *reinterpret_cast<float4*>(p) = a; }
-
-// The partial results of a unit that is cut between blocks, in the blocks' order: one wave per row and
-// head (those whose unit one block took whole have nothing to do).  Lane j first takes the maximum and sum of
-// partial j, then 64 / (D / 4) partials at a time are read and summed, whose sums meet at the end.
-// Bound: latency (three loads that wait for each other), or the partials' bytes.
-constexpr int kMergeWaves = 4;
-template <typename T, int D>
-__global__ __launch_bounds__(kMergeWaves * 64) void tree_attn_merge_kernel(TreeAttn p, TreeCut cut, TreeWs ws, int lg) {
-  constexpr int LPR = D / 4, RPW = 64 / LPR, U = 8;
-  const int l = threadIdx.x & 63, lc = l % LPR, lr = l / LPR;
-  const int64_t item = (int64_t)blockIdx.x * kMergeWaves + uni((int)threadIdx.x >> 6);
-  const int64_t bi = quotient(item, p.hq);
-  const int h = (int)(item - bi * p.hq);
-  const int b = (int)quotient(bi, p.max_q), i = (int)(bi - (int64_t)b * p.max_q);
-  if (b >= p.batch) return;
-  const int g = h >> lg, vec = (i << lg) + (h & ((1 << lg) - 1));
-  const int tile = vec >> cut.vt_log2, v = vec - (tile << cut.vt_log2);
-  const int2 held = ws.held[((int64_t)b * p.hkv + g) * cut.tiles + tile];
-  const TreeRequest q = tree_request(p, b);
-  if (i >= q.rows) return;
-  const int x0 = uni(held.x), x1 = uni(held.y);
-  if (x0 == x1) return;
-  auto slot = [&](int x) { return ((int64_t)(2 * x + (x == x0 ? 1 : 0)) << cut.vt_log2) + v; };
-  const float4* part = reinterpret_cast<const float4*>(ws.o);
-  float mx = -INFINITY, lt = 0.f;
-  float4 a = make_float4(0.f, 0.f, 0.f, 0.f);
-  for (int xb = x0; xb <= x1; xb += 64) {
-    const int n = min(64, x1 - xb + 1);
-    const float2 ml = l < n ? ws.ml[slot(xb + l)] : make_float2(-INFINITY, 0.f);
-    const float mn = fmaxf(mx, wave_max(ml.x));
-    const float f = __builtin_amdgcn_exp2f(ml.x - finite(mn)), fa = __builtin_amdgcn_exp2f(mx - finite(mn));
-    lt = lt * fa + wave_sum(ml.y * f);
-    mx = mn;
-    a.x *= fa;
-    a.y *= fa;
-    a.z *= fa;
-    a.w *= fa;
-    for (int j0 = 0; j0 < n; j0 += U * RPW) {
-      float4 o[U];
-#pragma unroll
-      for (int k = 0; k < U; ++k) o[k] = part[slot(xb + min(j0 + k * RPW + lr, n - 1)) * LPR + lc];
-#pragma unroll
-      for (int k = 0; k < U; ++k) {
-        const int j = j0 + k * RPW + lr;
-        const float fo = __shfl(f, min(j, 63), 64);
-        if (j >= n) continue;
-        a.x = fmaf(o[k].x, fo, a.x);
-        a.y = fmaf(o[k].y, fo, a.y);
-        a.z = fmaf(o[k].z, fo, a.z);
-        a.w = fmaf(o[k].w, fo, a.w);
-      }
-    }
-  }
-#pragma unroll
-  for (int m = LPR; m < 64; m <<= 1) {
-    a.x += __shfl_xor(a.x, m, 64);
-    a.y += __shfl_xor(a.y, m, 64);
-    a.z += __shfl_xor(a.z, m, 64);
-    a.w += __shfl_xor(a.w, m, 64);
-  }
-  const bool none = mx == -INFINITY;
-  const float inv = none ? 0.f : 1.f / lt;
-  const int64_t at = (q.r0 + i) * p.hq + h;
-  if (lr == 0)
-    store4(static_cast<T*>(p.out) + at * D + 4 * lc, make_float4(a.x * inv, a.y * inv, a.z * inv, a.w * inv));
-  if (p.lse && l == 0) p.lse[at] = none ? -INFINITY : (mx + log2f(lt)) * kLn2;
-}
-
-// ---------------------------------------------------------------------------
-// float32: one wave per row and head, 64 tokens at a time
-// ---------------------------------------------------------------------------
-template <int D>
-__global__ __launch_bounds__(256) void tree_attn_f32_kernel(TreeAttn p) {
-  constexpr int NC = D / 64;
-  const int l = threadIdx.x & 63;
-  const int h = blockIdx.y * 4 + (threadIdx.x >> 6);
-  const int b = blockIdx.x / p.max_q, i = blockIdx.x % p.max_q;
-  if (h >= p.hq) return;
-  const TreeRequest rq = tree_request(p, b);
-  if (i >= rq.rows) return;
-  const int64_t r = rq.r0 + i;
-  const int g = h / (p.hq / p.hkv);
-  const float* q = static_cast<const float*>(p.q) + (r * p.hq + h) * D;
-  float m = -INFINITY, sum = 0.f, o[NC];
-#pragma unroll
-  for (int c = 0; c < NC; ++c) o[c] = 0.f;
-  for (int t0 = 0; t0 < rq.end; t0 += 64) {
-    const uint64_t bits = tree_sees<32>(p, rq, r, i, t0) |
-                          (t0 + 32 < rq.end ? (uint64_t)tree_sees<32>(p, rq, r, i, t0 + 32) << 32 : 0);
-    const int64_t slot = max(slot_of(p, b, t0 + l, rq.end), (int64_t)-1);
-    const bool see = (bits >> l & 1) && slot >= 0;
-    float x = -INFINITY;
-    if (see) {
-      const float* k = static_cast<const float*>(p.k_cache) + slot * p.kv_stride + g * D;
-      float dot = 0.f;
-      for (int c = 0; c < D; c += 4) {
-        const float4 a = *reinterpret_cast<const float4*>(q + c), y = *reinterpret_cast<const float4*>(k + c);
-        dot = fmaf(a.x, y.x, fmaf(a.y, y.y, fmaf(a.z, y.z, fmaf(a.w, y.w, dot))));
-      }
-      x = dot * p.scale;
-    }
-    const float mn = fmaxf(m, wave_max(x));
-    const float w = see ? expf(x - finite(mn)) : 0.f, alpha = expf(m - finite(mn));
-    sum = sum * alpha + wave_sum(w);
-    m = mn;
-#pragma unroll
-    for (int c = 0; c < NC; ++c) o[c] *= alpha;
-    for (uint64_t vis = __ballot(see); vis; vis &= vis - 1) {
-      const int k = __builtin_ctzll(vis);
-      const float wk = __shfl(w, k, 64);
-      const int64_t sk = __shfl(slot, k, 64);
-      const float* v = static_cast<const float*>(p.v_cache) + sk * p.kv_stride + g * D;
-#pragma unroll
-      for (int c = 0; c < NC; ++c) o[c] = fmaf(wk, v[c * 64 + l], o[c]);
-    }
-  }
-  float* out = static_cast<float*>(p.out) + (r * p.hq + h) * D;
-  const bool none = m == -INFINITY;
-#pragma unroll
-  for (int c = 0; c < NC; ++c) out[c * 64 + l] = none ? 0.f : o[c] / sum;
-  if (p.lse && l == 0) p.lse[r * p.hq + h] = none ? -INFINITY : m + logf(sum);
-}
-
-int log2_of(int x) { return __builtin_ctz((unsigned)x); }
-
-constexpr int kBlocks = 512;  // two per CU
-
-// How a bf16 call is cut, from its bounds (lengths are on the device)
-TreeCut tree_cut(int batch, int max_q, int max_kv, int hq, int hkv) {
-  const int64_t vectors = (int64_t)max_q * (hq / hkv);
-  const int vt = vectors <= 16 ? 16 : vectors <= 32 ? 32 : vectors <= 64 ? 64 : 128;
-  TreeCut c;
-  c.vt_log2 = log2_of(vt);
-  c.tiles = (int)((vectors + vt - 1) / vt);
-  const int64_t steps = ((int64_t)max_kv + kTreeStep - 1) / kTreeStep;
-  const int64_t all = (int64_t)batch * hkv * c.tiles * steps;
-  // short units are taken whole; else as many blocks as run at once, with 4 steps each at least
-  c.blocks = 0;
-  c.start = 4;
-  if (steps > 8) c.blocks = (int)std::max<int64_t>(std::min<int64_t>(kBlocks, all / 4), 1);
-  return c;
-}
-
-struct WsLayout {
-  size_t ml, o, total;
-};
-WsLayout ws_layout(const TreeCut& c, int batch, int hkv, int d) {
-  const auto up = [](size_t x) { return (x + 255) / 256 * 256; };
-  WsLayout w{};
-  if (c.blocks == 0) return w;
-  w.ml = up((size_t)batch * hkv * c.tiles * sizeof(int2));
-  w.o = w.ml + up(((size_t)2 * c.blocks << c.vt_log2) * 8);
-  w.total = w.o + up(((size_t)2 * c.blocks << c.vt_log2) * d * 4);
-  return w;
-}
-
 template <int D>
 hipError_t launch_bf16(const TreeAttn& p, void* workspace, hipStream_t stream) {
   const int lg = log2_of(p.hq / p.hkv);
-  const TreeCut c = tree_cut(p.batch, p.max_q, p.max_kv, p.hq, p.hkv);
-  const WsLayout wl = ws_layout(c, p.batch, p.hkv, D);
-  char* base = static_cast<char*>(workspace);
-  const TreeWs ws{reinterpret_cast<int2*>(base), reinterpret_cast<float2*>(base + wl.ml),
-                  reinterpret_cast<float*>(base + wl.o)};
+  const TreeCut c = tree_cut(p.batch, p.max_q, p.max_kv, p.hq, p.hkv, true);
+  const TreeWs ws = tree_ws(c, p.batch, p.hkv, D, workspace);
   const int64_t blocks = c.blocks ? c.blocks : (int64_t)p.batch * p.hkv * c.tiles;
   if (blocks > 0x7fffffff) return hipErrorInvalidConfiguration;
   const dim3 grid((unsigned)blocks);
@@ -940,40 +753,30 @@ hipError_t launch_bf16(const TreeAttn& p, void* workspace, hipStream_t stream) {
     else tree_attn_narrow_kernel<D, NV, false><<<grid, kNW * 64, 0, stream>>>(p, c, ws, lg);     \
   } while (0)
 #define QCF_WIDE(VG)                                                                            \
-  case VG:                                                                                      \
+  do {                                                                                          \
     if (tiny) tree_attn_wide_kernel<D, VG, true><<<grid, VG * 64, 0, stream>>>(p, c, ws, lg);   \
     else tree_attn_wide_kernel<D, VG, false><<<grid, VG * 64, 0, stream>>>(p, c, ws, lg);       \
-    break
+  } while (0)
   if (c.vt_log2 == 4) QCF_NARROW(1);
   else if (c.vt_log2 == 5) QCF_NARROW(2);
-  else switch (1 << (c.vt_log2 - 5)) {
-    QCF_WIDE(2);
-    QCF_WIDE(4);
-  }
+  else if (c.vt_log2 == 6) QCF_WIDE(2);
+  else QCF_WIDE(4);
 #undef QCF_WIDE
 #undef QCF_NARROW
-  if (c.blocks) {
-    const int64_t rows = (int64_t)p.batch * p.max_q * p.hq;
-    tree_attn_merge_kernel<uint16_t, D>
-        <<<dim3((unsigned)((rows + kMergeWaves - 1) / kMergeWaves)), kMergeWaves * 64, 0, stream>>>(p, c, ws, lg);
-  }
+  if (c.blocks) launch_tree_merge<uint16_t, D>(p, c, ws, lg, stream);
   return hipGetLastError();
 }
 
 }  // namespace
 
 size_t tree_attn_workspace(int batch, int max_q, int max_kv, int hq, int hkv, int head_dim, bool bf16) {
-  if (!bf16) return 0;
-  return ws_layout(tree_cut(batch, max_q, max_kv, hq, hkv), batch, hkv, head_dim).total;
+  return tree_ws_layout(tree_cut(batch, max_q, max_kv, hq, hkv, bf16), batch, hkv, head_dim).total;
 }
 
 hipError_t launch_tree_attn(const TreeAttn& p, bool bf16, int head_dim, void* ws, hipStream_t stream) {
-  if ((int64_t)p.batch * p.max_q * p.hq > 0x7fffffff) return hipErrorInvalidConfiguration;
-  if (bf16) return head_dim == 64 ? launch_bf16<64>(p, ws, stream) : launch_bf16<128>(p, ws, stream);
-  const dim3 grid((unsigned)(p.batch * p.max_q), (unsigned)((p.hq + 3) / 4));
-  if (head_dim == 64) tree_attn_f32_kernel<64><<<grid, 256, 0, stream>>>(p);
-  else tree_attn_f32_kernel<128><<<grid, 256, 0, stream>>>(p);
-  return hipGetLastError();
+  if (((int64_t)p.batch * p.max_q * p.hq + kMergeWaves - 1) / kMergeWaves > 0x7fffffff) return hipErrorInvalidConfiguration;
+  if (!bf16) return launch_tree_attn_f32(p, head_dim, ws, stream);
+  return head_dim == 64 ? launch_bf16<64>(p, ws, stream) : launch_bf16<128>(p, ws, stream);
 }
 
 }  // namespace qcf
