@@ -15,7 +15,7 @@ namespace {
 
 constexpr int kThreads = 256;
 constexpr int kReq = kThreads;      // requests per scan
-constexpr int kTile = 1024;         // rows per block
+constexpr int kTile = kThreads;     // rows per block (one per thread: 256 trees of up to 40 rows 14.6 -> 6.8 us against four)
 constexpr int kTree = 1024;         // rows of the largest tree (QCF_MAX_TREE)
 
 __device__ __forceinline__ int64_t pages_of(int64_t tokens, int lp) {
@@ -77,10 +77,8 @@ __global__ __launch_bounds__(kThreads) void page_plan_kernel(PagePlan p) {
     }
     __syncthreads();
     const int64_t rows = (uint32_t)all;
-#pragma unroll
-    for (int k = 0; k < kTile / kThreads; ++k) {
-      const int64_t t = t0 + k * kThreads + tid, rel = t - row0;
-      if (rel < 0 || rel >= rows || t >= p.n_rows) continue;
+    const int64_t t = t0 + tid, rel = t - row0;
+    if (rel >= 0 && rel < rows && t < p.n_rows) {
       int lo = 0, hi = kReq;  // the last request that starts at or before the row
       while (hi - lo > 1) {
         const int mid = (lo + hi) >> 1;
@@ -138,10 +136,8 @@ __global__ __launch_bounds__(kThreads) void page_plan_kernel(PagePlan p) {
     if (p.free_head_out) p.free_head_out[0] = (int32_t)(head + page0);
   }
   // rows behind the last request (a block that left the loop early has none)
-#pragma unroll
-  for (int k = 0; k < kTile / kThreads; ++k) {
-    const int64_t t = t0 + k * kThreads + tid;
-    if (t < row0 || t >= p.n_rows) continue;
+  const int64_t t = t0 + tid;
+  if (t >= row0 && t < p.n_rows) {
     p.slots[t] = -1;
     p.positions[t] = -1;
     if (p.parents)

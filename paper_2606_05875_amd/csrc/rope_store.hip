@@ -12,6 +12,10 @@ namespace {
 
 constexpr int kThreads = 256;
 
+// One row per block.  The first kAhead units of every thread are asked for, unmasked from clamped units (a
+// load under a lane condition waits by itself), before the row's angles are formed.
+constexpr int kAhead = 3;
+
 template <typename T, int D, bool kInter>
 __global__ __launch_bounds__(kThreads) void rope_store_kernel(RopeStore p) {
   constexpr int VEC = Vec16<T>::N;
@@ -21,51 +25,72 @@ __global__ __launch_bounds__(kThreads) void rope_store_kernel(RopeStore p) {
   const int64_t s = p.src_idx ? (int64_t)p.src_idx[r] : r;
   if (s < 0 || s >= p.n_src_rows) return;
   const int half = p.rotary_dim / 2;
-  if (p.positions && (int)threadIdx.x < half)
-    cs[threadIdx.x] = angle_cs<true, true>((double)p.positions[r] * p.freq[threadIdx.x], (double)p.magnitude);
-  __syncthreads();
   const int64_t slot = p.k_cache ? p.slots[r] : -1;
   const bool store = slot >= 0 && slot < p.n_slots;
   const int nq = p.q_out ? p.hq : 0, nkv = store ? p.hkv : 0;
-  for (int u = threadIdx.x; u < (nq + 2 * nkv) * UPH; u += kThreads) {
+  const int units = (nq + 2 * nkv) * UPH;
+  if (units == 0) return;
+  struct Unit {
+    uint4 a, b;
+    T* dst;
+    int ia, ib;
+    bool turn;
+  };
+  auto load = [&](int u) {
+    Unit x;
     const int h = u / UPH, c = u % UPH;
     const T* src;
-    T* dst;
-    bool turn = p.positions != nullptr && c * 2 * VEC < p.rotary_dim;
+    x.turn = p.positions != nullptr && c * 2 * VEC < p.rotary_dim;
     if (h < nq) {
       src = static_cast<const T*>(p.q_new) + s * p.q_stride + h * D;
-      dst = static_cast<T*>(p.q_out) + (r * p.hq + h) * D;
+      x.dst = static_cast<T*>(p.q_out) + (r * p.hq + h) * D;
     } else if (h < nq + nkv) {
       src = static_cast<const T*>(p.k_new) + s * p.new_stride + (h - nq) * D;
-      dst = static_cast<T*>(p.k_cache) + slot * p.cache_stride + (h - nq) * D;
+      x.dst = static_cast<T*>(p.k_cache) + slot * p.cache_stride + (h - nq) * D;
     } else {
       src = static_cast<const T*>(p.v_new) + s * p.new_stride + (h - nq - nkv) * D;
-      dst = static_cast<T*>(p.v_cache) + slot * p.cache_stride + (h - nq - nkv) * D;
-      turn = false;
+      x.dst = static_cast<T*>(p.v_cache) + slot * p.cache_stride + (h - nq - nkv) * D;
+      x.turn = false;
     }
-    const int a = turn && !kInter ? c * VEC : c * 2 * VEC;
-    const int b = turn && !kInter ? a + half : a + VEC;
-    uint4 va = ld16(src + a), vb = ld16(src + b);
-    if (turn) {
+    x.ia = x.turn && !kInter ? c * VEC : c * 2 * VEC;
+    x.ib = x.turn && !kInter ? x.ia + half : x.ia + VEC;
+    x.a = ld16(src + x.ia);
+    x.b = ld16(src + x.ib);
+    return x;
+  };
+  auto finish = [&](const Unit& u) {
+    uint4 va = u.a, vb = u.b;
+    if (u.turn) {
       float x[VEC], y[VEC], xo[VEC], yo[VEC];
       Vec16<T>::unpack(va, x);
       Vec16<T>::unpack(vb, y);
       if (kInter) {
 #pragma unroll
         for (int e = 0; e < VEC; e += 2) {
-          rope_pair(x[e], x[e + 1], cs[(a + e) / 2], xo[e], xo[e + 1]);
-          rope_pair(y[e], y[e + 1], cs[(b + e) / 2], yo[e], yo[e + 1]);
+          rope_pair(x[e], x[e + 1], cs[(u.ia + e) / 2], xo[e], xo[e + 1]);
+          rope_pair(y[e], y[e + 1], cs[(u.ib + e) / 2], yo[e], yo[e + 1]);
         }
       } else {
 #pragma unroll
-        for (int e = 0; e < VEC; ++e) rope_pair(x[e], y[e], cs[a + e], xo[e], yo[e]);
+        for (int e = 0; e < VEC; ++e) rope_pair(x[e], y[e], cs[u.ia + e], xo[e], yo[e]);
       }
       va = Vec16<T>::pack(xo);
       vb = Vec16<T>::pack(yo);
     }
-    st16(dst + a, va);
-    st16(dst + b, vb);
-  }
+    st16(u.dst + u.ia, va);
+    st16(u.dst + u.ib, vb);
+  };
+  Unit x[kAhead];
+#pragma unroll
+  for (int k = 0; k < kAhead; ++k)
+    if (k * kThreads < units) x[k] = load(min((int)threadIdx.x + k * kThreads, units - 1));
+  if (p.positions && (int)threadIdx.x < half)
+    cs[threadIdx.x] = angle_cs<true, true>((double)p.positions[r] * p.freq[threadIdx.x], (double)p.magnitude);
+  __syncthreads();
+#pragma unroll
+  for (int k = 0; k < kAhead; ++k)
+    if ((int)threadIdx.x + k * kThreads < units) finish(x[k]);
+  for (int u = threadIdx.x + kAhead * kThreads; u < units; u += kThreads) finish(load(u));
 }
 
 template <typename T, int D>
