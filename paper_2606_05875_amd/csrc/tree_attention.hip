@@ -596,9 +596,7 @@ __global__ __launch_bounds__(VG * 64, VG == 2 ? 1 : 2) void tree_attn_wide_kerne
     auto plain_step = [&](int t, f32x16 (&s)[2], f32x16 (&sn)[2]) {
       bf16x8 pb[2][2];
       maximum(s);
-      __builtin_amdgcn_s_setprio(1);
       weights(std::true_type{}, k_ring + ((t + 1) & (NB - 1)) * TB, sn, s, pb);
-      __builtin_amdgcn_s_setprio(0);
       products_o(v_ring + (t & (NB - 1)) * TB, pb);
     };
     // Tiles with tokens that are not there or that some row does not see.  held: those that are there, as
