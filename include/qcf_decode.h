@@ -73,7 +73,8 @@ extern "C" {
  * No output may overlap an input other than block_table (free_head_out must
  * not be free_head: keep two and swap them).
  * Rows at and behind cu_new[batch] get slot and position -1 and an empty mask;
- * rows at and behind n_rows are counted in cu_new, but not written.
+ * rows at and behind n_rows are counted in cu_new, but not written (nor are the
+ * table entries of pages that begin with one of them).
  * Where the free list ends (free_head_out > n_free then), where a page number
  * lies outside [0, n_pages) or a request needs more than max_pages pages, the
  * table entry of a new page is -1 (beyond max_pages there is none) and the slots
@@ -175,8 +176,12 @@ qcf_status qcf_rope_store(void* k_cache, void* v_cache, int64_t n_slots, int64_t
  *              and keeps nothing; calls that overlap in time need separate ones.  The
  *              size for (batch, max_q, max_kv) covers every call whose three values
  *              do not exceed them (other arguments equal).
- * Sums, maxima and outputs are held in float32; bf16 calls round the weights
- * exp(x - max) to bf16 for the matrix units, after they entered the sum.
+ * Sums, maxima and partial results are float32; bf16 calls round the weights
+ * exp(x - max) to bf16 for the matrix units, after they entered the sum.  A row's
+ * bits do not depend on the other rows' values.
+ * Errors: null pointers, softmax_scale not positive and finite, page_size not a
+ * power of two (UNSUPPORTED), row strides of 128 MB and more, batch * max_q *
+ * n_q_heads beyond int32 or max_kv within 2^20 of it (UNSUPPORTED), workspace.
  */
 size_t qcf_tree_attn_workspace_size(int batch, int max_q, int max_kv, int n_q_heads,
                                     int n_kv_heads, int head_dim, qcf_dtype dtype);

@@ -103,7 +103,8 @@ def test_tree_attn_refusals(L):
                 dict(ps=0), dict(scale=0.0), dict(scale=math.nan), dict(scale=math.inf), dict(mask=A), dict(n=-1),
                 dict(batch=-1), dict(max_q=-1), dict(max_kv=-1), dict(slots=-1), dict(hq=36)):
         assert call(**bad) == INVALID, bad
-    for bad in (dict(dt=5), dict(d=96), dict(hq=24), dict(ps=48)):
+    for bad in (dict(dt=5), dict(d=96), dict(hq=24), dict(ps=48), dict(stride=1 << 26), dict(max_kv=2 ** 31 - 5),
+                dict(batch=1 << 14, max_q=1 << 14)):
         assert call(**bad) == UNSUPPORTED, bad
     if need:
         for bad in (dict(ws=None), dict(ws=A + 16), dict(wsb=need - 1)):

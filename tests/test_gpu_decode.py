@@ -569,6 +569,41 @@ def test_verify_large_trees():
         _verify([1024, 5], 97, "f32", draft, False, noise=0.05)
 
 
+# -- refusals of the binding --
+def test_binding_refusals():
+    say("binding refusals")
+    i, w = i32([0, 1, 2, 3]), i32([[0, 1], [2, 3]])
+    f, h = torch.zeros(4, 2, 64, device="cuda"), torch.zeros(4, 2, 64, device="cuda").bfloat16()
+    freq = qcf.rope_frequencies(64, 1e4)
+    plan = lambda table=w, kv=i[:2], new=i[:2], slots=i, pos=i, cu=i[:3], **k: \
+        qcf.qcf_page_plan(table, kv, new, i, slots, pos, cu, 16, 4, 1, **k)
+    rope = lambda kc=f, vc=f, kn=f, vn=f, slots=i, pos=i, fr=freq, **k: qcf.qcf_rope_store(kc, vc, kn, vn, slots, pos, fr, **k)
+    attn = lambda out=f, q=f.clone(), cu=i[:3], kc=f, vc=f, table=w, kv=i[:2], **k: \
+        qcf.qcf_tree_attn(out, q, cu, kc, vc, table, kv, 2, 2, 4, 0.1, **k)
+    t = torch.zeros(4, 5, device="cuda")
+    u = t[:, 0].contiguous()
+    ver = lambda n=i[:2], path=w, toks=w, target=t, tokens=i, cu=i[:3], ua=u, un=u[:2], **k: \
+        qcf.qcf_verify_drafts(n, path, toks, target, tokens, cu, ua, un, **k)
+    for call in (lambda: plan(table=w[:1]), lambda: plan(table=w.t()), lambda: plan(kv=i[:2].long()), lambda: plan(cu=i),
+                 lambda: plan(pos=i[:3]), lambda: plan(parents=i), lambda: plan(tree_mask=w), lambda: plan(kv=i[::2]),
+                 lambda: plan(parents=i, tree_mask=w), lambda: plan(free_head=i), lambda: plan(pages_held=i),
+                 lambda: rope(kc=h), lambda: rope(kc=None), lambda: rope(slots=None), lambda: rope(pos=None),
+                 lambda: rope(fr=None), lambda: rope(slots=i[:3]), lambda: rope(fr=freq.float()), lambda: rope(fr=freq[::2]),
+                 lambda: rope(kn=f[:3], vn=f[:3]), lambda: rope(q_new=f), lambda: rope(q_new=f, q_out=f[:3]),
+                 lambda: rope(kn=f[:, :1]), lambda: rope(vn=f.transpose(0, 1)), lambda: rope(src_idx=i[:2]),
+                 lambda: rope(kn=f, vn=f),                       # the cache itself
+                 lambda: attn(out=f[:3]), lambda: attn(q=h), lambda: attn(cu=i), lambda: attn(table=w[:1]),
+                 lambda: attn(kc=f[:, :1]), lambda: attn(tree_mask=w), lambda: attn(lse=u), lambda: attn(kv=i),
+                 lambda: attn(workspace=torch.zeros(4, dtype=torch.uint8)), lambda: attn(q=f.transpose(0, 1)),
+                 lambda: attn(out=f, q=f),                       # in place
+                 lambda: ver(path=w[:1]), lambda: ver(toks=i32([[0], [1]])), lambda: ver(target=t[:3]), lambda: ver(ua=u[:3]),
+                 lambda: ver(un=u), lambda: ver(tokens=i.long()), lambda: ver(draft=t[:, :4]), lambda: ver(draft=t.bfloat16()),
+                 lambda: ver(slots=i), lambda: ver(parents=i[:3]), lambda: ver(target=t.t().contiguous().t())):
+        with pytest.raises(qcf.QcfError):
+            call()
+    torch.cuda.synchronize()
+
+
 # -- streams and graphs ------------------------------------------------------------------------
 def test_calls_on_another_stream_and_in_a_graph():
     """A captured pass, replayed with other inputs in place and eager calls in between, gives what eager
