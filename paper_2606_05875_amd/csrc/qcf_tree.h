@@ -182,13 +182,15 @@ __device__ __forceinline__ void tree_walk(const TreeAttn& p, const TreeCut& cut,
     const int64_t to = min(u0 + start + steps, share1);
     const int first = (int)max(s - u0 - start, (int64_t)0), n = (int)(to - u0 - start) - first;
     if (n > 0) {
-      const int g = (int)quotient(u, tiles), tile = (int)(u - (int64_t)g * tiles);
+      const int g = uni((int)quotient(u, tiles)), tile = uni((int)(u - (int64_t)g * tiles));
       if (cut.blocks && first == 0 && threadIdx.x == 0) {
         const TreeShares shares(all, cut.blocks);
         ws.held[((int64_t)b * p.hkv + g) * cut.tiles + tile] =
             make_int2(x, n == steps ? x : shares.holder(u0 + start + steps - 1));
       }
-      unit(b, q, g, tile, first, n, steps, n == steps ? -1 : 2 * x + (first > 0 ? 0 : 1));
+      // (uniform values that passed the vector units' division would be taken for vectors', and with them
+      // the block table's entries: loads that a wait for copies in flight would follow)
+      unit(uni(b), q, g, tile, uni(first), uni(n), uni(steps), n == steps ? -1 : uni(2 * x + (first > 0 ? 0 : 1)));
     }
     s = to;
   }
