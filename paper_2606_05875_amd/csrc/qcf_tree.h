@@ -319,12 +319,11 @@ inline int log2_of(int x) { return __builtin_ctz((unsigned)x); }
 
 // How a call is cut, from its bounds (lengths are on the device).
 //
-// Vectors per unit: the fewest that hold a request's, since padded ones cost their products (32 vectors,
-// trees over 2000 to 12700 tokens, 64/8 heads of 128: 101 us as 32, 109 as 128; 64 vectors: 105 as 64, 112 as
-// 128).  More vectors than a unit holds read the keys again, mostly from an L2, which costs less than
-// 128 vectors' larger partial results up to two units and where blocks have many steps (128 vectors, 16 such
-// requests: 113 us as 64, 122 as 128; one of 8000 tokens: 25.5 and 23.2), more beyond (192 vectors: 167
-// and 131).  float32 blocks hold 16 vectors.
+// Vectors per unit: the fewest that hold a request's, up to 128, since padded ones cost their products (16
+// requests of 2000 to 12700 tokens, 32/8 heads of 128: 16 vectors 98 us as 16, 101 as 32, 109 as 128; 64
+// vectors 113 as 64, 122 as 128), and more than a unit holds read the keys again (128 vectors: 140 as 128, 173
+// as 64; only where all keys stay in the caches is that less, one request of 32896 tokens: 52 and 47).
+// float32 blocks hold 16 vectors.
 //
 // Short units are taken whole, one per block: up to 8 steps always (64 decoded rows over up to 500 tokens:
 // 21.5 us against 27.0 cut), up to 32 where there is one for every CU (256 units of up to 2000 tokens: 41.6 against
@@ -334,10 +333,8 @@ inline int log2_of(int x) { return __builtin_ctz((unsigned)x); }
 constexpr int kTreeBlocks = 512;
 inline TreeCut tree_cut(int batch, int max_q, int max_kv, int hq, int hkv, bool bf16) {
   const int64_t vectors = (int64_t)max_q * (hq / hkv);
-  const int64_t steps = ((int64_t)max_kv + kTreeStep - 1) / kTreeStep, keys = (int64_t)batch * hkv * steps;
-  const int vt = vectors <= 16 || !bf16 ? 16
-                 : vectors <= 32        ? 32
-                 : vectors <= 64 || (vectors <= 128 && keys >= 8 * kTreeBlocks) ? 64 : 128;
+  const int64_t steps = ((int64_t)max_kv + kTreeStep - 1) / kTreeStep;
+  const int vt = vectors <= 16 || !bf16 ? 16 : vectors <= 32 ? 32 : vectors <= 64 ? 64 : 128;
   TreeCut c;
   c.vt_log2 = log2_of(vt);
   c.tiles = (int)((vectors + vt - 1) / vt);
