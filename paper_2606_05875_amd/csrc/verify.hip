@@ -67,16 +67,33 @@ struct Row {
   __device__ __forceinline__ bool inside(int64_t j0, int64_t j1) const { return j0 >= lead && j1 <= (int64_t)vocab + lead; }
   // the piece that begins with token j - lead (j a multiple of VEC), which is inside the row ..
   __device__ __forceinline__ uint4 load(const T* x, int64_t j) const { return ld16(x + first + j); }
-  // .. or anywhere: elements outside the row are zeros
+  // .. or anywhere: elements outside the row are zeros.  No load is under a lane's condition, where each would
+  // wait by itself: four elements are read from clamped places (64 chains of float32: 24.6 us a call, 28.0 the
+  // other way), of eight the whole piece, and only the row's ends by element (16 trees of bfloat16: 50 us, 57).
   __device__ __forceinline__ uint4 load_any(const T* x, int64_t j) const {
-    if (inside(j, j + VEC)) return load(x, j);
-    T v[VEC];
+    const int64_t end = (int64_t)lead + vocab;
+    if constexpr (VEC == 4) {
+      uint32_t w[VEC];
 #pragma unroll
-    for (int e = 0; e < VEC; ++e) {
-      const int64_t t = j - lead + e;
-      v[e] = t >= 0 && t < vocab ? x[first + j + e] : T(0);
+      for (int e = 0; e < VEC; ++e) w[e] = __builtin_bit_cast(uint32_t, x[first + min(max(j + e, (int64_t)lead), end - 1)]);
+#pragma unroll
+      for (int e = 0; e < VEC; ++e) {
+        asm volatile("" : "+v"(w[e]));
+        if (j + e < lead || j + e >= end) w[e] = 0;
+      }
+      return make_uint4(w[0], w[1], w[2], w[3]);
+    } else {
+      const int64_t lo = lead ? VEC : 0, hi = (end & ~(int64_t)(VEC - 1)) - VEC;  // the first and the last whole piece
+      uint4 v = make_uint4(0, 0, 0, 0);
+      if (lo <= hi) v = load(x, min(max(j, lo), hi));
+      if (j < lo || j > hi) {
+        T w[VEC];
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) w[e] = j + e >= lead && j + e < end ? x[first + j + e] : T(0);
+        v = __builtin_bit_cast(uint4, w);
+      }
+      return v;
     }
-    return __builtin_bit_cast(uint4, v);
   }
   __device__ __forceinline__ static void unpack(const uint4& x, float (&v)[VEC]) {
     Vec16<T>::unpack(x, v);
@@ -200,8 +217,16 @@ __device__ __forceinline__ void walk(const VerifyDrafts& p, int64_t r0, int n, W
       } else {
 #pragma unroll
         for (int k = 0; k < U; ++k) {
-          a[k] = row.load_any(target, j + k * NT * VEC);
-          d[k] = row.load_any(draft, j + k * NT * VEC);
+          const int64_t jk = j0 + (int64_t)k * NT * VEC;
+          if (row.inside(jk, jk + NT * VEC)) {
+            a[k] = row.load(target, j + k * NT * VEC);
+            d[k] = row.load(draft, j + k * NT * VEC);
+          } else if (jk < end) {
+            a[k] = row.load_any(target, j + k * NT * VEC);
+            d[k] = row.load_any(draft, j + k * NT * VEC);
+          } else {
+            a[k] = d[k] = make_uint4(0, 0, 0, 0);
+          }
         }
       }
 #pragma unroll
@@ -320,9 +345,10 @@ __global__ __launch_bounds__(kThreads) void verify_sums_kernel(VerifyDrafts p, W
   Residual<T> x[NV];
 #pragma unroll
   for (int k = 0; k < NV; ++k) {
-    const int64_t j = (int64_t)c * kChunk + (k * kThreads + tid) * VEC;
-    if (row.inside((int64_t)c * kChunk, (int64_t)(c + 1) * kChunk)) x[k].load(p, row, j);
-    else x[k].load_any(p, row, j);
+    const int64_t jk = (int64_t)c * kChunk + k * kThreads * VEC;
+    if (row.inside(jk, jk + kThreads * VEC)) x[k].load(p, row, jk + tid * VEC);
+    else if (jk < (int64_t)p.vocab + row.lead) x[k].load_any(p, row, jk + tid * VEC);
+    else x[k].a = x[k].d = make_uint4(0, 0, 0, 0);
   }
   if (kWalk && !p.draft) {
     for (int i = cur + 1 + tid; i < n; i += kThreads) mark_rejected(bits, s.par[i], s.tok[i], cur, (int64_t)c * kChunk - row.lead);
