@@ -251,7 +251,8 @@ __device__ __forceinline__ void store4(float* p, const float4& a) { *reinterpret
 // The partial results of a unit that is cut between blocks, in the blocks' order: one wave per row and
 // head (those whose unit one block took whole have nothing to do).  Lane j first takes the maximum and sum of
 // partial j, then 64 / (D / 4) partials at a time are read and summed, whose sums meet at the end.
-// Bound: latency (three loads that wait for each other), or the partials' bytes.
+// Bound: latency (three loads that wait for each other; 64 rows of 32 heads 5 us), or the partials' bytes (64
+// rows of 64 heads in 512 pieces, 34 MB: 9 us).
 constexpr int kMergeWaves = 4;
 template <typename T, int D>
 __global__ __launch_bounds__(kMergeWaves * 64) void tree_attn_merge_kernel(TreeAttn p, TreeCut cut, TreeWs ws, int lg) {
@@ -330,8 +331,11 @@ inline int log2_of(int x) { return __builtin_ctz((unsigned)x); }
 // 47.2; 128 units: 27.8 against 25.2; float32 units, whose steps take longer, not).  Else as many blocks as run at
 // once, two per CU (trees: 256 blocks 152 us, 512 142, 768 157), with 4 steps each at least.  `start` 4: 209, 203,
 // 205 us with 0, 4, 8 for 64 decoded rows over 512 to 8192 tokens.
+//
+// The workspace is sized as if units for every CU were cut too (`cut_all`): it then grows with every bound, and one
+// for the largest batch serves smaller ones.
 constexpr int kTreeBlocks = 512;
-inline TreeCut tree_cut(int batch, int max_q, int max_kv, int hq, int hkv, bool bf16) {
+inline TreeCut tree_cut(int batch, int max_q, int max_kv, int hq, int hkv, bool bf16, bool cut_all = false) {
   const int64_t vectors = (int64_t)max_q * (hq / hkv);
   const int64_t steps = ((int64_t)max_kv + kTreeStep - 1) / kTreeStep;
   const int vt = vectors <= 16 || !bf16 ? 16 : vectors <= 32 ? 32 : vectors <= 64 ? 64 : 128;
@@ -341,7 +345,7 @@ inline TreeCut tree_cut(int batch, int max_q, int max_kv, int hq, int hkv, bool 
   const int64_t units = (int64_t)batch * hkv * c.tiles;
   c.blocks = 0;
   c.start = 4;
-  if (steps > 32 || (steps > 8 && (units < kTreeBlocks / 2 || !bf16)))
+  if (steps > 32 || (steps > 8 && (units < kTreeBlocks / 2 || !bf16 || cut_all)))
     c.blocks = (int)std::max<int64_t>(std::min<int64_t>(kTreeBlocks, units * steps / 4), 1);
   return c;
 }

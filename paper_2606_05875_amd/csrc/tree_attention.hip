@@ -10,10 +10,14 @@
 //  narrow  up to 32 query vectors per request and KV head (one token, short chains).  Bound: HBM.  Four
 //          waves take 16-token tiles in turn, each on its own (two stages of LDS, no barrier in the loop),
 //          v_mfma_f32_16x16x32/16x16x16_bf16; their results are summed through LDS once per unit.
+//          64 decoded rows over 512 to 8192 tokens, 32/8 heads of 128: 204 us with the merge, 5.57 TB/s (a
+//          copy reaches 5.1); one row over 8192 tokens 16.4 us, over 32768 32 us.
 //  wide    more vectors (trees).  A wave holds 32 of them (v_mfma_f32_32x32x16_bf16) and the 2 or 4
 //          waves of a block share every 64-token tile (a ring of stages, one barrier per tile); the
-//          products of the next tile's S run beside this tile's exponentials.  Bound: HBM
-//          up to about 128 vectors, the matrix units beyond.
+//          products of the next tile's S run beside this tile's exponentials.  Bound: HBM and the latency of
+//          pages up to about 128 vectors (16 trees of 8 to 40 rows over 2000 to 12700 tokens, 32/8 heads of
+//          128: 142 us, 3.5 TB/s), products and exponentials beyond (64 rows of 64/8 heads: 92 us over 32896
+//          tokens, 0.75 PFLOP/s; 304 us over 131584, 0.91 PFLOP/s, the matrix units busy 56% of the cycles).
 #include <math.h>
 
 #include <type_traits>
@@ -768,7 +772,7 @@ hipError_t launch_bf16(const TreeAttn& p, void* workspace, hipStream_t stream) {
 }  // namespace
 
 size_t tree_attn_workspace(int batch, int max_q, int max_kv, int hq, int hkv, int head_dim, bool bf16) {
-  return tree_ws_layout(tree_cut(batch, max_q, max_kv, hq, hkv, bf16), batch, hkv, head_dim).total;
+  return tree_ws_layout(tree_cut(batch, max_q, max_kv, hq, hkv, bf16, true), batch, hkv, head_dim).total;
 }
 
 hipError_t launch_tree_attn(const TreeAttn& p, bool bf16, int head_dim, void* ws, hipStream_t stream) {
