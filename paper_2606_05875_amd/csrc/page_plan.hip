@@ -6,7 +6,8 @@
 // of rows, and nothing has to meet between blocks: one launch, no atomics, the same result in any
 // order.  A new page begins with a new row, so whoever writes that row's slot writes the table entry.
 //
-// Bound: latency (a few dependent loads; the largest calls move about a megabyte).
+// Bound: latency (a few dependent loads; the largest calls move about a megabyte): 64 requests of one row 4.3 us,
+// 3.2 of them the kernel; 256 trees of up to 40 rows 6.4 us; 16 requests of 117000 rows in all 4.7 us.
 #include "qcf_decode_launch.h"
 #include "qcf_device.h"
 

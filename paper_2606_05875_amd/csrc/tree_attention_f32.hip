@@ -11,8 +11,9 @@
 //  * O^T += V^T P^T with P^T straight from those registers: product (r, mb) contracts over the tokens
 //    4 (l / 16) + r and fills the d-columns NB (l % 16) + mb, so a lane's V operands are NB contiguous floats.
 //  * exp2f, not the bare instruction: weights below 2^-126 stay subnormal numbers.
-// Bound: latency at test sizes, HBM or the float32 matrix rate beyond (each K and V row is read once per 16
-// vectors).
+// Bound: latency at test sizes (3 requests of up to 700 tokens, 8/2 heads of 64: 13.9 us, 4 of them the merge),
+// HBM or the float32 matrix rate beyond (each K and V row is read once per 16 vectors; 3 trees over 20000
+// tokens, 32/8 heads of 128: 105 us, 4.7 TB/s).
 #include "qcf_tree.h"
 
 namespace qcf {

@@ -14,7 +14,9 @@
 // Everything that decides a token is float64 (probabilities are widened exactly): with float32 sums a
 // draw next to a border would hang on the order of the additions.
 //
-// Bound: one vocabulary row of P (and D) per request from HBM; for few requests latency.
+// Bound: one vocabulary row of P (and D) per request from HBM; for few requests latency.  64 chains of 5 over
+// 128000 float32 probabilities of both: 24.6 us (66 MB; sums 14, pick 8); 16 trees over 150001 of bfloat16
+// without D 14.7 us, one tree 12.6.  64 trees of 5 with D 57 us: siblings' sums wait for each other on one CU each (31).
 #include "qcf_decode_launch.h"
 #include "qcf_device.h"
 
