@@ -324,21 +324,26 @@ inline int log2_of(int x) { return __builtin_ctz((unsigned)x); }
 // requests of 2000 to 12700 tokens, 32/8 heads of 128: 16 vectors 98 us as 16, 101 as 32, 109 as 128; 64
 // vectors 113 as 64, 122 as 128), and more than a unit holds read the keys again (128 vectors: 140 as 128, 173
 // as 64; only where all keys stay in the caches is that less, one request of 32896 tokens: 52 and 47).
-// float32 blocks hold 16 vectors.
+// Units of 256, which take a CU each, where every CU has 32 steps of KV heads' keys or more and units are cut (160
+// vectors: 16 such requests 152 us against 188 as 128, 6 requests 69 against 79; fewer steps lose: 192 vectors
+// of one request of 32896 tokens 58 against 53, 64 requests of up to 1980 tokens 140 against 130).  float32
+// blocks hold 16 vectors.
 //
 // Short units are taken whole, one per block: up to 8 steps always (64 decoded rows over up to 500 tokens:
 // 21.5 us against 27.0 cut), up to 32 where there is one for every CU (256 units of up to 2000 tokens: 41.6 against
 // 47.2; 128 units: 27.8 against 25.2; float32 units, whose steps take longer, not).  Else as many blocks as run at
-// once, two per CU (trees: 256 blocks 152 us, 512 142, 768 157), with 4 steps each at least.  `start` 4: 209, 203,
-// 205 us with 0, 4, 8 for 64 decoded rows over 512 to 8192 tokens.
+// once, two per CU (trees, units of 128: 256 blocks 152 us, 512 142, 768 157), with 4 steps each at least.
+// `start` 4: 209, 203, 205 us with 0, 4, 8 for 64 decoded rows over 512 to 8192 tokens.
 //
-// The workspace is sized as if units for every CU were cut too (`cut_all`): it then grows with every bound, and one
-// for the largest batch serves smaller ones.
+// The workspace is sized as if units for every CU were cut too and no unit held 256 (`cut_all`; 256 blocks of
+// 256 vectors need what 512 of 128 do): it then grows with every bound, and one for the largest batch serves
+// smaller ones.
 constexpr int kTreeBlocks = 512;
 inline TreeCut tree_cut(int batch, int max_q, int max_kv, int hq, int hkv, bool bf16, bool cut_all = false) {
   const int64_t vectors = (int64_t)max_q * (hq / hkv);
   const int64_t steps = ((int64_t)max_kv + kTreeStep - 1) / kTreeStep;
-  const int vt = vectors <= 16 || !bf16 ? 16 : vectors <= 32 ? 32 : vectors <= 64 ? 64 : 128;
+  const bool cu_wide = vectors > 128 && steps > 32 && (int64_t)batch * hkv * steps >= 16 * kTreeBlocks && !cut_all;
+  const int vt = vectors <= 16 || !bf16 ? 16 : vectors <= 32 ? 32 : vectors <= 64 ? 64 : cu_wide ? 256 : 128;
   TreeCut c;
   c.vt_log2 = log2_of(vt);
   c.tiles = (int)((vectors + vt - 1) / vt);
@@ -346,7 +351,7 @@ inline TreeCut tree_cut(int batch, int max_q, int max_kv, int hq, int hkv, bool 
   c.blocks = 0;
   c.start = 4;
   if (steps > 32 || (steps > 8 && (units < kTreeBlocks / 2 || !bf16 || cut_all)))
-    c.blocks = (int)std::max<int64_t>(std::min<int64_t>(kTreeBlocks, units * steps / 4), 1);
+    c.blocks = (int)std::max<int64_t>(std::min<int64_t>(vt == 256 ? kTreeBlocks / 2 : kTreeBlocks, units * steps / 4), 1);
   return c;
 }
 

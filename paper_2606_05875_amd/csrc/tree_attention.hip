@@ -12,12 +12,13 @@
 //          v_mfma_f32_16x16x32/16x16x16_bf16; their results are summed through LDS once per unit.
 //          64 decoded rows over 512 to 8192 tokens, 32/8 heads of 128: 204 us with the merge, 5.57 TB/s (a
 //          copy reaches 5.1); one row over 8192 tokens 16.4 us, over 32768 32 us.
-//  wide    more vectors (trees).  A wave holds 32 of them (v_mfma_f32_32x32x16_bf16) and the 2 or 4
+//  wide    more vectors (trees).  A wave holds 32 of them (v_mfma_f32_32x32x16_bf16) and the 2, 4 or 8
 //          waves of a block share every 64-token tile (a ring of stages, one barrier per tile); the
 //          products of the next tile's S run beside this tile's exponentials.  Bound: HBM and the latency of
 //          pages up to about 128 vectors (16 trees of 8 to 40 rows over 2000 to 12700 tokens, 32/8 heads of
-//          128: 142 us, 3.5 TB/s), products and exponentials beyond (64 rows of 64/8 heads: 92 us over 32896
-//          tokens, 0.75 PFLOP/s; 304 us over 131584, 0.91 PFLOP/s, the matrix units busy 56% of the cycles).
+//          128: 145 us, 3.5 TB/s; all of 40 rows 152 us), products and exponentials beyond (64 rows of 64/8
+//          heads: 92 us over 32896 tokens, 0.75 PFLOP/s; 299 us over 131584, 0.92 PFLOP/s, the matrix units
+//          busy 50% of the cycles).
 #include <math.h>
 
 #include <type_traits>
@@ -345,10 +346,9 @@ __global__ __launch_bounds__(kNW * 64, 2) void tree_attn_narrow_kernel(TreeAttn 
 // wide
 // ---------------------------------------------------------------------------
 constexpr int kWT = kTreeStep;
-// Stages of the K and V rings (64 KB, so that a CU holds two blocks, which run beside each other's starts,
-// ends and exponentials: blocks of 8 waves, one per CU, took 106 us against 102 for 64 rows over 32896
-// tokens with 64/8 heads, and 174 against 147 for trees of 8 to 40 rows over 2000 to 12700 tokens)
-constexpr int wide_stages(int d) { return d == 64 ? 4 : 2; }
+// Stages of the K and V rings: 64 KB, so that a CU holds two blocks, which run beside each other's starts, ends
+// and exponentials; 128 KB for 8 waves, which have a CU to themselves
+constexpr int wide_stages(int d, int vg) { return d == 64 || vg == 8 ? 4 : 2; }
 
 template <int D, int VG, bool kTiny>
 __global__ __launch_bounds__(VG * 64, VG == 2 ? 1 : 2) void tree_attn_wide_kernel(TreeAttn p, TreeCut cut, TreeWs ws, int lg) {
@@ -357,13 +357,14 @@ __global__ __launch_bounds__(VG * 64, VG == 2 ? 1 : 2) void tree_attn_wide_kerne
   constexpr int RB = D * 2;        // bytes per row
   constexpr int TB = kWT * RB;     // bytes of a tile of K or V
   constexpr int VT = 32 * VG;
-  constexpr int NB = wide_stages(D);
+  constexpr int NB = wide_stages(D, VG);
   // Copies go by groups of 16 rows, which lie in one page: wave w takes groups w, w + VG, .. of the
-  // tile's four
-  constexpr int WC = 16 / RPC;   // copies per group, K or V
-  constexpr int WG = 4 / VG;     // groups per wave
+  // tile's four, of 8 waves half of group w / 2
+  constexpr int GC = 16 / RPC;               // copies per group, K or V
+  constexpr int WC = VG == 8 ? GC / 2 : GC;  // of them a wave's
+  constexpr int WG = VG == 8 ? 1 : 4 / VG;   // groups per wave
   constexpr int WI = WG * WC;
-  static_assert(VG == 2 || VG == 4, "groups are shared evenly");
+  static_assert((VG == 2 || VG == 4 || VG == 8) && GC % 2 == 0, "groups are shared evenly");
   __shared__ __attribute__((aligned(1024))) uint8_t k_ring[NB * TB];
   __shared__ __attribute__((aligned(1024))) uint8_t v_ring[NB * TB];
   __shared__ uint32_t loose_l[2];
@@ -392,7 +393,8 @@ __global__ __launch_bounds__(VG * 64, VG == 2 ? 1 : 2) void tree_attn_wide_kerne
     const uint16_t* vc = static_cast<const uint16_t*>(p.v_cache) + (int64_t)g * D;
     const bool pool = p.n_pages > 0 && (kTiny || p.page_log2 >= 4);
     const int t_first = first * kWT;
-    auto group = [&](int k) { return w + VG * k; };
+    auto group = [&](int k) { return VG == 8 ? w >> 1 : w + VG * k; };
+    const int c0 = VG == 8 ? WC * (w & 1) : 0;  // this wave's first copy of a group
     auto page_at = [&](int t, int k) {
       return kTiny || t >= n ? -1 : page_of(p, table, t_first + t * kWT + 16 * group(k), rq.end);
     };
@@ -409,12 +411,12 @@ __global__ __launch_bounds__(VG * 64, VG == 2 ? 1 : 2) void tree_attn_wide_kerne
         const int64_t at = page[k] < 0 ? 0 : ((int64_t)page[k] << p.page_log2) + (t0 & ((1 << p.page_log2) - 1));
 #pragma unroll
         for (int i = 0; i < WC; ++i) {
-          const uint32_t dst = to + (group(k) * WC + i) * 1024;
-          const uint32_t chunk = kK ? kx ^ (i * 64) : vx;
+          const uint32_t dst = to + (group(k) * GC + c0 + i) * 1024;
+          const uint32_t chunk = kK ? kx ^ ((c0 + i) * 64) : vx;
           if (!kTiny)
-            copy16(from + (at + RPC * i) * p.kv_stride, coff + chunk, dst);
+            copy16(from + (at + RPC * (c0 + i)) * p.kv_stride, coff + chunk, dst);
           else
-            copy16(from + max(slot_of(p, b, t0 + RPC * i + cr, rq.end), (int64_t)0) * p.kv_stride + chunk / 2, dst);
+            copy16(from + max(slot_of(p, b, t0 + RPC * (c0 + i) + cr, rq.end), (int64_t)0) * p.kv_stride + chunk / 2, dst);
         }
       }
     };
@@ -762,7 +764,8 @@ hipError_t launch_bf16(const TreeAttn& p, void* workspace, hipStream_t stream) {
   if (c.vt_log2 == 4) QCF_NARROW(1);
   else if (c.vt_log2 == 5) QCF_NARROW(2);
   else if (c.vt_log2 == 6) QCF_WIDE(2);
-  else QCF_WIDE(4);
+  else if (c.vt_log2 == 7) QCF_WIDE(4);
+  else QCF_WIDE(8);
 #undef QCF_WIDE
 #undef QCF_NARROW
   if (c.blocks) launch_tree_merge<uint16_t, D>(p, c, ws, lg, stream);

@@ -362,6 +362,39 @@ def test_tree_attn_long(dtype, kv, new, hq, hkv, d):
     x.check(*x.call(max_q=x.max_q + 9, max_kv=x.max_kv + 5000))
 
 
+@pytest.mark.parametrize("kv,new,hq,hkv,d,ps", [
+    ([3000, 2000], [40, 30], 16, 4, 128, 16), ([0, 700, 64, 1], [33, 1, 70, 0], 8, 2, 64, 64), ([4100], [130], 8, 4, 64, 128),
+    ([40, 2500, 9], [17, 20, 1], 64, 4, 128, 128), ([90, 5], [65, 3], 4, 1, 128, 4), ([900], [300], 2, 1, 64, 8)])
+@pytest.mark.parametrize("tree", [False, True, "random"])
+def test_tree_attn_many_keys_by_the_bounds(kv, new, hq, hkv, d, ps, tree):
+    """More than 128 vectors per KV head and bounds that promise many keys: units of 256 vectors.  Values that are
+    not seen, pages that are not there, twice over a dirty workspace."""
+    say("tree attention many keys", kv, new, hq, hkv, d, ps, tree)
+    x = Batch(kv, new, hq, hkv, d, "bf16", ps, tree, seed=15, back=9)
+    most = 64 * (-(-8192 // (len(kv) * hkv)) + 1)
+    assert x.max_q * (hq // hkv) > 128 and most > x.max_kv
+    need = qcf.qcf_tree_attn_workspace_size(len(kv), x.max_q, most, hq, hkv, d, DT["bf16"])
+    ws = torch.full((need + 256,), 0xFF, dtype=torch.uint8, device="cuda")
+    a, b = x.call(ws=ws, max_kv=most), x.call(ws=ws, max_kv=most)
+    x.check(*a)
+    assert all(torch.equal(s, t) for s, t in zip(a, b))
+    bad = new[0] // 2
+    if new[0] > 1:
+        slot, sees = int(x.slot[0][kv[0] + bad]), x.see[0][:, kv[0] + bad]
+        for value in (math.inf, math.nan):
+            keep = x.v[slot].clone()
+            x.v[slot, :, 3] = value
+            o, c = host(x.call(max_kv=most)[0])[:new[0]], host(a[0])[:new[0]]
+            x.v[slot] = keep
+            np.testing.assert_array_equal(o[~sees], c[~sees])
+            np.testing.assert_array_equal(o[sees][..., 3], np.full_like(o[sees][..., 3], value))
+    t = x.table_h.copy()
+    t[0, 1] = -1
+    see = [s.copy() for s in x.see]
+    see[0][:, ps:2 * ps] = False
+    x.check(*x.call(table=i32(t), max_kv=most), see=see)
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 def test_tree_attn_unseen_values_stay_out(dtype):
     """Infinities and NaN in keys and values of drafted tokens reach the rows that see them and no other."""
