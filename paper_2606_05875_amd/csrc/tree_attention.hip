@@ -542,6 +542,7 @@ __global__ __launch_bounds__(VG * 64, VG == 2 ? 1 : 2) void tree_attn_wide_kerne
           pb[e >> 4][(e >> 3) & 1][e & 7] = pk[0];
           pb[e >> 4][(e >> 3) & 1][(e & 7) + 1] = pk[1];
         }
+        asm volatile("" : "+v"(psum));  // (in its group, not a chain of 32 sums behind the products)
       };
       if (kNext) {
 #pragma unroll
