@@ -589,12 +589,20 @@ __global__ __launch_bounds__(VG * 64, VG == 2 ? 1 : 2) void tree_attn_wide_kerne
     // K(t + 1) and V(t) are there, and everyone has read K(t) and V(t - 1), whose stages are filled next
     auto begin = [&](int t) {
       meet(t + NB - 1 < n ? NB - 2 : 0);
+      // the next page numbers are asked for before the copies and looked at behind them
+      int next[WG], at[WG];
+#pragma unroll
+      for (int k = 0; k < WG; ++k) {
+        at[k] = t_first + (t + NB + 1) * kWT + 16 * group(k);
+        next[k] = kTiny ? -1 : table[min(at[k] >> p.page_log2, p.max_pages - 1)];
+      }
       if (t + NB < n) copy(K, k_lds, t + NB, page);
       if (t + NB - 1 < n) copy(V, v_lds, t + NB - 1, pagev);
 #pragma unroll
       for (int k = 0; k < WG; ++k) {
         pagev[k] = page[k];
-        page[k] = page_at(t + NB + 1, k);
+        const int x = uni(next[k]);
+        page[k] = !kTiny && at[k] < rq.end && at[k] >> p.page_log2 < p.max_pages && x < p.n_pages ? max(x, -1) : -1;
       }
     };
     // element e of s is token t0 + 32 (e / 16) + 8 (e / 4 % 4) + 4 hi + e % 4
