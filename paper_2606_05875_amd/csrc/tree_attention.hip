@@ -16,9 +16,9 @@
 //          waves of a block share every 64-token tile (a ring of stages, one barrier per tile); the
 //          products of the next tile's S run beside this tile's exponentials.  Bound: HBM and the latency of
 //          pages up to about 128 vectors (16 trees of 8 to 40 rows over 2000 to 12700 tokens, 32/8 heads of
-//          128: 145 us, 3.5 TB/s; all of 40 rows 152 us), products and exponentials beyond (64 rows of 64/8
-//          heads: 92 us over 32896 tokens, 0.75 PFLOP/s; 299 us over 131584, 0.92 PFLOP/s, the matrix units
-//          busy 50% of the cycles).
+//          128: 132 to 140 us, 3.7 TB/s; all of 40 rows 148 us), products and exponentials beyond (64 rows of
+//          64/8 heads: 89 to 94 us over 32896 tokens, 0.75 PFLOP/s; 296 us over 131584, 0.93 PFLOP/s, the matrix
+//          units busy 50% of the cycles).
 #include <math.h>
 
 #include <type_traits>
