@@ -25,10 +25,12 @@ __device__ __forceinline__ uint32_t lds_addr(const void* p) {
 // address lds + 16 * lane (zeros when voff is past the descriptor's range).
 // Issued as inline assembly so that the compiler adds no waits of its own for
 // it: the caller orders the LDS traffic with explicit counter waits and barriers.
+// The load takes its LDS address from m0 and needs a wait state behind the write of m0,
+// which the compiler does not add inside an asm block either.
 __device__ __forceinline__ void dma16(const i32x4& rsrc, uint32_t voff, uint32_t lds) {
   // the LDS address is wave-uniform; readfirstlane keeps it in a scalar register
   const uint32_t la = __builtin_amdgcn_readfirstlane(lds);
-  asm volatile("s_mov_b32 m0, %0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds"
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds"
                :
                : "s"(la), "v"(voff), "s"(rsrc)
                : "memory");

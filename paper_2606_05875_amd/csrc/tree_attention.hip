@@ -33,14 +33,18 @@ typedef short v4s __attribute__((ext_vector_type(4)));
 typedef v4s __attribute__((address_space(3))) * lds_v4s;
 
 // 16 bytes per lane from base + off into LDS at byte address lds + 16 * lane, past the registers and
-// without a wait of the compiler's (the caller counts)
+// without a wait of the compiler's (the caller counts).  A load that takes its LDS address from m0 needs a wait
+// state behind the write of m0, which the compiler does not add inside an asm block.
 __device__ __forceinline__ void copy16(const void* base, uint32_t off, uint32_t lds) {
   const uint32_t la = __builtin_amdgcn_readfirstlane(lds);
-  asm volatile("s_mov_b32 m0, %0\n\tglobal_load_lds_dwordx4 %1, %2" : : "s"(la), "v"(off), "s"(uni((int64_t)base)) : "memory");
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2"
+               :
+               : "s"(la), "v"(off), "s"(uni((int64_t)base))
+               : "memory");
 }
 __device__ __forceinline__ void copy16(const void* from, uint32_t lds) {
   const uint32_t la = __builtin_amdgcn_readfirstlane(lds);
-  asm volatile("s_mov_b32 m0, %0\n\tglobal_load_lds_dwordx4 %1, off" : : "s"(la), "v"(from) : "memory");
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" : : "s"(la), "v"(from) : "memory");
 }
 
 // Weights are exp2(s * scale2 - ref) with a fused multiply-add, which keeps the product exact; its
