@@ -49,8 +49,9 @@ __device__ __forceinline__ void copy16(const void* from, uint32_t lds) {
 
 // Weights are exp2(s * scale2 - ref) with a fused multiply-add, which keeps the product exact; its
 // difference to the rounded maximum reaches 2^-24 of that, too much to be an exponent where maxima
-// pass 2^28.  Such logits are scaled (and rounded) first.
-__device__ __forceinline__ bool is_big(float m) { return __ballot(fabsf(finite(m)) > 0x1p28f) != 0; }
+// pass 2^28.  Such a vector's logits are scaled (and rounded) first; each lane's by its own vector's
+// maximum, so that the other vectors' bits do not hang on it.
+__device__ __forceinline__ bool is_big(float m) { return fabsf(finite(m)) > 0x1p28f; }
 
 // any of a 16-byte piece's 8 values infinite or NaN
 __device__ __forceinline__ bool not_finite(const uint4& x) {
@@ -247,8 +248,8 @@ __global__ __launch_bounds__(kNW * 64, 2) void tree_attn_narrow_kernel(TreeAttn 
           big[c] = is_big(mn);
         }
         const float ref = finite(m[c]);
-        if (big[c]) s[c] *= scale2;
         const float sc = big[c] ? 1.f : scale2;
+        if (__ballot(big[c])) s[c] *= big[c] ? scale2 : 1.f;
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
           pw[c][r] = __builtin_amdgcn_exp2f(fmaf(s[c][r], sc, -ref));
@@ -518,9 +519,10 @@ __global__ __launch_bounds__(VG * 64, VG == 2 ? 1 : 2) void tree_attn_wide_kerne
         m = mn;
         big = is_big(mn);
       }
-      if (big) {
-        s[0] *= scale2;
-        s[1] *= scale2;
+      if (__ballot(big)) {
+        const float f = big ? scale2 : 1.f;
+        s[0] *= f;
+        s[1] *= f;
       }
     };
     typedef float f32x2_t __attribute__((ext_vector_type(2)));

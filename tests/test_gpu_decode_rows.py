@@ -1,0 +1,35 @@
+"""What single rows of the attention over pages may rely on whatever the other rows hold.  Sizes reach every kernel: up to 16 and 32
+query vectors per KV head, 64, 128 and 256 per block, float32; short caches and ones that are cut over blocks."""
+import pytest
+import torch
+
+from test_gpu_decode import Batch, say
+
+pytestmark = pytest.mark.gpu
+
+# kv, new, hq, hkv, d, page size, max_kv (None: the batch's own)
+SIZES = [([70, 0], [3, 2], 8, 2, 64, 16, None), ([3000, 40], [1, 3], 16, 4, 128, 64, None), ([2500], [8], 8, 2, 128, 16, None),
+         ([200, 31], [16, 9], 8, 2, 64, 128, None), ([2600, 5], [15, 4], 32, 8, 128, 32, None), ([90], [11], 8, 2, 128, 4, None)]
+WIDE = [([900, 12], [30, 7], 16, 4, 128, 64, None), ([2300], [20], 16, 4, 64, 16, None), ([700, 64], [40, 9], 16, 4, 128, 16, 140000),
+        ([400], [33], 16, 4, 64, 32, 140000), ([60, 9], [17, 20], 8, 2, 128, 8, None)]
+
+
+@pytest.mark.parametrize("kv,new,hq,hkv,d,ps,most", SIZES + WIDE)
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_large_logits_leave_other_rows_bits(kv, new, hq, hkv, d, ps, most, dtype):
+    """One row and head with logits beyond 2^28: the others' bits are those of a call without it."""
+    say("large logits beside others", kv, new, hq, hkv, d, ps, most, dtype)
+    x = Batch(kv, new, hq, hkv, d, dtype, ps, True, seed=32, back=9)
+    most = x.max_kv if most is None else most
+    was = x.call(max_kv=most)
+    for row, head in ((0, 1), (new[0] - 1, hq - 1)):
+        keep = x.q[row, head].clone()
+        x.q[row, head] = 1e18
+        now = x.call(max_kv=most)
+        x.q[row, head] = keep
+        rest = torch.ones(was[1].shape, dtype=torch.bool, device="cuda")
+        rest[row, head] = False
+        assert now[1][row, head].abs() > 1e15
+        for a, b in zip(was, now):
+            n = int(x.cu[-1])
+            assert torch.equal(a[:n][rest[:n]], b[:n][rest[:n]])
