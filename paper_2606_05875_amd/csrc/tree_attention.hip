@@ -5,6 +5,13 @@
 // kernels of this library: a lane holds tokens' logits of ONE query vector, so its p are the second
 // product's operand as they stand.
 //
+// Weights enter the sum l as float32, and the second product as bf16.  Up to 64 query vectors they are two
+// bf16 numbers, the rounded p and what that rounding left (16 bits), and the output is off by its own rounding
+// alone (1.66e-3 of its norm from 64 bits, 64 decoded rows): a second product per V fragment, which waits for pages
+// hide (203.5 -> 204.7 us; 16 trees of 16 rows 114.0 -> 115.3).  Beyond, where products and exponentials
+// bound it, they are one bf16 number and the output 2.3e-3 off: two cost 16 trees of 8 to 40 rows 133 -> 170 us,
+// 64 rows over 32896 tokens 91 -> 116, over 131584 298 -> 406, and vector registers spill.
+//
 // Keys and values go from the pages into LDS without passing registers (16 bytes per lane); the
 // block table's entries come through the scalar cache, one per 16 tokens, a step ahead.
 //  narrow  up to 32 query vectors per request and KV head (one token, short chains).  Bound: HBM.  Four
@@ -229,7 +236,7 @@ __global__ __launch_bounds__(kNW * 64, 2) void tree_attn_narrow_kernel(TreeAttn 
         }
         asm volatile("" ::: "memory");
       }
-      v4s pb[NV];
+      v4s pb[NV], pl[NV];  // weights as bf16, and what that left of them
       float pw[NV][4];
 #pragma unroll
       for (int c = 0; c < NV; ++c) {
@@ -254,6 +261,7 @@ __global__ __launch_bounds__(kNW * 64, 2) void tree_attn_narrow_kernel(TreeAttn 
         for (int r = 0; r < 4; ++r) {
           pw[c][r] = __builtin_amdgcn_exp2f(fmaf(s[c][r], sc, -ref));
           pb[c][r] = (short)f2bf(pw[c][r]);
+          pl[c][r] = (short)f2bf(pw[c][r] - bf2f((uint16_t)pb[c][r]));
         }
         ls[c] += (pw[c][0] + pw[c][1]) + (pw[c][2] + pw[c][3]);
       }
@@ -287,7 +295,10 @@ __global__ __launch_bounds__(kNW * 64, 2) void tree_attn_narrow_kernel(TreeAttn 
       for (int mb = 0; mb < MB; ++mb) {
         const v4s va = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4s)(vl + vrd + ((mb ^ vsw) << 5)));
 #pragma unroll
-        for (int c = 0; c < NV; ++c) o[c][mb] = __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(va, pb[c], o[c][mb], 0, 0, 0);
+        for (int c = 0; c < NV; ++c) {
+          o[c][mb] = __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(va, pb[c], o[c][mb], 0, 0, 0);
+          o[c][mb] = __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(va, pl[c], o[c][mb], 0, 0, 0);
+        }
       }
       page = page1;
       page1 = page2;
@@ -363,6 +374,7 @@ __global__ __launch_bounds__(VG * 64, VG == 2 ? 1 : 2) void tree_attn_wide_kerne
   constexpr int TB = kWT * RB;     // bytes of a tile of K or V
   constexpr int VT = 32 * VG;
   constexpr int NB = wide_stages(D, VG);
+  constexpr bool kTwo = VG == 2;   // weights of two bf16 numbers
   // Copies go by groups of 16 rows, which lie in one page: wave w takes groups w, w + VG, .. of the
   // tile's four, of 8 waves half of group w / 2
   constexpr int GC = 16 / RPC;               // copies per group, K or V
@@ -527,9 +539,9 @@ __global__ __launch_bounds__(VG * 64, VG == 2 ? 1 : 2) void tree_attn_wide_kerne
     };
     typedef float f32x2_t __attribute__((ext_vector_type(2)));
     typedef __bf16 bf16x2_t __attribute__((ext_vector_type(2)));
-    // P of the tile; with kNext S of the next one beside it: one product per fenced group with its K fragment
+    // P of the tile (kTwo: what rounding left of it in pl); with kNext S of the next one beside it: one product per fenced group with its K fragment
     // read four groups ahead, a group's arguments, exponentials and sums in three groups in turn
-    auto weights = [&](auto next, const uint8_t* kn, f32x16 (&sn)[2], f32x16 (&s)[2], bf16x8 (&pb)[2][2]) {
+    auto weights = [&](auto next, const uint8_t* kn, f32x16 (&sn)[2], f32x16 (&s)[2], bf16x8 (&pb)[2][2], bf16x8 (&pl)[2][2]) {
       constexpr bool kNext = decltype(next)::value;
       constexpr int NM = 2 * NS, EG = 32 / NM, PF = 4;
       const float nm = -finite(m), sc = big ? 1.f : scale2;
@@ -547,6 +559,11 @@ __global__ __launch_bounds__(VG * 64, VG == 2 ? 1 : 2) void tree_attn_wide_kerne
           const bf16x2_t pk = __builtin_convertvector((f32x2_t){pw[e], pw[e + 1]}, bf16x2_t);
           pb[e >> 4][(e >> 3) & 1][e & 7] = pk[0];
           pb[e >> 4][(e >> 3) & 1][(e & 7) + 1] = pk[1];
+          if constexpr (kTwo) {
+            const bf16x2_t rest = __builtin_convertvector((f32x2_t){pw[e] - (float)pk[0], pw[e + 1] - (float)pk[1]}, bf16x2_t);
+            pl[e >> 4][(e >> 3) & 1][e & 7] = rest[0];
+            pl[e >> 4][(e >> 3) & 1][(e & 7) + 1] = rest[1];
+          }
         }
         asm volatile("" : "+v"(psum));  // (in its group, not a chain of 32 sums behind the products)
       };
@@ -572,7 +589,7 @@ __global__ __launch_bounds__(VG * 64, VG == 2 ? 1 : 2) void tree_attn_wide_kerne
       ls += psum;
     };
     // O += V^T P^T, one product per fenced group with its V fragment read four groups ahead
-    auto products_o = [&](const uint8_t* vl, bf16x8 (&pb)[2][2]) {
+    auto products_o = [&](const uint8_t* vl, bf16x8 (&pb)[2][2], bf16x8 (&pl)[2][2]) {
       constexpr int MB = D / 32, NM = 4 * MB, PF = 4;
       auto v_frag = [&](int j) {
         const uint8_t* at = vl + (j / MB) * 16 * RB + (vrd ^ ((j % MB) << 6));
@@ -588,6 +605,8 @@ __global__ __launch_bounds__(VG * 64, VG == 2 ? 1 : 2) void tree_attn_wide_kerne
         __builtin_amdgcn_sched_barrier(0);
         if (j + PF < NM) vf[j + PF] = v_frag(j + PF);
         o[j % MB] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[j], pb[j / (2 * MB)][(j / MB) & 1], o[j % MB], 0, 0, 0);
+        if constexpr (kTwo)
+          o[j % MB] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[j], pl[j / (2 * MB)][(j / MB) & 1], o[j % MB], 0, 0, 0);
       }
       __builtin_amdgcn_sched_barrier(0);
     };
@@ -615,10 +634,10 @@ __global__ __launch_bounds__(VG * 64, VG == 2 ? 1 : 2) void tree_attn_wide_kerne
     // the tiles before the first that is the last one or has tokens that are not there or not seen by all
     const int plain = holes ? 0 : min(n - 1, (min(rq.kv, rq.end) - t_first) / kWT) & ~1;
     auto plain_step = [&](int t, f32x16 (&s)[2], f32x16 (&sn)[2]) {
-      bf16x8 pb[2][2];
+      bf16x8 pb[2][2], pl[2][2];
       maximum(s);
-      weights(std::true_type{}, k_ring + ((t + 1) & (NB - 1)) * TB, sn, s, pb);
-      products_o(v_ring + (t & (NB - 1)) * TB, pb);
+      weights(std::true_type{}, k_ring + ((t + 1) & (NB - 1)) * TB, sn, s, pb, pl);
+      products_o(v_ring + (t & (NB - 1)) * TB, pb, pl);
     };
     // Tiles with tokens that are not there or that some row does not see.  held: those that are there, as
     // bits; true if there is something to do (for the whole block).
@@ -656,7 +675,7 @@ __global__ __launch_bounds__(VG * 64, VG == 2 ? 1 : 2) void tree_attn_wide_kerne
       const int t0 = t_first + t * kWT;
       const uint8_t* kn = k_ring + ((t + 1) & (NB - 1)) * TB;
       const uint8_t* vl = v_ring + (t & (NB - 1)) * TB;
-      bf16x8 pb[2][2];
+      bf16x8 pb[2][2], pl[2][2];
       uint64_t held, loose = 0;
       uint32_t sees[2] = {0, 0};
       if (is_edge(t, held)) {
@@ -671,7 +690,7 @@ __global__ __launch_bounds__(VG * 64, VG == 2 ? 1 : 2) void tree_attn_wide_kerne
         }
       }
       maximum(s);
-      weights(std::false_type{}, kn, s, s, pb);
+      weights(std::false_type{}, kn, s, s, pb, pl);
       if (loose) {
         for (uint64_t left = loose; left; left &= left - 1) {
           const int k = __builtin_ctzll(left);
@@ -695,7 +714,7 @@ __global__ __launch_bounds__(VG * 64, VG == 2 ? 1 : 2) void tree_attn_wide_kerne
         }
         take_out(t, loose);
       }
-      products_o(vl, pb);
+      products_o(vl, pb, pl);
       if (t + 1 < n) products(kn, s);
     };
 

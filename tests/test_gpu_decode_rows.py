@@ -1,9 +1,12 @@
-"""What single rows of the attention over pages may rely on whatever the other rows hold.  Sizes reach every kernel: up to 16 and 32
-query vectors per KV head, 64, 128 and 256 per block, float32; short caches and ones that are cut over blocks."""
+"""What single rows of the attention over pages may rely on: how exact their weights are, and that no other row's
+values change their bits.  Sizes reach every kernel: up to 16 and 32 query vectors per KV head, 64, 128 and 256 per
+block, float32; short caches and ones that are cut over blocks."""
+import numpy as np
 import pytest
 import torch
 
-from test_gpu_decode import Batch, say
+from oracle import decode as D
+from test_gpu_decode import HALF, Batch, host, say, within
 
 pytestmark = pytest.mark.gpu
 
@@ -12,6 +15,24 @@ SIZES = [([70, 0], [3, 2], 8, 2, 64, 16, None), ([3000, 40], [1, 3], 16, 4, 128,
          ([200, 31], [16, 9], 8, 2, 64, 128, None), ([2600, 5], [15, 4], 32, 8, 128, 32, None), ([90], [11], 8, 2, 128, 4, None)]
 WIDE = [([900, 12], [30, 7], 16, 4, 128, 64, None), ([2300], [20], 16, 4, 64, 16, None), ([700, 64], [40, 9], 16, 4, 128, 16, 140000),
         ([400], [33], 16, 4, 64, 32, 140000), ([60, 9], [17, 20], 8, 2, 128, 8, None)]
+
+
+@pytest.mark.parametrize("kv,new,hq,hkv,d,ps,most", SIZES)
+def test_weights_keep_16_bits(kv, new, hq, hkv, d, ps, most):
+    """Up to 64 query vectors per KV head a bf16 call's weights are two bf16 numbers: the first is off by at most
+    2^-8 of the weight, the second by 2^-8 of that.  The other terms are those of test_gpu_decode."""
+    say("weights keep 16 bits", kv, new, hq, hkv, d, ps)
+    x = Batch(kv, new, hq, hkv, d, "bf16", ps, True, seed=31, back=9)
+    assert x.max_q * (hq // hkv) <= 64
+    out, lse = x.call()
+    x.check(out, lse)
+    o = host(out)
+    for b in range(len(kv)):
+        a, z = x.cu[b], x.cu[b + 1]
+        s = x.see[b]
+        want, wl, absv, absx = D.tree_attention(host(x.q[a:z]), x.kh[b], x.vh[b], s, x.scale)
+        off = d * 2.0 ** -24 * absx + 3 * 2.0 ** -23 * (np.abs(wl) + absx) + (s.shape[1] + 16) * 2.0 ** -24
+        within(o[a:z], want, HALF["bf16"] * np.abs(want) + (2 * off + 2.0 ** -16)[..., None] * absv, f"request {b}")
 
 
 @pytest.mark.parametrize("kv,new,hq,hkv,d,ps,most", SIZES + WIDE)
