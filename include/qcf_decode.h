@@ -155,7 +155,8 @@ qcf_status qcf_rope_store(void* k_cache, void* v_cache, int64_t n_slots, int64_t
  * t = kv_len[b] + j (whose keys and values are in their slots already), those
  * whose bit j of row r's mask is set; without a mask those with j <= i (one
  * decoded token, a chain of drafts, a prompt).  Token t sits in the slot that the
- * block table gives it.  A row that sees no token gets zeros (and lse = -inf).
+ * block table gives it.  A row that sees no token gets zeros (and lse = -inf); one
+ * that sees only logits of -infinity, or a NaN, is NaN (lse too).
  * Values a row does not see never reach it, whatever they hold.
  *   out, q     [n_rows, n_q_heads, head_dim]; rows at and behind cu_q[batch] are
  *              neither read nor written

@@ -223,6 +223,17 @@ __device__ __forceinline__ uint32_t tree_sees(const TreeAttn& p, const TreeReque
 // a running maximum as the reference of exponentials: 0 while nothing has been seen
 __device__ __forceinline__ float finite(float m) { return m == -INFINITY ? 0.f : m; }
 
+// A row whose maximum stays -infinity either saw no token, and gives zeros, or only logits of -infinity or NaN,
+// and is NaN, as 0 / 0 is.  Its sum tells: while the maximum is -infinity, a tile with tokens that it sees adds 1 (or
+// the NaN), which the factor of a later, finite maximum turns to nothing.
+__device__ __forceinline__ float gap(float m, float to) { return m == to ? 0.f : m - to; }  // exponent of that factor
+__device__ __forceinline__ float row_scale(float m, float l) {
+  return m != -INFINITY ? 1.f / l : l == 0.f ? 0.f : __builtin_nanf("");
+}
+__device__ __forceinline__ float row_lse(float m, float l) {
+  return m != -INFINITY ? (m + log2f(l)) * kLn2 : l == 0.f ? -INFINITY : __builtin_nanf("");
+}
+
 typedef const int32_t __attribute__((address_space(4))) * const_i32;
 
 // The page of 16 tokens from t0 on (t0 a multiple of 16, pages of 16 rows and more), or -1
@@ -278,7 +289,7 @@ __global__ __launch_bounds__(kMergeWaves * 64) void tree_attn_merge_kernel(TreeA
     const int n = min(64, x1 - xb + 1);
     const float2 ml = l < n ? ws.ml[slot(xb + l)] : make_float2(-INFINITY, 0.f);
     const float mn = fmaxf(mx, wave_max(ml.x));
-    const float f = __builtin_amdgcn_exp2f(ml.x - finite(mn)), fa = __builtin_amdgcn_exp2f(mx - finite(mn));
+    const float f = __builtin_amdgcn_exp2f(gap(ml.x, mn)), fa = __builtin_amdgcn_exp2f(gap(mx, mn));
     lt = lt * fa + wave_sum(ml.y * f);
     mx = mn;
     a.x *= fa;
@@ -308,12 +319,11 @@ __global__ __launch_bounds__(kMergeWaves * 64) void tree_attn_merge_kernel(TreeA
     a.z += __shfl_xor(a.z, m, 64);
     a.w += __shfl_xor(a.w, m, 64);
   }
-  const bool none = mx == -INFINITY;
-  const float inv = none ? 0.f : 1.f / lt;
+  const float inv = row_scale(mx, lt);
   const int64_t at = (q.r0 + i) * p.hq + h;
   if (lr == 0)
     store4(static_cast<T*>(p.out) + at * D + 4 * lc, make_float4(a.x * inv, a.y * inv, a.z * inv, a.w * inv));
-  if (p.lse && l == 0) p.lse[at] = none ? -INFINITY : (mx + log2f(lt)) * kLn2;
+  if (p.lse && l == 0) p.lse[at] = row_lse(mx, lt);
 }
 
 inline int log2_of(int x) { return __builtin_ctz((unsigned)x); }

@@ -243,12 +243,12 @@ __global__ __launch_bounds__(kNW * 64, 2) void tree_attn_narrow_kernel(TreeAttn 
         float mt = fmaxf(fmaxf(s[c][0], s[c][1]), fmaxf(s[c][2], s[c][3])) * scale2;
         // lazy rescale: a stale maximum stays unless the vector's grew by more than 2^8 (by each
         // vector's own, so that no row's bits hang on another's)
-        if (__ballot(mt > m[c] + 8.f)) {
+        if (__ballot(!(mt < m[c] + 8.f))) {  // (no maximum yet: row_scale)
           mt = fmaxf(mt, __shfl_xor(mt, 16, 64));
           mt = fmaxf(mt, __shfl_xor(mt, 32, 64));
           const float mn = mt > m[c] + 8.f ? mt : m[c];
-          const float alpha = __builtin_amdgcn_exp2f(m[c] - finite(mn));
-          ls[c] *= alpha;
+          const float alpha = __builtin_amdgcn_exp2f(gap(m[c], mn));
+          ls[c] = fmaf(ls[c], alpha, mn == -INFINITY && (!edge || sees[c]) ? 1.f : 0.f);
 #pragma unroll
           for (int mb = 0; mb < MB; ++mb) o[c][mb] *= alpha;
           m[c] = mn;
@@ -332,7 +332,7 @@ __global__ __launch_bounds__(kNW * 64, 2) void tree_attn_narrow_kernel(TreeAttn 
       float4 a = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
       for (int k = 0; k < kNW; ++k) {
-        const float f = __builtin_amdgcn_exp2f(ml[k].x - finite(mx));
+        const float f = __builtin_amdgcn_exp2f(gap(ml[k].x, mx));
         const float4 x = o_l[(k * VT + v) * (D / 4) + (i4 ^ (v & 7))];
         lt += f * ml[k].y;
         a.x += f * x.x;
@@ -345,11 +345,10 @@ __global__ __launch_bounds__(kNW * 64, 2) void tree_attn_narrow_kernel(TreeAttn 
         if (i4 == 0) ws.ml[(int64_t)slot * VT + v] = make_float2(mx, lt);
       } else {
         const int64_t at = (rq.r0 + i) * p.hq + (g << lg) + (vec & ((1 << lg) - 1));
-        const bool none = mx == -INFINITY;
-        const float inv = none ? 0.f : 1.f / lt;
+        const float inv = row_scale(mx, lt);
         *reinterpret_cast<uint2*>(static_cast<uint16_t*>(p.out) + at * D + 4 * i4) =
             make_uint2(pack_bf16x2(a.x * inv, a.y * inv), pack_bf16x2(a.z * inv, a.w * inv));
-        if (p.lse && i4 == 0) p.lse[at] = none ? -INFINITY : (mx + log2f(lt)) * kLn2;
+        if (p.lse && i4 == 0) p.lse[at] = row_lse(mx, lt);
       }
     }
     // everyone has read the results, which the next unit's tiles go over (stores need not be waited for)
@@ -514,18 +513,19 @@ __global__ __launch_bounds__(VG * 64, VG == 2 ? 1 : 2) void tree_attn_wide_kerne
           s[hb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k_frag(kl, hb * NS + st), qreg[st], s[hb], 0, 0, 0);
       }
     };
-    // the running maximum of the tile's logits, and what the exponentials are taken of
-    auto maximum = [&](f32x16 (&s)[2]) {
+    // the running maximum of the tile's logits (with tokens that the vector sees or without), and what the
+    // exponentials are taken of
+    auto maximum = [&](f32x16 (&s)[2], bool any) {
       float mt = s[0][0];
 #pragma unroll
       for (int e = 1; e < 32; ++e) mt = fmaxf(mt, s[e >> 4][e & 15]);
       mt *= scale2;
       // lazily and by each vector's own growth (see the narrow kernel)
-      if (__ballot(mt > m + 8.f)) {
+      if (__ballot(!(mt < m + 8.f))) {
         mt = fmaxf(mt, __shfl_xor(mt, 32, 64));
         const float mn = mt > m + 8.f ? mt : m;
-        const float alpha = __builtin_amdgcn_exp2f(m - finite(mn));
-        ls *= alpha;
+        const float alpha = __builtin_amdgcn_exp2f(gap(m, mn));
+        ls = fmaf(ls, alpha, mn == -INFINITY && any ? 1.f : 0.f);
 #pragma unroll
         for (int mb = 0; mb < D / 32; ++mb) o[mb] *= alpha;
         m = mn;
@@ -635,7 +635,7 @@ __global__ __launch_bounds__(VG * 64, VG == 2 ? 1 : 2) void tree_attn_wide_kerne
     const int plain = holes ? 0 : min(n - 1, (min(rq.kv, rq.end) - t_first) / kWT) & ~1;
     auto plain_step = [&](int t, f32x16 (&s)[2], f32x16 (&sn)[2]) {
       bf16x8 pb[2][2], pl[2][2];
-      maximum(s);
+      maximum(s, true);
       weights(std::true_type{}, k_ring + ((t + 1) & (NB - 1)) * TB, sn, s, pb, pl);
       products_o(v_ring + (t & (NB - 1)) * TB, pb, pl);
     };
@@ -678,7 +678,8 @@ __global__ __launch_bounds__(VG * 64, VG == 2 ? 1 : 2) void tree_attn_wide_kerne
       bf16x8 pb[2][2], pl[2][2];
       uint64_t held, loose = 0;
       uint32_t sees[2] = {0, 0};
-      if (is_edge(t, held)) {
+      const bool edge = is_edge(t, held);
+      if (edge) {
         loose = clean(t, held);
 #pragma unroll
         for (int hb = 0; hb < 2; ++hb) {
@@ -689,7 +690,7 @@ __global__ __launch_bounds__(VG * 64, VG == 2 ? 1 : 2) void tree_attn_wide_kerne
             if (!(sees[hb] >> (8 * (v >> 2) + 4 * hi + (v & 3)) & 1)) s[hb][v] = -INFINITY;
         }
       }
-      maximum(s);
+      maximum(s, !edge || (sees[0] | sees[1]) != 0);
       weights(std::false_type{}, kn, s, s, pb, pl);
       if (loose) {
         for (uint64_t left = loose; left; left &= left - 1) {
@@ -746,7 +747,6 @@ __global__ __launch_bounds__(VG * 64, VG == 2 ? 1 : 2) void tree_attn_wide_kerne
     }
     ls += __shfl_xor(ls, 32, 64);
     if (valid) {
-      const bool none = m == -INFINITY;
       if (slot >= 0) {
         const int64_t at = (int64_t)slot * VT + 32 * w + lq;
         if (hi == 0) ws.ml[at] = make_float2(m, ls);
@@ -757,7 +757,7 @@ __global__ __launch_bounds__(VG * 64, VG == 2 ? 1 : 2) void tree_attn_wide_kerne
             reinterpret_cast<float4*>(ws.o)[at * (D / 4) + 8 * mb + 2 * c + hi] =
                 make_float4(o[mb][4 * c], o[mb][4 * c + 1], o[mb][4 * c + 2], o[mb][4 * c + 3]);
       } else {
-        const float inv = none ? 0.f : 1.f / ls;
+        const float inv = row_scale(m, ls);
         const int64_t at = row * p.hq + head;
         uint16_t* out = static_cast<uint16_t*>(p.out) + at * D + 4 * hi;
 #pragma unroll
@@ -767,7 +767,7 @@ __global__ __launch_bounds__(VG * 64, VG == 2 ? 1 : 2) void tree_attn_wide_kerne
             *reinterpret_cast<uint2*>(out + 32 * mb + 8 * c) =
                 make_uint2(pack_bf16x2(o[mb][4 * c] * inv, o[mb][4 * c + 1] * inv),
                            pack_bf16x2(o[mb][4 * c + 2] * inv, o[mb][4 * c + 3] * inv));
-        if (p.lse && hi == 0) p.lse[at] = none ? -INFINITY : (m + log2f(ls)) * kLn2;
+        if (p.lse && hi == 0) p.lse[at] = row_lse(m, ls);
       }
     }
     // everyone has read its tiles, which the next unit's go over (stores need not be waited for)

@@ -140,12 +140,12 @@ __global__ __launch_bounds__(kW * 64, 2) void tree_attn_f32_kernel(TreeAttn p, T
       }
       // lazy rescale: a stale maximum stays unless the vector's grew by more than 2^8 (by each vector's
       // own, so that no row's bits hang on another's)
-      if (__ballot(mt > m + 8.f)) {
+      if (__ballot(!(mt < m + 8.f))) {  // (no maximum yet: row_scale)
         mt = fmaxf(mt, __shfl_xor(mt, 16, 64));
         mt = fmaxf(mt, __shfl_xor(mt, 32, 64));
         const float mn = mt > m + 8.f ? mt : m;
-        const float alpha = exp2f(m - finite(mn));
-        ls *= alpha;
+        const float alpha = exp2f(gap(m, mn));
+        ls = fmaf(ls, alpha, mn == -INFINITY && sees ? 1.f : 0.f);
 #pragma unroll
         for (int mb = 0; mb < NB; ++mb) o[mb] *= alpha;
         m = mn;
@@ -207,7 +207,7 @@ __global__ __launch_bounds__(kW * 64, 2) void tree_attn_f32_kernel(TreeAttn p, T
       float4 a = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
       for (int k = 0; k < kW; ++k) {
-        const float f = exp2f(ml[k].x - finite(mx));
+        const float f = exp2f(gap(ml[k].x, mx));
         const float4 y = o_l[(k * kVt + v) * (D / 4) + (i4 ^ (v & 7))];
         lt += f * ml[k].y;
         a.x += f * y.x;
@@ -220,10 +220,9 @@ __global__ __launch_bounds__(kW * 64, 2) void tree_attn_f32_kernel(TreeAttn p, T
         if (i4 == 0) ws.ml[(int64_t)slot * kVt + v] = make_float2(mx, lt);
       } else {
         const int64_t at = (rq.r0 + i) * p.hq + (g << lg) + (mine & ((1 << lg) - 1));
-        const bool none = mx == -INFINITY;
-        const float inv = none ? 0.f : 1.f / lt;
+        const float inv = row_scale(mx, lt);
         store4(static_cast<float*>(p.out) + at * D + 4 * i4, make_float4(a.x * inv, a.y * inv, a.z * inv, a.w * inv));
-        if (p.lse && i4 == 0) p.lse[at] = none ? -INFINITY : (mx + log2f(lt)) * kLn2;
+        if (p.lse && i4 == 0) p.lse[at] = row_lse(mx, lt);
       }
     }
     __syncthreads();  // (the next unit's results go over them)

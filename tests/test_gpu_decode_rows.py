@@ -1,6 +1,8 @@
-"""What single rows of the attention over pages may rely on: how exact their weights are, and that no other row's
-values change their bits.  Sizes reach every kernel: up to 16 and 32 query vectors per KV head, 64, 128 and 256 per
+"""What single rows of the attention over pages may rely on: how exact their weights are, that no other row's
+values change their bits, and what they give where logits are not numbers.  Sizes reach every kernel: up to 16 and 32 query vectors per KV head, 64, 128 and 256 per
 block, float32; short caches and ones that are cut over blocks."""
+import math
+
 import numpy as np
 import pytest
 import torch
@@ -54,3 +56,57 @@ def test_large_logits_leave_other_rows_bits(kv, new, hq, hkv, d, ps, most, dtype
         for a, b in zip(was, now):
             n = int(x.cu[-1])
             assert torch.equal(a[:n][rest[:n]], b[:n][rest[:n]])
+
+
+@pytest.mark.parametrize("kv,new,hq,hkv,d,ps,most", SIZES + WIDE)
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_logits_that_are_not_finite(kv, new, hq, hkv, d, ps, most, dtype):
+    """As the formula gives: a row whose logits are all NaN, or all -infinity, is NaN (its log-sum-exp too: -infinity
+    stands for a row that sees no token); where some are -infinity these weigh nothing."""
+    say("logits that are not finite", kv, new, hq, hkv, d, ps, most, dtype)
+    x = Batch(kv, new, hq, hkv, d, dtype, ps, "random", seed=33)
+    most = x.max_kv if most is None else most
+    n = int(x.cu[-1])
+    was, wl = (host(t)[:n] for t in x.call(max_kv=most))
+    rest = np.ones(wl.shape, bool)
+    row, head = new[0] - 1, hq - 1
+    rest[row, head] = False
+    keep = x.q[row, head].clone()
+    x.q[row, head, 5] = math.nan
+    o, e = (host(t)[:n] for t in x.call(max_kv=most))
+    x.q[row, head] = keep
+    if x.see[0][row].any():
+        assert np.isnan(o[row, head]).all() and np.isnan(e[row, head])
+    else:
+        assert (o[row, head] == 0).all() and e[row, head] == -math.inf
+    np.testing.assert_array_equal(o[rest], was[rest])
+    np.testing.assert_array_equal(e[rest], wl[rest])
+
+    x.q[:n, :, 7] = 1.0
+    was, wl = (host(t)[:n] for t in x.call(max_kv=most))
+    x.check(*x.call(max_kv=most))
+    half = x.slot[0][::2]                                   # every other token of request 0, then all of them
+    kbuf, kh = x.kbuf.clone(), x.kh[0].copy()
+    x.k[torch.from_numpy(half).cuda(), :, 7] = -math.inf
+    see = [s.copy() for s in x.see]
+    see[0][:, ::2] = False
+    o, e = (host(t)[:n] for t in x.call(max_kv=most))
+    some, any_ = see[0].any(1), x.see[0].any(1)
+    for i in range(new[0]):
+        if some[i]:
+            want, _, absv, _ = D.tree_attention(host(x.q[i:i + 1]), kh, x.vh[0], see[0][i:i + 1], x.scale)
+            within(o[i:i + 1], want, HALF[dtype] * np.abs(want) + (2.0 ** -8 + 2.0 ** -10) * absv, f"row {i}")
+        elif any_[i]:
+            assert np.isnan(o[i]).all() and np.isnan(e[i]).all(), i
+        else:
+            assert (o[i] == 0).all() and (e[i] == -math.inf).all(), i
+    x.k[torch.from_numpy(x.slot[0]).cuda(), :, 7] = -math.inf
+    o, e = (host(t)[:n] for t in x.call(max_kv=most))
+    x.kbuf.copy_(kbuf)
+    for i in range(new[0]):
+        if any_[i]:
+            assert np.isnan(o[i]).all() and np.isnan(e[i]).all(), i
+        else:
+            assert (o[i] == 0).all() and (e[i] == -math.inf).all(), i
+    np.testing.assert_array_equal(o[new[0]:], was[new[0]:])  # the other requests
+    np.testing.assert_array_equal(e[new[0]:], wl[new[0]:])
