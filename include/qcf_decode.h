@@ -183,7 +183,9 @@ qcf_status qcf_rope_store(void* k_cache, void* v_cache, int64_t n_slots, int64_t
  * bits do not depend on the other rows' values.
  * Errors: null pointers, softmax_scale not positive and finite, page_size not a
  * power of two (UNSUPPORTED), row strides of 128 MB and more, batch * max_q *
- * n_q_heads beyond int32 or max_kv within 2^20 of it (UNSUPPORTED), workspace.
+ * n_q_heads beyond int32, max_kv within 2^20 of it, or, with max_kv up to 2048, 2^23
+ * tiles and more (of 16 to 128 query vectors, each of one request and KV head;
+ * UNSUPPORTED), workspace.
  */
 size_t qcf_tree_attn_workspace_size(int batch, int max_q, int max_kv, int n_q_heads,
                                     int n_kv_heads, int head_dim, qcf_dtype dtype);
@@ -214,11 +216,11 @@ qcf_status qcf_tree_attn(void* out, float* lse, const void* q, int64_t n_rows,
  * P is too, the token is -1.  Probabilities that are not above zero (NaN too)
  * count as zero.  Sums, products and comparisons are float64.
  *   target, draft  [n_rows, vocab], rows row_stride elements apart (any stride >=
- *              vocab; the same for both); draft may be NULL; vocab <= 2^28
+ *              vocab; the same for both); draft may be NULL; vocab <= 2^28 - 8192
  *   tokens     int32 [n_rows]; a child's token outside [0, vocab) is rejected (R unchanged)
  *   parents    int32 [n_rows] index of the parent within the request, below the
  *              row's own (others are not reached), or NULL: a chain, parent i - 1
- *   cu_rows    int32 [batch + 1]; max_rows >= every request's rows, at most QCF_MAX_TREE
+ *   cu_rows    int32 [batch + 1], batch < 2^22; max_rows >= every request's rows, at most QCF_MAX_TREE
  *              (further rows are ignored)
  *   u_accept   float32 [n_rows], u_next float32 [batch], in [0, 1)
  *   n_out      int32 [batch] accepted drafts + 1 (0 for a request without rows)

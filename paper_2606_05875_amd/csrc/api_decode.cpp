@@ -156,7 +156,8 @@ qcf_status qcf_tree_attn(void* out, float* lse, const void* q, int64_t n_rows,
   if (!kv_stride_ok(kv_row_stride, n_kv_heads, head_dim, dtype)) return QCF_ERR_INVALID_ARG;
   // the kernels' 32-bit numbers: offsets inside 16 rows, (row, head) pairs, tokens a few tiles on
   if (kv_row_stride > INT32_MAX / (16 * esize(dtype)) || max_kv > INT32_MAX - (1 << 20) ||
-      (int64_t)batch * max_q > INT32_MAX / n_q_heads)
+      (int64_t)batch * max_q > INT32_MAX / n_q_heads ||
+      !qcf::tree_attn_fits(batch, max_q, max_kv, n_q_heads, n_kv_heads, dtype == QCF_BF16))
     return QCF_ERR_UNSUPPORTED;
   const bool empty = n_rows == 0 || batch == 0 || max_q == 0;
   const bool no_kv = empty || max_kv == 0 || max_pages == 0 || n_slots >> lp == 0;
@@ -194,7 +195,7 @@ qcf_status qcf_verify_drafts(int32_t* n_out, int32_t* path, int32_t* out_tokens,
   if (!dtype_ok(dtype)) return QCF_ERR_UNSUPPORTED;
   if (n_rows < 0 || n_rows > INT32_MAX || vocab <= 0 || batch < 0 || max_rows < 0 || row_stride < vocab)
     return QCF_ERR_INVALID_ARG;
-  if (max_rows > QCF_MAX_TREE || vocab > 1 << 28) return QCF_ERR_UNSUPPORTED;
+  if (max_rows > QCF_MAX_TREE || vocab > qcf::kVerifyMaxVocab || batch > qcf::kVerifyMaxBatch) return QCF_ERR_UNSUPPORTED;
   const bool empty = batch == 0, no_rows = empty || n_rows == 0 || max_rows == 0;
   if (!index_ok(n_out, empty) || !index_ok(path, empty || max_rows == 0) ||
       !index_ok(out_tokens, empty || max_rows == 0) || !index_ok(cu_rows, empty) ||

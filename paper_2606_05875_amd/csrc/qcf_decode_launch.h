@@ -7,6 +7,13 @@
 
 namespace qcf {
 
+// A launch takes fewer than 2^32 threads along x: longer grids go on along y.
+constexpr int kGridLog2 = 23;
+inline dim3 grid_of(int64_t blocks) {
+  const int64_t x = (int64_t)1 << kGridLog2;
+  return blocks <= x ? dim3((unsigned)blocks) : dim3((unsigned)x, (unsigned)((blocks + x - 1) >> kGridLog2));
+}
+
 struct PagePlan {
   int32_t* block_table;
   int64_t table_stride;
@@ -61,6 +68,8 @@ struct TreeAttn {
   int batch, max_q, max_kv, hq, hkv;
   float scale;
 };
+// Whether a call whose units are taken whole, a block each, is one grid (cut ones always are).
+bool tree_attn_fits(int batch, int max_q, int max_kv, int hq, int hkv, bool bf16);
 size_t tree_attn_workspace(int batch, int max_q, int max_kv, int hq, int hkv, int head_dim, bool bf16);
 hipError_t launch_tree_attn_f32(const TreeAttn& p, int head_dim, void* ws, hipStream_t stream);
 hipError_t launch_tree_attn(const TreeAttn& p, bool bf16, int head_dim, void* ws, hipStream_t stream);
@@ -78,6 +87,8 @@ struct VerifyDrafts {
   const int32_t* slots;
   int32_t *move_src, *move_dst;
 };
+constexpr int kVerifyMaxBatch = (1 << 22) - 1;       // blocks of 1024 threads along x
+constexpr int kVerifyMaxVocab = (1 << 28) - 8192;    // pieces of 4096 tokens along y
 size_t verify_drafts_workspace(int batch, int vocab);
 hipError_t launch_verify_drafts(const VerifyDrafts& p, bool bf16, void* ws, hipStream_t stream);
 

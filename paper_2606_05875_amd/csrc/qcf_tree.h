@@ -269,11 +269,12 @@ template <typename T, int D>
 __global__ __launch_bounds__(kMergeWaves * 64) void tree_attn_merge_kernel(TreeAttn p, TreeCut cut, TreeWs ws, int lg) {
   constexpr int LPR = D / 4, RPW = 64 / LPR, U = 8;
   const int l = threadIdx.x & 63, lc = l % LPR, lr = l / LPR;
-  const int64_t item = (int64_t)blockIdx.x * kMergeWaves + uni((int)threadIdx.x >> 6);
+  const int64_t block = (int64_t)blockIdx.y << kGridLog2 | blockIdx.x;
+  const int64_t item = block * kMergeWaves + uni((int)threadIdx.x >> 6);
+  if (item >= (int64_t)p.batch * p.max_q * p.hq) return;
   const int64_t bi = quotient(item, p.hq);
   const int h = (int)(item - bi * p.hq);
   const int b = (int)quotient(bi, p.max_q), i = (int)(bi - (int64_t)b * p.max_q);
-  if (b >= p.batch) return;
   const int g = h >> lg, vec = (i << lg) + (h & ((1 << lg) - 1));
   const int tile = vec >> cut.vt_log2, v = vec - (tile << cut.vt_log2);
   const int2 held = ws.held[((int64_t)b * p.hkv + g) * cut.tiles + tile];
@@ -388,8 +389,7 @@ inline TreeWs tree_ws(const TreeCut& c, int batch, int hkv, int d, void* workspa
 template <typename T, int D>
 inline void launch_tree_merge(const TreeAttn& p, const TreeCut& c, const TreeWs& ws, int lg, hipStream_t stream) {
   const int64_t rows = (int64_t)p.batch * p.max_q * p.hq;
-  tree_attn_merge_kernel<T, D>
-      <<<dim3((unsigned)((rows + kMergeWaves - 1) / kMergeWaves)), kMergeWaves * 64, 0, stream>>>(p, c, ws, lg);
+  tree_attn_merge_kernel<T, D><<<grid_of((rows + kMergeWaves - 1) / kMergeWaves), kMergeWaves * 64, 0, stream>>>(p, c, ws, lg);
 }
 
 }  // namespace

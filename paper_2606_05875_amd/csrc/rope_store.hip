@@ -22,7 +22,8 @@ __global__ __launch_bounds__(kThreads) void rope_store_kernel(RopeStore p) {
   constexpr int VEC = Vec16<T>::N;
   constexpr int UPH = D / (2 * VEC);  // units per head
   __shared__ float2 cs[D / 2];
-  const int64_t r = blockIdx.x;
+  const int64_t r = (int64_t)blockIdx.y << kGridLog2 | blockIdx.x;
+  if (r >= p.n_rows) return;
   const int64_t s = p.src_idx ? (int64_t)p.src_idx[r] : r;
   if (s < 0 || s >= p.n_src_rows) return;
   const int half = p.rotary_dim / 2;
@@ -96,7 +97,7 @@ __global__ __launch_bounds__(kThreads) void rope_store_kernel(RopeStore p) {
 
 template <typename T, int D>
 hipError_t launch_t(const RopeStore& p, bool interleaved, hipStream_t stream) {
-  const dim3 grid((unsigned)p.n_rows);
+  const dim3 grid = grid_of(p.n_rows);
   if (interleaved)
     rope_store_kernel<T, D, true><<<grid, kThreads, 0, stream>>>(p);
   else

@@ -782,7 +782,6 @@ hipError_t launch_bf16(const TreeAttn& p, void* workspace, hipStream_t stream) {
   const TreeCut c = tree_cut(p.batch, p.max_q, p.max_kv, p.hq, p.hkv, true);
   const TreeWs ws = tree_ws(c, p.batch, p.hkv, D, workspace);
   const int64_t blocks = c.blocks ? c.blocks : (int64_t)p.batch * p.hkv * c.tiles;
-  if (blocks > 0x7fffffff) return hipErrorInvalidConfiguration;
   const dim3 grid((unsigned)blocks);
   const bool tiny = p.page_log2 < 4;
 #define QCF_NARROW(NV)                                                                          \
@@ -808,12 +807,16 @@ hipError_t launch_bf16(const TreeAttn& p, void* workspace, hipStream_t stream) {
 
 }  // namespace
 
+bool tree_attn_fits(int batch, int max_q, int max_kv, int hq, int hkv, bool bf16) {
+  const TreeCut c = tree_cut(batch, max_q, max_kv, hq, hkv, bf16);
+  return c.blocks || (int64_t)batch * hkv * c.tiles < (int64_t)1 << kGridLog2;  // (up to 512 threads a block)
+}
+
 size_t tree_attn_workspace(int batch, int max_q, int max_kv, int hq, int hkv, int head_dim, bool bf16) {
   return tree_ws_layout(tree_cut(batch, max_q, max_kv, hq, hkv, bf16, true), batch, hkv, head_dim).total;
 }
 
 hipError_t launch_tree_attn(const TreeAttn& p, bool bf16, int head_dim, void* ws, hipStream_t stream) {
-  if (((int64_t)p.batch * p.max_q * p.hq + kMergeWaves - 1) / kMergeWaves > 0x7fffffff) return hipErrorInvalidConfiguration;
   if (!bf16) return launch_tree_attn_f32(p, head_dim, ws, stream);
   return head_dim == 64 ? launch_bf16<64>(p, ws, stream) : launch_bf16<128>(p, ws, stream);
 }

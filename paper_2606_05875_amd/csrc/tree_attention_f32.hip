@@ -235,7 +235,6 @@ hipError_t launch_t(const TreeAttn& p, void* workspace, hipStream_t stream) {
   const TreeCut c = tree_cut(p.batch, p.max_q, p.max_kv, p.hq, p.hkv, false);
   const TreeWs ws = tree_ws(c, p.batch, p.hkv, D, workspace);
   const int64_t blocks = c.blocks ? c.blocks : (int64_t)p.batch * p.hkv * c.tiles;
-  if (blocks > 0x7fffffff) return hipErrorInvalidConfiguration;
   const dim3 grid((unsigned)blocks);
   if (p.page_log2 < 4) tree_attn_f32_kernel<D, true><<<grid, kW * 64, 0, stream>>>(p, c, ws, lg);
   else tree_attn_f32_kernel<D, false><<<grid, kW * 64, 0, stream>>>(p, c, ws, lg);
