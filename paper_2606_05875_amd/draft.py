@@ -49,10 +49,12 @@ class DraftStep:
     """One pass of up to ``max_rows`` packed new rows, at most ``max_new`` per request.
 
     ``freq``: the model's rotary frequencies (qcf.rope_frequencies), with ``interleaved`` and ``magnitude`` as
-    qcf_rope_store takes them.  Inputs of a pass are given to its stages and are only read by them."""
+    qcf_rope_store takes them.  ``vocab``: entries of the probabilities that verify takes; without it, and for more,
+    the first such verify allocates their workspace.  Inputs of a pass are given to its stages and are only read
+    by them."""
 
     def __init__(self, cache: PagedCache, max_rows, max_new, n_q_heads, freq, interleaved=False, magnitude=1.0,
-                 scale=None):
+                 scale=None, vocab=None):
         self.cache, self.max_rows, self.max_new = cache, int(max_rows), int(max_new)
         self.freq, self.interleaved, self.magnitude = freq, bool(interleaved), float(magnitude)
         d, hkv, dt, dev, B = cache.head_dim, cache.n_kv_heads, cache.dtype, cache.device, cache.batch
@@ -68,9 +70,18 @@ class DraftStep:
         self.ws_attn = torch.empty(max(need, 256), dtype=torch.uint8, device=dev)
         self.n_out, self.path, self.tokens_out = i32(B), i32(B, self.max_new), i32(B, self.max_new)
         self.move_src, self.move_dst = i32(B, self.max_new), i32(B, self.max_new)
-        self.ws_verify = None
+        self.ws_verify, self._outgrown = None, []
+        if vocab is not None:
+            self._room(vocab)
         self.k_move, self.v_move = (torch.zeros((B * self.max_new, hkv, d), dtype=dt, device=dev) for _ in range(2))
         self.tree = False
+
+    def _room(self, vocab):
+        """ws_verify for ``vocab``; one that became too small is kept, for a captured pass may write to it."""
+        need = max(qcf.qcf_verify_drafts_workspace_size(self.cache.batch, vocab), 256)
+        if self.ws_verify is None or self.ws_verify.numel() < need:
+            self._outgrown.append(self.ws_verify)
+            self.ws_verify = torch.empty(need, dtype=torch.uint8, device=self.cache.device)
 
     def plan(self, new_len, parents=None):
         """Pages and slots for ``new_len`` rows of each request: drafted trees (``parents``, see
@@ -112,9 +123,7 @@ class DraftStep:
         ``parents`` as given to plan."""
         if (parents is not None) != self.tree:
             raise qcf.QcfError("verify takes the parents that plan was given")
-        if self.ws_verify is None:
-            need = qcf.qcf_verify_drafts_workspace_size(self.cache.batch, target.shape[1])
-            self.ws_verify = torch.empty(max(need, 256), dtype=torch.uint8, device=self.cache.device)
+        self._room(target.shape[1])
         qcf.qcf_verify_drafts(self.n_out, self.path, self.tokens_out, target, tokens, self.cu, u_accept, u_next,
                               draft=draft, parents=parents, slots=self.slots, move_src=self.move_src,
                               move_dst=self.move_dst, workspace=self.ws_verify)
