@@ -121,13 +121,11 @@ __global__ __launch_bounds__(kNW * 64, 2) void tree_attn_narrow_kernel(TreeAttn 
     bf16x8 qf[NV][ST];
     int64_t row[NV];
     int idx[NV], head[NV];
-    bool valid[NV];
 #pragma unroll
     for (int c = 0; c < NV; ++c) {
       const int v = tile * VT + 16 * c + ln;
       idx[c] = v >> lg;
       head[c] = (g << lg) + (v & ((1 << lg) - 1));
-      valid[c] = idx[c] < rq.rows;
       row[c] = rq.r0 + min(idx[c], rq.rows - 1);
       const uint16_t* q = static_cast<const uint16_t*>(p.q) + (row[c] * p.hq + head[c]) * D + 8 * lk;
 #pragma unroll
