@@ -761,6 +761,8 @@ def qcf_rope_store(k_cache, v_cache, k_new, v_new, slots, positions=None, freq=N
 
 
 def qcf_tree_attn_workspace_size(batch, max_q, max_kv, n_q_heads, n_kv_heads, head_dim, dtype=torch.bfloat16):
+    if dtype not in _DT:
+        raise QcfError(f"unsupported dtype {dtype}")
     return int(lib().qcf_tree_attn_workspace_size(batch, max_q, max_kv, n_q_heads, n_kv_heads, head_dim, _DT[dtype]))
 
 

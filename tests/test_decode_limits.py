@@ -2,6 +2,7 @@
 import os
 
 import pytest
+import torch
 
 from paper_2606_05875_amd import qcf
 
@@ -36,3 +37,10 @@ def test_verification(L):
         return L.qcf_verify_drafts(A, A, A, A, None, vocab, F32, 20, vocab, A, None, batch, A, 8, A, A, A, None, None, A, 0, None)
     assert call(batch=1 << 22) == UNSUPPORTED and call(vocab=(1 << 28) - 8191) == UNSUPPORTED
     assert call(batch=(1 << 22) - 1) == INVALID and call(vocab=(1 << 28) - 8192) == INVALID
+
+
+def test_types_without_kernels():
+    """The binding's own error, not that of a lookup."""
+    for dt in (torch.float16, torch.float64, torch.int32):
+        with pytest.raises(qcf.QcfError):
+            qcf.qcf_tree_attn_workspace_size(1, 1, 100, 8, 2, 64, dt)
