@@ -110,3 +110,12 @@ def test_logits_that_are_not_finite(kv, new, hq, hkv, d, ps, most, dtype):
             assert (o[i] == 0).all() and (e[i] == -math.inf).all(), i
     np.testing.assert_array_equal(o[new[0]:], was[new[0]:])  # the other requests
     np.testing.assert_array_equal(e[new[0]:], wl[new[0]:])
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("kv,new,hq,hkv,d,ps", [([0], [1500], 2, 1, 128, 64), ([300, 0], [700, 1100], 4, 2, 64, 16)])
+def test_prompts(kv, new, hq, hkv, d, ps, dtype):
+    """Many new rows without a mask: every row sees the tokens up to its own."""
+    say("prompts", kv, new, hq, hkv, d, ps, dtype)
+    x = Batch(kv, new, hq, hkv, d, dtype, ps, False, seed=34)
+    x.check(*x.call())
