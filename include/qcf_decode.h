@@ -179,7 +179,7 @@ qcf_status qcf_rope_store(void* k_cache, void* v_cache, int64_t n_slots, int64_t
  *              do not exceed them (other arguments equal).
  * Sums, maxima and partial results are float32; bf16 calls hand the weights
  * exp(x - max) to the matrix units, after they entered the sum, as two bf16 numbers
- * (16 bits) up to max_q * n_q_heads / n_kv_heads = 64, as one beyond.  A row's
+ * (15 bits) up to max_q * n_q_heads / n_kv_heads = 64, as one beyond.  A row's
  * bits do not depend on the other rows' values.
  * Errors: null pointers, softmax_scale not positive and finite, page_size not a
  * power of two (UNSUPPORTED), row strides of 128 MB and more, batch * max_q *

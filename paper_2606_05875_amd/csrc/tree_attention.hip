@@ -6,7 +6,7 @@
 // product's operand as they stand.
 //
 // Weights enter the sum l as float32, and the second product as bf16.  Up to 64 query vectors they are two
-// bf16 numbers, the rounded p and what that rounding left (16 bits), and the output is off by its own rounding
+// bf16 numbers, p cut short and what that left (15 bits), and the output is off by its own rounding
 // alone (1.66e-3 of its norm from 64 bits, 64 decoded rows): a second product per V fragment, which waits for pages
 // hide (203.5 -> 204.7 us; 16 trees of 16 rows 114.0 -> 115.3).  Beyond, where products and exponentials
 // bound it, they are one bf16 number and the output 2.3e-3 off: two cost 16 trees of 8 to 40 rows 133 -> 170 us,
@@ -59,6 +59,13 @@ __device__ __forceinline__ void copy16(const void* from, uint32_t lds) {
 // pass 2^28.  Such a vector's logits are scaled (and rounded) first; each lane's by its own vector's
 // maximum, so that the other vectors' bits do not hang on it.
 __device__ __forceinline__ bool is_big(float m) { return fabsf(finite(m)) > 0x1p28f; }
+
+// A weight p as two bf16 numbers, cut_of (the upper half of its bits) and rest_of, which is off by 2^-8 of less than
+// 2^-7 p.  Both are above zero wherever p is, so that a product with an infinite value that is seen is infinite and
+// never the difference of two, nor 0 times infinity: hence cut, not rounded, 2^-23 p more, and 2^-126 at least
+// (as no weight is between that and 0).
+__device__ __forceinline__ float cut_of(float p) { return __builtin_bit_cast(float, __builtin_bit_cast(uint32_t, p) & 0xffff0000u); }
+__device__ __forceinline__ float rest_of(float p) { return fmaxf(fmaf(p, 0x1.000002p0f, -cut_of(p)), fminf(p, 0x1p-126f)); }
 
 // any of a 16-byte piece's 8 values infinite or NaN
 __device__ __forceinline__ bool not_finite(const uint4& x) {
@@ -234,7 +241,7 @@ __global__ __launch_bounds__(kNW * 64, 2) void tree_attn_narrow_kernel(TreeAttn 
         }
         asm volatile("" ::: "memory");
       }
-      v4s pb[NV], pl[NV];  // weights as bf16, and what that left of them
+      v4s pb[NV], pl[NV];  // weights cut to bf16, and what that left of them
       float pw[NV][4];
 #pragma unroll
       for (int c = 0; c < NV; ++c) {
@@ -258,8 +265,8 @@ __global__ __launch_bounds__(kNW * 64, 2) void tree_attn_narrow_kernel(TreeAttn 
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
           pw[c][r] = __builtin_amdgcn_exp2f(fmaf(s[c][r], sc, -ref));
-          pb[c][r] = (short)f2bf(pw[c][r]);
-          pl[c][r] = (short)f2bf(pw[c][r] - bf2f((uint16_t)pb[c][r]));
+          pb[c][r] = (short)(__builtin_bit_cast(uint32_t, pw[c][r]) >> 16);
+          pl[c][r] = (short)f2bf(rest_of(pw[c][r]));
         }
         ls[c] += (pw[c][0] + pw[c][1]) + (pw[c][2] + pw[c][3]);
       }
@@ -537,7 +544,7 @@ __global__ __launch_bounds__(VG * 64, VG == 2 ? 1 : 2) void tree_attn_wide_kerne
     };
     typedef float f32x2_t __attribute__((ext_vector_type(2)));
     typedef __bf16 bf16x2_t __attribute__((ext_vector_type(2)));
-    // P of the tile (kTwo: what rounding left of it in pl); with kNext S of the next one beside it: one product per fenced group with its K fragment
+    // P of the tile (kTwo: cut, and what that left of it in pl); with kNext S of the next one beside it: one product per fenced group with its K fragment
     // read four groups ahead, a group's arguments, exponentials and sums in three groups in turn
     auto weights = [&](auto next, const uint8_t* kn, f32x16 (&sn)[2], f32x16 (&s)[2], bf16x8 (&pb)[2][2], bf16x8 (&pl)[2][2]) {
       constexpr bool kNext = decltype(next)::value;
@@ -554,11 +561,12 @@ __global__ __launch_bounds__(VG * 64, VG == 2 ? 1 : 2) void tree_attn_wide_kerne
         for (int e = EG * i; e < EG * (i + 1); e += 2) {
           psum += pw[e];
           psum += pw[e + 1];
-          const bf16x2_t pk = __builtin_convertvector((f32x2_t){pw[e], pw[e + 1]}, bf16x2_t);
+          const bf16x2_t pk = kTwo ? (bf16x2_t){(__bf16)cut_of(pw[e]), (__bf16)cut_of(pw[e + 1])}
+                                   : __builtin_convertvector((f32x2_t){pw[e], pw[e + 1]}, bf16x2_t);
           pb[e >> 4][(e >> 3) & 1][e & 7] = pk[0];
           pb[e >> 4][(e >> 3) & 1][(e & 7) + 1] = pk[1];
           if constexpr (kTwo) {
-            const bf16x2_t rest = __builtin_convertvector((f32x2_t){pw[e] - (float)pk[0], pw[e + 1] - (float)pk[1]}, bf16x2_t);
+            const bf16x2_t rest = __builtin_convertvector((f32x2_t){rest_of(pw[e]), rest_of(pw[e + 1])}, bf16x2_t);
             pl[e >> 4][(e >> 3) & 1][e & 7] = rest[0];
             pl[e >> 4][(e >> 3) & 1][(e & 7) + 1] = rest[1];
           }
