@@ -154,7 +154,8 @@ qcf_status qcf_rope_store(void* k_cache, void* v_cache, int64_t n_slots, int64_t
  * over the tokens t < kv_len[b] (all of them) and, of the new rows' own tokens
  * t = kv_len[b] + j (whose keys and values are in their slots already), those
  * whose bit j of row r's mask is set; without a mask those with j <= i (one
- * decoded token, a chain of drafts, a prompt).  Token t sits in the slot that the
+ * decoded token, a chain of drafts, a prompt; a long one costs all its rows times
+ * all its tokens, whatever they see).  Token t sits in the slot that the
  * block table gives it.  A row that sees no token gets zeros (and lse = -inf); one
  * that sees only logits of -infinity, or a NaN, is NaN (lse too).
  * Values a row does not see never reach it, whatever they hold.

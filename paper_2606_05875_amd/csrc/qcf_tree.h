@@ -337,7 +337,10 @@ inline int log2_of(int x) { return __builtin_ctz((unsigned)x); }
 // as 64; only where all keys stay in the caches is that less, one request of 32896 tokens: 52 and 47).
 // Units of 256, which take a CU each, where every CU has 32 steps of KV heads' keys or more and units are cut (160
 // vectors: 16 such requests 152 us against 188 as 128, 6 requests 69 against 79; fewer steps lose: 192 vectors
-// of one request of 32896 tokens 58 against 53, 64 requests of up to 1980 tokens 140 against 130).  float32
+// of one request of 32896 tokens 58 against 53, 64 requests of up to 1980 tokens 140 against 130).  At head size
+// 64, where registers too leave one such block per CU: 160 vectors of 16 requests 100 us against 103, of 64 requests
+// 359 against 444, of 6 requests 45 against 47; requests of 8 to 40 rows, whose units such bounds leave half empty,
+// lose there (95 against 77; at 128 they gain or lose 3%), and the bounds do not tell them apart.  float32
 // blocks hold 16 vectors.
 //
 // Short units are taken whole, one per block: up to 8 steps always (64 decoded rows over up to 500 tokens:

@@ -18,14 +18,21 @@
 //          waves take 16-token tiles in turn, each on its own (two stages of LDS, no barrier in the loop),
 //          v_mfma_f32_16x16x32/16x16x16_bf16; their results are summed through LDS once per unit.
 //          64 decoded rows over 512 to 8192 tokens, 32/8 heads of 128: 204 us with the merge, 5.57 TB/s (a
-//          copy reaches 5.1); one row over 8192 tokens 16.4 us, over 32768 32 us.
+//          copy reaches 5.1); one row over 8192 tokens 16.7 us, over 32768 32 us.
 //  wide    more vectors (trees).  A wave holds 32 of them (v_mfma_f32_32x32x16_bf16) and the 2, 4 or 8
 //          waves of a block share every 64-token tile (a ring of stages, one barrier per tile); the
 //          products of the next tile's S run beside this tile's exponentials.  Bound: HBM and the latency of
 //          pages up to about 128 vectors (16 trees of 8 to 40 rows over 2000 to 12700 tokens, 32/8 heads of
-//          128: 132 to 140 us, 3.7 TB/s; all of 40 rows 148 us), products and exponentials beyond (64 rows of
-//          64/8 heads: 89 to 94 us over 32896 tokens, 0.75 PFLOP/s; 296 us over 131584, 0.93 PFLOP/s, the matrix
-//          units busy 50% of the cycles).
+//          128: 133 to 140 us, 3.7 TB/s; all of 40 rows 140 to 146 us), products and exponentials beyond (64 rows
+//          of 64/8 heads: 88 to 96 us over 32896 tokens, 0.75 PFLOP/s; 292 to 303 us over 131584, 0.93 PFLOP/s, the
+//          matrix units busy 49% of the cycles).
+// Pages of fewer than 16 rows are looked up by every lane, and every tile of such pages, as those of a unit with
+// a page that is not there, goes the way of the last ones, next products behind the exponentials (64 decoded rows 303
+// us against 206, 16 trees of 8 to 40 rows 298 against 140; there, one missing page in every request 194); their
+// kernels for head size 128 also spill 2 to 10 vector registers.
+// Without a mask, too, a unit goes through all of its request's tokens, and tiles of the new rows' own are such
+// last ones: a prompt costs its full rectangle (4096 rows, 64/8 heads of 128, over an empty cache 954 us, 0.29
+// PFLOP/s of what its rows see; 2000 rows over 30000 tokens 2.2 ms, 0.92).
 #include <math.h>
 
 #include <type_traits>
