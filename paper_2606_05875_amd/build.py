@@ -18,7 +18,8 @@ BUILD = os.path.join(PKG, "_build")
 LIB = os.path.join(PKG, "libqcf.so")
 SOURCES = ["api.cpp", "api_decode.cpp", "rerope.hip", "assemble.hip", "gather_scatter.hip", "topk.hip", "probe_scores.hip", "probe_scores_f32.hip",
            "attention.hip", "attention_f32.hip", "attention_keysplit.hip", "attention_w4.hip", "noalloc.hip", "peak.hip",
-           "page_plan.hip", "rope_store.hip", "tree_attention.hip", "tree_attention_f32.hip", "verify.hip"]
+           "page_plan.hip", "rope_store.hip", "tree_attention.hip", "tree_attention_f32.hip", "verify.hip",
+           "api_turns.cpp", "norm_rope.hip", "chunk_attention.hip", "chunk_attention_f32.hip", "shape_logits.hip", "page_share.hip"]
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-Wall", "-Wno-unused-function",
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",

@@ -9,18 +9,6 @@
 #include "qcf_checks.h"
 #include "qcf_decode_launch.h"
 
-namespace {
-
-inline bool optional_index_ok(const void* p) { return !p || index_ok(p, false); }
-
-// log2 of a page size, or -1 where it is not a power of two
-int page_log2(int page_size) {
-  if (page_size <= 0 || (page_size & (page_size - 1)) != 0) return -1;
-  return __builtin_ctz((unsigned)page_size);
-}
-
-}  // namespace
-
 extern "C" {
 
 qcf_status qcf_page_plan(int32_t* block_table, int64_t table_stride, int max_pages, int batch,
@@ -92,35 +80,10 @@ qcf_status qcf_rope_store(void* k_cache, void* v_cache, int64_t n_slots, int64_t
                           int64_t n_rows, const int32_t* slots, const int32_t* positions,
                           const double* freq, int rotary_dim, int interleaved, float magnitude,
                           int n_q_heads, int n_kv_heads, int head_dim, hipStream_t stream) {
-  if (!dtype_ok(dtype)) return QCF_ERR_UNSUPPORTED;
-  qcf_status st = check_heads(n_q_heads, n_kv_heads, head_dim);
+  const qcf_status st = check_rope_store(k_cache, v_cache, n_slots, cache_row_stride, q_out, k_new, v_new, new_row_stride,
+                                         q_new, q_row_stride, n_src_rows, src_idx, dtype, n_rows, slots, positions,
+                                         freq, rotary_dim, magnitude, n_q_heads, n_kv_heads, head_dim);
   if (st != QCF_OK) return st;
-  if (n_rows < 0 || n_rows > INT32_MAX || n_slots < 0 || n_slots > INT32_MAX || n_src_rows < 0 ||
-      n_src_rows > INT32_MAX)
-    return QCF_ERR_INVALID_ARG;
-  if ((k_cache == nullptr) != (v_cache == nullptr)) return QCF_ERR_INVALID_ARG;
-  if (q_out && !q_new) return QCF_ERR_INVALID_ARG;
-  if (rotary_dim < 0 || rotary_dim > head_dim) return QCF_ERR_INVALID_ARG;
-  if (rotary_dim % 16 != 0) return QCF_ERR_UNSUPPORTED;
-  // positions, frequencies and a rotated part go together
-  if (n_rows > 0 && ((positions == nullptr) != (rotary_dim == 0) || (freq == nullptr) != (rotary_dim == 0)))
-    return QCF_ERR_INVALID_ARG;
-  if (!isfinite(magnitude) || (rotary_dim == 0 && magnitude != 1.f)) return QCF_ERR_INVALID_ARG;
-  if (k_cache) {
-    if (!kv_stride_ok(cache_row_stride, n_kv_heads, head_dim, dtype) ||
-        !kv_stride_ok(new_row_stride, n_kv_heads, head_dim, dtype))
-      return QCF_ERR_INVALID_ARG;
-    if (!aligned16(k_cache) || !aligned16(v_cache) || !tensor_ok(k_new, n_rows == 0 || n_src_rows == 0) ||
-        !tensor_ok(v_new, n_rows == 0 || n_src_rows == 0) || !index_ok(slots, n_rows == 0))
-      return QCF_ERR_INVALID_ARG;
-  }
-  if (q_out && (!aligned16(q_out) || !aligned16(q_new) || q_out == q_new ||
-                !kv_stride_ok(q_row_stride, n_q_heads, head_dim, dtype)))
-    return QCF_ERR_INVALID_ARG;
-  if (!optional_index_ok(positions) || !optional_index_ok(src_idx) ||
-      (reinterpret_cast<uintptr_t>(freq) & 7u) != 0)
-    return QCF_ERR_INVALID_ARG;
-  if (k_cache && (k_cache == k_new || v_cache == v_new)) return QCF_ERR_INVALID_ARG;
   if (n_rows == 0 || n_src_rows == 0 || (!k_cache && !q_out)) return QCF_OK;
   const qcf::RopeStore p{k_cache,  v_cache,    n_slots,   cache_row_stride, q_out,     k_new,  v_new,
                          new_row_stride, q_new, q_row_stride, n_src_rows,   src_idx,   n_rows, slots,

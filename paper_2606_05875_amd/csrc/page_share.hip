@@ -1,0 +1,270 @@
+// Requests that continue others, and the pages behind them (qcf_page_fork, qcf_copy_pages, qcf_page_release).
+//
+// Pages have no holders' counts: a page is held by whoever's table names it, and what nobody's names any
+// more is found by marking the pages of the tables before and after a change in two bit sets.  There is
+// nothing to keep in step, and no result hangs on the order of blocks.
+#include "qcf_device.h"
+#include "qcf_turns_launch.h"
+
+namespace qcf {
+namespace {
+
+constexpr int kThreads = 256;
+
+// ---------------------------------------------------------------------------
+// fork: one block per request, which counts the pages that the requests before it take on its own (three
+// dependent loads each, 256 requests at a time)
+// ---------------------------------------------------------------------------
+struct ForkRow {
+  int source;      // -1: the request ends
+  int64_t n;       // tokens
+  int64_t full;    // pages that they fill
+  int part;        // rows of the page that they start
+  int from;        // that page's number at the source where it has to be copied, else -1
+};
+
+__device__ __forceinline__ ForkRow fork_row(const PageFork& p, int b) {
+  ForkRow f;
+  const int s = p.source[b];
+  f.source = s >= 0 && s < p.batch ? s : -1;
+  f.n = f.source < 0 ? 0 : max(p.kv_len[f.source], 0);
+  if (p.keep_len) f.n = min(f.n, (int64_t)max(p.keep_len[b], 0));
+  f.full = f.n >> p.page_log2;
+  f.part = (int)(f.n & ((1ll << p.page_log2) - 1));
+  f.from = -1;
+  if (f.part > 0 && f.full < p.max_pages && !(f.source == b && f.full == max(p.kv_len[b], 0) >> p.page_log2)) {
+    const int page = p.block_table[(int64_t)f.source * p.table_stride + f.full];
+    if (page >= 0 && page < p.n_pages) f.from = page;
+  }
+  return f;
+}
+
+__global__ __launch_bounds__(kThreads) void page_fork_kernel(PageFork p) {
+  __shared__ int taken_l[kThreads / 64];
+  const int tid = threadIdx.x, b = blockIdx.x;
+  const int64_t head = p.free_head ? p.free_head[0] : 0;
+  if (b >= p.batch) {  // (a batch of none)
+    if (tid == 0) p.free_head_out[0] = (int)head;
+    return;
+  }
+  const ForkRow f = fork_row(p, b);
+  int taken = 0;
+  for (int i = tid; i < b; i += kThreads) taken += fork_row(p, i).from >= 0 ? 1 : 0;
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) taken += __shfl_xor(taken, o, 64);
+  if ((tid & 63) == 0) taken_l[tid >> 6] = taken;
+  __syncthreads();
+  taken = 0;
+#pragma unroll
+  for (int i = 0; i < kThreads / 64; ++i) taken += taken_l[i];
+  int page = -1;
+  if (f.from >= 0) {
+    const int64_t at = head + taken;
+    if (at >= 0 && at < p.n_free) page = p.free_pages[at];
+    if (page < 0 || page >= p.n_pages) page = -1;
+  }
+  const int held = (int)min(f.full + (f.part > 0 ? 1 : 0), (int64_t)p.max_pages);
+  int32_t* out = p.table_out + (int64_t)b * p.table_out_stride;
+  const int32_t* in = p.block_table + (int64_t)max(f.source, 0) * p.table_stride;
+  for (int c = tid; c < p.max_pages; c += kThreads) {
+    int x = -1;
+    if (c < held) x = f.from >= 0 && c == f.full ? page : in[c];
+    out[c] = x;
+  }
+  if (tid == 0) {
+    p.kv_out[b] = (int)f.n;
+    p.held_out[b] = held;
+    p.copy_src[b] = page >= 0 ? f.from : -1;
+    p.copy_dst[b] = page;
+    p.copy_rows[b] = page >= 0 ? f.part : 0;
+    if (b == p.batch - 1) p.free_head_out[0] = (int)(head + taken + (f.from >= 0 ? 1 : 0));
+  }
+}
+
+// ---------------------------------------------------------------------------
+// copy: a block moves up to 16 KB of one pair in one pool.  Bound: HBM (or launch, for few rows)
+// ---------------------------------------------------------------------------
+constexpr int kCopyBytes = 16384;
+constexpr int kCopyUnroll = kCopyBytes / 16 / kThreads;
+
+// rows of one block's part
+inline __host__ __device__ int copy_rows_of(int64_t row_bytes) {
+  return row_bytes >= kCopyBytes ? 1 : (int)(kCopyBytes / row_bytes);
+}
+
+__global__ __launch_bounds__(kThreads) void copy_pages_kernel(CopyPages p, int rows_per, int parts) {
+  const int64_t block = (int64_t)blockIdx.y << kGridLog2 | blockIdx.x;
+  // parts of a page, then pools, then pairs
+  const int64_t item = block / parts;
+  const int part = (int)(block - item * parts);
+  const int64_t i = item / p.n_pools;
+  const int pool = (int)(item - i * p.n_pools);
+  if (i >= p.n_pairs) return;
+  const int64_t from = p.src_page[i], to = p.dst_page[i];
+  const int rows = p.rows ? min(p.rows[i], 1 << p.page_log2) : 1 << p.page_log2;
+  if (from < 0 || from >= p.n_pages || to < 0 || to >= p.n_pages || from == to) return;
+  const int r0 = part * rows_per, n = min(rows - r0, rows_per);
+  if (n <= 0) return;
+  char* base = static_cast<char*>(p.pools[pool]);
+  const char* src = base + ((from << p.page_log2) + r0) * p.row_stride;
+  char* dst = base + ((to << p.page_log2) + r0) * p.row_stride;
+  const int per_row = (int)(p.row_bytes >> 4);
+  const int64_t vecs = (int64_t)n * per_row;
+  for (int64_t v0 = threadIdx.x; v0 < vecs; v0 += kThreads * kCopyUnroll) {
+    uint4 x[kCopyUnroll];
+    int64_t at[kCopyUnroll];
+#pragma unroll
+    for (int k = 0; k < kCopyUnroll; ++k) {
+      const int64_t v = min(v0 + k * kThreads, vecs - 1);
+      const int64_t row = n == 1 ? 0 : (int64_t)((uint32_t)v / (uint32_t)per_row);
+      at[k] = row * p.row_stride + (v - row * per_row) * 16;
+      x[k] = ld16(src + at[k]);
+    }
+#pragma unroll
+    for (int k = 0; k < kCopyUnroll; ++k)
+      if (v0 + k * kThreads < vecs) st16(dst + at[k], x[k]);
+  }
+}
+
+// ---------------------------------------------------------------------------
+// release: one block, which marks the pages of both tables in LDS (two bits per page; larger pools in
+// several goes) and writes those that are only in the first.  Bound: latency, and for large tables what one
+// compute unit reads.
+// ---------------------------------------------------------------------------
+constexpr int kRelThreads = 1024;
+constexpr int kRelWords = 1 << 14;  // of 32 pages, per bit set
+
+__global__ __launch_bounds__(kRelThreads) void page_release_kernel(PageRelease p) {
+  __shared__ uint32_t was_l[kRelWords], is_l[kRelWords];
+  __shared__ int32_t first_l[kRelThreads + 1];  // 64-entry pieces before each request of a go
+  __shared__ int wave_l[kRelThreads / 64];
+  const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
+  constexpr int kWaves = kRelThreads / 64;
+  const int64_t head = min(max((int64_t)p.free_head[0], (int64_t)0), p.n_free);
+  constexpr int64_t kPages = (int64_t)kRelWords * 32;
+  const int goes = (int)((p.n_pages + kPages - 1) / kPages);
+
+  // inclusive sum over the block's threads of x; `all` is the total
+  auto scan = [&](int x, int& all) {
+    int sum = x;
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+      const int y = __shfl_up(sum, o, 64);
+      if (lane >= o) sum += y;
+    }
+    __syncthreads();
+    if (lane == 63) wave_l[w] = sum;
+    __syncthreads();
+    all = 0;
+    for (int i = 0; i < kWaves; ++i) {
+      if (i < w) sum += wave_l[i];
+      all += wave_l[i];
+    }
+    return sum;
+  };
+  // marks the pages p0 .. p0 + kPages - 1 of a table
+  auto mark = [&](const int32_t* table, int64_t stride, const int32_t* held, uint32_t* bits, int64_t p0) {
+    for (int b0 = 0; b0 < p.batch; b0 += kRelThreads) {
+      const int mine = b0 + tid < p.batch ? min(max(held[b0 + tid], 0), p.max_pages) : 0;
+      int all;
+      const int pieces = (mine + 63) >> 6;
+      const int sum = scan(pieces, all);
+      first_l[tid] = sum - pieces;
+      if (tid == 0) first_l[kRelThreads] = all;
+      __syncthreads();
+      // a wave takes 64 pieces at a time; each lane looks up one of them
+      for (int i0 = w * 64; i0 < all; i0 += kWaves * 64) {
+        const int mine_i = min(i0 + lane, all - 1);
+        int lo = 0, hi = kRelThreads;
+        while (hi - lo > 1) {
+          const int mid = (lo + hi) >> 1;
+          if (first_l[mid] <= mine_i) lo = mid; else hi = mid;
+        }
+        const int64_t row = (int64_t)(b0 + lo) * stride;
+        const int col = (mine_i - first_l[lo]) * 64;
+        const int n_row = min(max(held[b0 + lo], 0), p.max_pages);
+        const int n = min(64, all - i0);
+        constexpr int U = 8;
+        for (int k0 = 0; k0 < n; k0 += U) {
+          int x[U];
+#pragma unroll
+          for (int k = 0; k < U; ++k) {
+            const int from = min(k0 + k, n - 1);
+            const int64_t r = __shfl(row, from, 64);
+            const int c = __shfl(col, from, 64), end = __shfl(n_row, from, 64);
+            x[k] = table[r + min(c + lane, end - 1)];
+          }
+#pragma unroll
+          for (int k = 0; k < U; ++k) {
+            const int64_t at = (int64_t)x[k] - p0;
+            if (x[k] >= 0 && x[k] < p.n_pages && at >= 0 && at < kPages) atomicOr(&bits[at >> 5], 1u << (at & 31));
+          }
+        }
+      }
+      __syncthreads();
+    }
+  };
+  // marks go g's pages of both tables; own: how many of this thread's are released, before: of the threads' before
+  // it; returns the number of all
+  int words, own, before;
+  auto go = [&](int g) {
+    const int64_t p0 = g * kPages;
+    words = (int)((min(p.n_pages - p0, kPages) + 31) >> 5);
+    __syncthreads();
+    for (int i = tid; i < words; i += kRelThreads) was_l[i] = is_l[i] = 0;
+    __syncthreads();
+    mark(p.before, p.before_stride, p.held_before, was_l, p0);
+    mark(p.after, p.after_stride, p.held_after, is_l, p0);
+    const int per = (words + kRelThreads - 1) / kRelThreads;
+    const int i0 = min(tid * per, words), i1 = min(i0 + per, words);
+    own = 0;
+    for (int i = i0; i < i1; ++i) own += __popc(was_l[i] & ~is_l[i]);
+    int all;
+    before = scan(own, all) - own;
+    return all;
+  };
+  int64_t n = 0;
+  for (int g = 0; g < goes; ++g) n += go(g);
+  int64_t put = head - n;
+  if (tid == 0) p.free_head_out[0] = (int)max(put, (int64_t)0);
+  for (int g = 0; g < goes; ++g) {
+    const int all = goes > 1 ? go(g) : (int)n;  // (a single one's marks are still there)
+    const int per = (words + kRelThreads - 1) / kRelThreads;
+    const int i0 = min(tid * per, words), i1 = min(i0 + per, words);
+    int64_t at = put + before;
+    for (int i = i0; i < i1; ++i)
+      for (uint32_t left = was_l[i] & ~is_l[i]; left; left &= left - 1, ++at)
+        if (at >= 0) p.free_pages[at] = (int)(g * kPages + i * 32 + __builtin_ctz(left));
+    put += all;
+  }
+}
+
+}  // namespace
+
+hipError_t launch_page_fork(const PageFork& p, hipStream_t stream) {
+  page_fork_kernel<<<dim3((unsigned)(p.batch > 0 ? p.batch : 1)), kThreads, 0, stream>>>(p);
+  return hipGetLastError();
+}
+
+static int64_t copy_parts(const CopyPages& p) {
+  const int64_t rows = copy_rows_of(p.row_bytes);
+  return ((1ll << p.page_log2) + rows - 1) / rows;
+}
+
+int64_t copy_pages_blocks(const CopyPages& p) {
+  const int64_t most = INT32_MAX, parts = copy_parts(p);
+  if (p.n_pairs > most / p.n_pools || p.n_pairs * p.n_pools > most / parts) return -1;
+  return p.n_pairs * p.n_pools * parts;
+}
+
+hipError_t launch_copy_pages(const CopyPages& p, hipStream_t stream) {
+  copy_pages_kernel<<<grid_of(copy_pages_blocks(p)), kThreads, 0, stream>>>(p, copy_rows_of(p.row_bytes), (int)copy_parts(p));
+  return hipGetLastError();
+}
+
+hipError_t launch_page_release(const PageRelease& p, hipStream_t stream) {
+  page_release_kernel<<<dim3(1), kRelThreads, 0, stream>>>(p);
+  return hipGetLastError();
+}
+
+}  // namespace qcf

@@ -1,0 +1,271 @@
+// Device code shared by the kernels of qcf_chunk_attn: which tokens a tile of rows sees, and how the work is
+// cut over blocks.
+//
+// A unit is a tile of query vectors (rows times the heads that share a KV head) of one request and KV
+// head; its work is one step per 64 tokens between the first that its first row sees and the last one's own.
+// Tiles hold a power of two of rows, so the steps of a request's first tiles have a closed form, and
+// every block finds its share of all steps by itself.  The steps of all units, laid end to end (request, KV
+// head, tile), are shared evenly over a fixed number of blocks; a unit that is cut between blocks is
+// merged from float32 partial results.  Beginning and ending a unit counts as `start` steps in the
+// shares.  A block has at most two partial results: of a unit that others began (slot 2 x) and of one
+// that it begins (slot 2 x + 1), which it enters in a list for the merge.
+#pragma once
+#include "qcf_tree.h"
+#include "qcf_turns_launch.h"
+
+namespace qcf {
+
+constexpr int kChunkStep = 64;  // tokens per step
+
+struct ChunkCut {
+  int vt_log2;  // query vectors per unit
+  int blocks;   // blocks that share the steps, 0: one block per unit
+  int start;    // what beginning a unit counts as, in steps
+  int tiles;    // units of the longest request per KV head
+};
+
+struct ChunkWs {
+  int4* cut;   // [blocks] the unit (request, KV head, tile) that a block begins and others end, the last of them; or -1
+  float2* ml;  // [2 * blocks][vt] running maximum (log2 units) and sum
+  float* o;    // [2 * blocks][vt][d]
+};
+
+// Work of one request per KV head.  Lengths beyond the caller's bound (whose tokens are not seen) count as that.
+struct ChunkCost {
+  int64_t kv, rows;
+  int tiles, rl;  // rows per tile, as a power of two
+  int window, start;
+
+  __device__ __forceinline__ ChunkCost(const ChunkAttn& p, const TreeRequest& q, int lg, const ChunkCut& cut) {
+    kv = min(q.kv, p.max_kv);
+    rows = q.rows;
+    rl = cut.vt_log2 - lg;
+    tiles = (int)((rows + (1 << rl) - 1) >> rl);
+    window = p.window;
+    start = cut.start;
+  }
+  // sum over i < n of floor((a + i * 2^rl) / 64), a >= 0
+  __device__ __forceinline__ int64_t floors(int64_t a, int64_t n) const {
+    if (rl >= 6) return n * (a >> 6) + ((n * (n - 1) / 2) << (rl - 6));
+    const int ml = 6 - rl;
+    const auto below = [&](int64_t x) {  // sum over i < x of floor(i / 2^ml)
+      const int64_t q = x >> ml, r = x & ((1 << ml) - 1);
+      return ((q * (q - 1) / 2) << ml) + q * r;
+    };
+    return below((a >> rl) + n) - below(a >> rl);
+  }
+  // the first step of a tile, and the one behind its last
+  __device__ __forceinline__ int64_t first(int tile) const {
+    return window ? max(kv + ((int64_t)tile << rl) - window + 1, (int64_t)0) >> 6 : 0;
+  }
+  __device__ __forceinline__ int64_t last(int tile) const {
+    return (kv + min((int64_t)(tile + 1) << rl, rows) + 63) >> 6;
+  }
+  // steps of the first n <= tiles tiles, with their starts
+  __device__ __forceinline__ int64_t before(int n) const {
+    if (n == 0) return 0;
+    int64_t s = floors(kv + (1 << rl) + 63, min(n, tiles - 1)) + (int64_t)start * n;
+    if (n == tiles) s += last(tiles - 1);
+    if (window) {
+      const int64_t a = kv - window + 1;
+      const int64_t i0 = a >= 0 ? 0 : min((int64_t)n, ((1 << rl) - 1 - a) >> rl);
+      s -= floors(a + (i0 << rl), n - i0);
+    }
+    return s;
+  }
+};
+
+// Runs `unit(b, request, g, tile, first, n, slot)` for this block's share: steps first .. first+n-1 (of 64
+// tokens, counted from token 0) of a unit, to be written out whole (slot < 0) or as a partial result.  NT threads.
+template <int NT, typename F>
+__device__ __forceinline__ void chunk_walk(const ChunkAttn& p, const ChunkCut& cut, const ChunkWs& ws, int lg,
+                                           F&& unit) {
+  if (cut.blocks == 0) {
+    const int g = blockIdx.x % p.hkv, rest = blockIdx.x / p.hkv;
+    // the longest tiles first
+    const int tile = cut.tiles - 1 - rest % cut.tiles, b = rest / cut.tiles;
+    const TreeRequest q = tree_request_uni(p, b);
+    const ChunkCost c(p, q, lg, cut);
+    if (tile >= c.tiles) return;
+    const int s0 = (int)c.first(tile);
+    unit(b, q, g, tile, uni(s0), uni((int)c.last(tile) - s0), -1);
+    return;
+  }
+  __shared__ int64_t sum_l[NT + 1];  // steps before each thread's requests
+  __shared__ int64_t wave_l[NT / 64];
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int per = (p.batch + NT - 1) / NT;
+  int64_t own = 0;
+  for (int i = tid * per; i < min((tid + 1) * per, p.batch); ++i) {
+    const ChunkCost c(p, tree_request(p, i), lg, cut);
+    own += p.hkv * c.before(c.tiles);
+  }
+  int64_t sum = own;
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) {
+    const int64_t y = __shfl_up(sum, o, 64);
+    if (lane >= o) sum += y;
+  }
+  if (lane == 63) wave_l[tid >> 6] = sum;
+  __syncthreads();
+  for (int i = 0; i < tid >> 6; ++i) sum += wave_l[i];
+  sum_l[tid] = sum - own;
+  if (tid == NT - 1) sum_l[NT] = sum;
+  __syncthreads();
+  const TreeShares shares(uni(sum_l[NT]), cut.blocks);
+  const bool works = (int)blockIdx.x < shares.blocks && shares.all > 0;
+  const int x = works ? shares.block(blockIdx.x) : (int)blockIdx.x;
+  if (tid == 0) ws.cut[x] = make_int4(-1, 0, 0, 0);
+  if (!works) return;
+  int64_t s = shares.first(x);
+  const int64_t share1 = shares.first(x + 1);
+  // the last thread whose requests start at or before s: each lane looks at one of a wave's
+  int lo = 0;
+#pragma unroll
+  for (int i = 0; i < NT; i += 64) lo += __builtin_popcountll(__ballot(sum_l[i + lane] <= s));
+  lo = max(lo - 1, 0);
+  int b = lo * per;
+  int64_t before = uni(sum_l[lo]);
+  while (s < share1) {  // (ends: the requests' costs sum to more than s)
+    const TreeRequest q = tree_request_uni(p, b);
+    const ChunkCost c(p, q, lg, cut);
+    const int64_t head = c.before(c.tiles), all = p.hkv * head;
+    if (before + all <= s) {
+      before += all;
+      ++b;
+      continue;
+    }
+    int g = (int)((s - before) / head);
+    int64_t h0 = before + g * head;  // where the KV head begins
+    int tile = 0;
+    for (int n = c.tiles; n > 1;) {  // the last tile that begins at or before s
+      const int half = n >> 1;
+      if (h0 + c.before(tile + half) <= s) tile += half, n -= half;
+      else n = half;
+    }
+    while (s < share1 && g < p.hkv) {
+      const int64_t u0 = h0 + c.before(tile), u1 = h0 + c.before(tile + 1);
+      const int64_t to = min(u1, share1);
+      const int steps = (int)(u1 - u0) - c.start;
+      const int first = (int)max(s - u0 - c.start, (int64_t)0), n = (int)(to - u0) - c.start - first;
+      if (n > 0) {
+        if (first == 0 && n < steps && tid == 0) ws.cut[x] = make_int4(b, g, tile, shares.holder(u1 - 1));
+        unit(uni(b), q, uni(g), uni(tile), uni((int)c.first(tile) + first), uni(n),
+             n == steps ? -1 : uni(2 * x + (first > 0 ? 0 : 1)));
+      }
+      s = to;
+      if (s == u1 && ++tile == c.tiles) {
+        tile = 0;
+        h0 += head;
+        ++g;
+      }
+    }
+  }
+}
+
+namespace {
+
+// The partial results of the units that are cut, in the blocks' order: one wave per query vector of the unit that
+// a block begins.  Lane j first takes the maximum and sum of partial j, then 64 / (D / 4) partials at a time are
+// read and summed, whose sums meet at the end.  Bound: the partials' bytes.
+constexpr int kChunkMergeWaves = 4;
+template <typename T, int D>
+__global__ __launch_bounds__(kChunkMergeWaves * 64) void chunk_merge_kernel(ChunkAttn p, ChunkCut cut, ChunkWs ws, int lg) {
+  constexpr int LPR = D / 4, RPW = 64 / LPR, U = 8;
+  const int l = threadIdx.x & 63, lc = l % LPR, lr = l / LPR;
+  const int x0 = blockIdx.x;
+  const int4 c = ws.cut[x0];
+  const int b = uni(c.x), g = uni(c.y), tile = uni(c.z), x1 = uni(c.w);
+  if (b < 0) return;
+  const TreeRequest q = tree_request_uni(p, b);
+  const int v = blockIdx.y * kChunkMergeWaves + uni((int)threadIdx.x >> 6);
+  const int64_t vec = ((int64_t)tile << cut.vt_log2) + v;
+  const int i = (int)(vec >> lg), h = (g << lg) + (int)(vec & ((1 << lg) - 1));
+  if (i >= q.rows) return;
+  auto slot = [&](int x) { return ((int64_t)(2 * x + (x == x0 ? 1 : 0)) << cut.vt_log2) + v; };
+  const float4* part = reinterpret_cast<const float4*>(ws.o);
+  float mx = -INFINITY, lt = 0.f;
+  float4 a = make_float4(0.f, 0.f, 0.f, 0.f);
+  for (int xb = x0; xb <= x1; xb += 64) {
+    const int n = min(64, x1 - xb + 1);
+    const float2 ml = ws.ml[slot(min(xb + l, x1))];
+    const float m1 = l < n ? ml.x : -INFINITY, l1 = l < n ? ml.y : 0.f;
+    const float mn = fmaxf(mx, wave_max(m1));
+    const float f = __builtin_amdgcn_exp2f(gap(m1, mn)), fa = __builtin_amdgcn_exp2f(gap(mx, mn));
+    lt = lt * fa + wave_sum(l1 * f);
+    mx = mn;
+    a.x *= fa;
+    a.y *= fa;
+    a.z *= fa;
+    a.w *= fa;
+    for (int j0 = 0; j0 < n; j0 += U * RPW) {
+      float4 o[U];
+#pragma unroll
+      for (int k = 0; k < U; ++k) o[k] = part[slot(xb + min(j0 + k * RPW + lr, n - 1)) * LPR + lc];
+#pragma unroll
+      for (int k = 0; k < U; ++k) {
+        const int j = j0 + k * RPW + lr;
+        const float fo = __shfl(f, min(j, 63), 64);
+        if (j >= n) continue;
+        a.x = fmaf(o[k].x, fo, a.x);
+        a.y = fmaf(o[k].y, fo, a.y);
+        a.z = fmaf(o[k].z, fo, a.z);
+        a.w = fmaf(o[k].w, fo, a.w);
+      }
+    }
+  }
+#pragma unroll
+  for (int m = LPR; m < 64; m <<= 1) {
+    a.x += __shfl_xor(a.x, m, 64);
+    a.y += __shfl_xor(a.y, m, 64);
+    a.z += __shfl_xor(a.z, m, 64);
+    a.w += __shfl_xor(a.w, m, 64);
+  }
+  const float inv = row_scale(mx, lt);
+  const int64_t at = (q.r0 + i) * p.hq + h;
+  if (lr == 0)
+    store4(static_cast<T*>(p.out) + at * D + 4 * lc, make_float4(a.x * inv, a.y * inv, a.z * inv, a.w * inv));
+  if (p.lse && l == 0) p.lse[at] = row_lse(mx, lt);
+}
+
+// How a call is cut, from its bounds (lengths are on the device): tiles of 128 vectors (float32: 32), as many
+// blocks as run at once, two per CU, with 4 steps each at least.
+constexpr int kChunkBlocks = 512;
+inline ChunkCut chunk_cut(int batch, int max_q, int max_kv, int hq, int hkv, bool bf16) {
+  const int64_t vectors = (int64_t)max_q * (hq / hkv);
+  ChunkCut c;
+  c.vt_log2 = bf16 ? 7 : 5;
+  c.tiles = (int)((vectors + (1 << c.vt_log2) - 1) >> c.vt_log2);
+  c.start = 4;
+  c.blocks = kChunkBlocks;
+  return c;
+}
+
+struct ChunkWsLayout {
+  size_t ml, o, total;
+};
+inline ChunkWsLayout chunk_ws_layout(const ChunkCut& c, int d) {
+  const auto up = [](size_t x) { return (x + 255) / 256 * 256; };
+  ChunkWsLayout w{};
+  if (c.blocks == 0) return w;
+  w.ml = up((size_t)c.blocks * sizeof(int4));
+  w.o = w.ml + up(((size_t)2 * c.blocks << c.vt_log2) * 8);
+  w.total = w.o + up(((size_t)2 * c.blocks << c.vt_log2) * d * 4);
+  return w;
+}
+
+inline ChunkWs chunk_ws(const ChunkCut& c, int d, void* workspace) {
+  const ChunkWsLayout w = chunk_ws_layout(c, d);
+  char* base = static_cast<char*>(workspace);
+  return ChunkWs{reinterpret_cast<int4*>(base), reinterpret_cast<float2*>(base + w.ml),
+                 reinterpret_cast<float*>(base + w.o)};
+}
+
+template <typename T, int D>
+inline void launch_chunk_merge(const ChunkAttn& p, const ChunkCut& c, const ChunkWs& ws, int lg, hipStream_t stream) {
+  chunk_merge_kernel<T, D><<<dim3((unsigned)c.blocks, (1u << c.vt_log2) / kChunkMergeWaves), kChunkMergeWaves * 64, 0, stream>>>(p, c, ws, lg);
+}
+
+}  // namespace
+
+}  // namespace qcf

@@ -37,35 +37,10 @@
 
 #include <type_traits>
 
-#include "qcf_attn.h"
-#include "qcf_tree.h"
+#include "qcf_paged.h"
 
 namespace qcf {
 namespace {
-
-typedef short v4s __attribute__((ext_vector_type(4)));
-typedef v4s __attribute__((address_space(3))) * lds_v4s;
-
-// 16 bytes per lane from base + off into LDS at byte address lds + 16 * lane, past the registers and
-// without a wait of the compiler's (the caller counts).  A load that takes its LDS address from m0 needs a wait
-// state behind the write of m0, which the compiler does not add inside an asm block.
-__device__ __forceinline__ void copy16(const void* base, uint32_t off, uint32_t lds) {
-  const uint32_t la = __builtin_amdgcn_readfirstlane(lds);
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2"
-               :
-               : "s"(la), "v"(off), "s"(uni((int64_t)base))
-               : "memory");
-}
-__device__ __forceinline__ void copy16(const void* from, uint32_t lds) {
-  const uint32_t la = __builtin_amdgcn_readfirstlane(lds);
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" : : "s"(la), "v"(from) : "memory");
-}
-
-// Weights are exp2(s * scale2 - ref) with a fused multiply-add, which keeps the product exact; its
-// difference to the rounded maximum reaches 2^-24 of that, too much to be an exponent where maxima
-// pass 2^28.  Such a vector's logits are scaled (and rounded) first; each lane's by its own vector's
-// maximum, so that the other vectors' bits do not hang on it.
-__device__ __forceinline__ bool is_big(float m) { return fabsf(finite(m)) > 0x1p28f; }
 
 // A weight p as two bf16 numbers, cut_of (the upper half of its bits) and rest_of, which is off by 2^-8 of less than
 // 2^-7 p.  Both are above zero wherever p is, so that a product with an infinite value that is seen is infinite and
@@ -73,16 +48,6 @@ __device__ __forceinline__ bool is_big(float m) { return fabsf(finite(m)) > 0x1p
 // (as no weight is between that and 0).
 __device__ __forceinline__ float cut_of(float p) { return __builtin_bit_cast(float, __builtin_bit_cast(uint32_t, p) & 0xffff0000u); }
 __device__ __forceinline__ float rest_of(float p) { return fmaxf(fmaf(p, 0x1.000002p0f, -cut_of(p)), fminf(p, 0x1p-126f)); }
-
-// any of a 16-byte piece's 8 values infinite or NaN
-__device__ __forceinline__ bool not_finite(const uint4& x) {
-  const uint32_t w[4] = {x.x, x.y, x.z, x.w};
-  bool bad = false;
-#pragma unroll
-  for (int i = 0; i < 4; ++i)
-    bad = bad || (w[i] & 0x7f80u) == 0x7f80u || (w[i] & 0x7f800000u) == 0x7f800000u;
-  return bad;
-}
 
 // ---------------------------------------------------------------------------
 // narrow

@@ -9,6 +9,7 @@ no fallback.
 from __future__ import annotations
 
 import ctypes
+import math
 import os
 import threading
 
@@ -24,6 +25,8 @@ __all__ = [
     "qcf_mfma_loop",
     "qcf_page_plan", "qcf_rope_frequencies", "rope_frequencies", "qcf_rope_store", "qcf_tree_attn_workspace_size",
     "qcf_tree_attn", "qcf_verify_drafts_workspace_size", "qcf_verify_drafts",
+    "qcf_norm_rope_store", "qcf_chunk_attn_workspace_size", "qcf_chunk_attn", "qcf_shape_logits_workspace_size",
+    "qcf_shape_logits", "qcf_page_fork", "PoolSet", "qcf_copy_pages", "qcf_page_release",
     "EXPORTS", "Prepared", "prepare",
 ]
 
@@ -38,7 +41,7 @@ _SZ = ctypes.c_size_t
 _D = ctypes.c_double
 _F = ctypes.c_float
 
-# name -> (restype, argtypes); mirrors include/qcf.h and include/qcf_decode.h
+# name -> (restype, argtypes); mirrors include/qcf.h, include/qcf_decode.h and include/qcf_turns.h
 EXPORTS = {
     "qcf_version": (_I, []),
     "qcf_status_string": (ctypes.c_char_p, [_I]),
@@ -82,6 +85,17 @@ EXPORTS = {
     "qcf_verify_drafts_workspace_size": (_SZ, [_I, _I]),
     "qcf_verify_drafts": (_I, [_P, _P, _P, _P, _P, _I64, _I, _I64, _I, _P, _P, _I, _P, _I, _P, _P, _P, _P, _P,
                                _P, _SZ, _P]),
+    "qcf_norm_rope_store": (_I, [_P, _P, _I64, _I64, _P, _P, _P, _I64, _P, _I64, _I64, _P, _I, _I64, _P, _P, _P, _I,
+                                 _I, _F, _P, _I64, _P, _I64, _F, _I, _I, _I, _P]),
+    "qcf_chunk_attn_workspace_size": (_SZ, [_I, _I, _I, _I, _I, _I, _I]),
+    "qcf_chunk_attn": (_I, [_P, _P, _P, _I64, _P, _P, _P, _I64, _I64, _P, _I64, _I, _I, _P, _I, _I, _I, _I, _I,
+                            _I, _I, _I, _F, _P, _SZ, _P]),
+    "qcf_shape_logits_workspace_size": (_SZ, [_I64, _I]),
+    "qcf_shape_logits": (_I, [_P, _I64, _I, _P, _I64, _I, _I64, _I, _I, _P, _P, _I64, _I, _P, _P, _P, _P, _I, _P, _P,
+                              _P, _P, _P, _P, _I64, _P, _I64, _P, _I, _P, _SZ, _P]),
+    "qcf_page_fork": (_I, [_P, _I64, _P, _P, _P, _I64, _I, _I, _P, _P, _P, _P, _I64, _P, _I64, _I, _P, _P, _P, _P, _P]),
+    "qcf_copy_pages": (_I, [_P, _I, _I64, _I64, _I64, _I, _P, _P, _P, _I64, _P]),
+    "qcf_page_release": (_I, [_P, _I64, _P, _P, _I64, _P, _I, _I, _P, _I64, _P, _P, _I64, _P]),
 }
 
 
@@ -706,14 +720,11 @@ def rope_frequencies(rotary_dim, rope_theta, device="cuda", **scaling):
     return freq.to(device)
 
 
-def qcf_rope_store(k_cache, v_cache, k_new, v_new, slots, positions=None, freq=None, interleaved=False,
-                   magnitude=1.0, q_new=None, q_out=None, src_idx=None):
-    """New rows' keys (turned) and values into cache slots, queries turned into q_out; the rotated
-    part of a head is 2 * len(freq) wide.  Without positions nothing is turned; k_cache, v_cache,
-    k_new, v_new and slots may be None together (queries only)."""
+def _rope_rows(call, k_cache, v_cache, k_new, v_new, slots, positions, freq, q_new, q_out, src_idx):
+    """Checks of the tensors that qcf_rope_store and qcf_norm_rope_store share; the C arguments made of their sizes."""
     some = k_cache if k_cache is not None else q_new
     if some is None:
-        raise QcfError("qcf_rope_store needs keys and values or queries")
+        raise QcfError(f"{call} needs keys and values or queries")
     dt = some.dtype
     for name, t in (("k_cache", k_cache), ("v_cache", v_cache), ("k_new", k_new), ("v_new", v_new),
                     ("q_new", q_new), ("q_out", q_out)):
@@ -752,12 +763,22 @@ def qcf_rope_store(k_cache, v_cache, k_new, v_new, slots, positions=None, freq=N
         if (q_new.dim() != 3 or q_new.shape[2] != d or q_new.shape[0] != src.shape[0] or q_out.shape != (n, hq, d)
                 or not q_out.is_contiguous()):
             raise QcfError("q_new must be [n_src_rows, H_q, d] and q_out dense [n_rows, H_q, d]")
+    return dict(some=some, n=n, n_slots=n_slots, c_stride=c_stride, n_stride=n_stride, q_stride=q_stride,
+                n_src=src.shape[0], rotary=0 if freq is None else 2 * freq.numel(), hq=hq, hkv=hkv, d=d)
+
+
+def qcf_rope_store(k_cache, v_cache, k_new, v_new, slots, positions=None, freq=None, interleaved=False,
+                   magnitude=1.0, q_new=None, q_out=None, src_idx=None):
+    """New rows' keys (turned) and values into cache slots, queries turned into q_out; the rotated
+    part of a head is 2 * len(freq) wide.  Without positions nothing is turned; k_cache, v_cache,
+    k_new, v_new and slots may be None together (queries only)."""
+    s = _rope_rows("qcf_rope_store", k_cache, v_cache, k_new, v_new, slots, positions, freq, q_new, q_out, src_idx)
     _here("qcf_rope_store", k_cache=k_cache, v_cache=v_cache, k_new=k_new, v_new=v_new, slots=slots,
           positions=positions, freq=freq, q_new=q_new, q_out=q_out, src_idx=src_idx)
-    _invoke("qcf_rope_store", _ptr(k_cache), _ptr(v_cache), n_slots, c_stride, _ptr(q_out), _ptr(k_new), _ptr(v_new),
-            n_stride, _ptr(q_new), q_stride, src.shape[0], _ptr(src_idx), _dtype(some), n, _ptr(slots),
-            _ptr(positions), _ptr(freq), 0 if freq is None else 2 * freq.numel(), int(bool(interleaved)),
-            float(magnitude), hq, hkv, d)
+    _invoke("qcf_rope_store", _ptr(k_cache), _ptr(v_cache), s["n_slots"], s["c_stride"], _ptr(q_out), _ptr(k_new),
+            _ptr(v_new), s["n_stride"], _ptr(q_new), s["q_stride"], s["n_src"], _ptr(src_idx), _dtype(s["some"]),
+            s["n"], _ptr(slots), _ptr(positions), _ptr(freq), s["rotary"], int(bool(interleaved)), float(magnitude),
+            s["hq"], s["hkv"], s["d"])
 
 
 def qcf_tree_attn_workspace_size(batch, max_q, max_kv, n_q_heads, n_kv_heads, head_dim, dtype=torch.bfloat16):
@@ -843,3 +864,208 @@ def qcf_verify_drafts(n_out, path, out_tokens, target, tokens, cu_rows, u_accept
             _dtype(target), n, vocab, _ptr(tokens), _ptr(parents), batch, _ptr(cu_rows), path.shape[1],
             _ptr(u_accept), _ptr(u_next), _ptr(slots), _ptr(move_src), _ptr(move_dst), _ptr(workspace),
             workspace.numel(), keep=workspace)
+
+
+# -- further turns on the paged caches (include/qcf_turns.h) ---------------------
+def _head_weight(w, name, heads, d, dtype):
+    """A weight [d] of all heads or [heads, d] of each: its heads' distance."""
+    if w is None:
+        return 0
+    _dev(w, name, dtype)
+    if w.shape[-1] != d or w.shape[:-1] not in ((), (heads,)) or w.stride(-1) != 1:
+        raise QcfError(f"{name} must be [head_dim] or [heads, head_dim] with dense rows")
+    return 0 if w.dim() == 1 else max(w.stride(0), d) if heads == 1 else w.stride(0)
+
+
+def qcf_norm_rope_store(k_cache, v_cache, k_new, v_new, slots, positions=None, freq=None, interleaved=False,
+                        magnitude=1.0, q_new=None, q_out=None, src_idx=None, q_weight=None, k_weight=None, eps=1e-6):
+    """qcf_rope_store with queries and keys normed per head first: x / sqrt(mean(x^2) + eps) times the weight
+    ([head_dim] for all heads or [heads, head_dim]; None: ones)."""
+    s = _rope_rows("qcf_norm_rope_store", k_cache, v_cache, k_new, v_new, slots, positions, freq, q_new, q_out, src_idx)
+    if (q_weight is not None and q_new is None) or (k_weight is not None and k_cache is None):
+        raise QcfError("q_weight goes with q_new, k_weight with k_cache")
+    qs = _head_weight(q_weight, "q_weight", s["hq"], s["d"], s["some"].dtype)
+    ks = _head_weight(k_weight, "k_weight", s["hkv"], s["d"], s["some"].dtype)
+    _here("qcf_norm_rope_store", k_cache=k_cache, v_cache=v_cache, k_new=k_new, v_new=v_new, slots=slots,
+          positions=positions, freq=freq, q_new=q_new, q_out=q_out, src_idx=src_idx, q_weight=q_weight, k_weight=k_weight)
+    _invoke("qcf_norm_rope_store", _ptr(k_cache), _ptr(v_cache), s["n_slots"], s["c_stride"], _ptr(q_out), _ptr(k_new),
+            _ptr(v_new), s["n_stride"], _ptr(q_new), s["q_stride"], s["n_src"], _ptr(src_idx), _dtype(s["some"]),
+            s["n"], _ptr(slots), _ptr(positions), _ptr(freq), s["rotary"], int(bool(interleaved)), float(magnitude),
+            _ptr(q_weight), qs, _ptr(k_weight), ks, float(eps), s["hq"], s["hkv"], s["d"])
+
+
+def qcf_chunk_attn_workspace_size(batch, max_q, max_kv, n_q_heads, n_kv_heads, head_dim, dtype=torch.bfloat16):
+    if dtype not in _DT:
+        raise QcfError(f"unsupported dtype {dtype}")
+    return int(lib().qcf_chunk_attn_workspace_size(batch, max_q, max_kv, n_q_heads, n_kv_heads, head_dim, _DT[dtype]))
+
+
+def qcf_chunk_attn(out, q, cu_q, k_cache, v_cache, block_table, kv_len, page_size, max_q, max_kv, softmax_scale,
+                   window=0, lse=None, workspace=None):
+    """Attention of a chunk of new rows of each request over its pages: every row up to its own token, with a
+    window only the last ``window`` of them."""
+    for name, t in (("out", out), ("k_cache", k_cache), ("v_cache", v_cache)):
+        _dev(t, name, q.dtype)
+    _dev(q, "q")
+    _dev(lse, "lse", torch.float32)
+    stride = _table(block_table)
+    batch = kv_len.numel()
+    _one_or_none(kv_len, "kv_len", batch)
+    _one_or_none(cu_q, "cu_q", batch + 1)
+    if q.dim() != 3 or k_cache.dim() != 3 or not (q.is_contiguous() and out.is_contiguous()) or out.shape != q.shape:
+        raise QcfError("q and out must be dense [rows, H_q, d] tensors of the same shape")
+    n, hq, d = q.shape
+    n_slots, hkv, d2 = k_cache.shape
+    rs = _row_stride(k_cache, "k_cache", hkv * d)
+    if v_cache.shape != k_cache.shape or _row_stride(v_cache, "v_cache", hkv * d) != rs or d2 != d:
+        raise QcfError("k_cache and v_cache must match each other and q's head_dim")
+    if block_table.shape[0] != batch:
+        raise QcfError("block_table needs a row per request")
+    if lse is not None and (lse.shape != (n, hq) or not lse.is_contiguous()):
+        raise QcfError("lse must be dense [n_rows, H_q]")
+    _here("qcf_chunk_attn", out=out, q=q, cu_q=cu_q, k_cache=k_cache, v_cache=v_cache, block_table=block_table,
+          kv_len=kv_len, lse=lse, workspace=workspace)
+    need = qcf_chunk_attn_workspace_size(batch, max_q, max_kv, hq, hkv, d, q.dtype)
+    if workspace is None and need > 0:
+        workspace = torch.empty(need, dtype=torch.uint8, device=q.device)
+    _invoke("qcf_chunk_attn", _ptr(out), _ptr(lse), _ptr(q), n, _ptr(cu_q), _ptr(k_cache), _ptr(v_cache), n_slots, rs,
+            _ptr(block_table), stride, block_table.shape[1], int(page_size), _ptr(kv_len), int(window), _dtype(q), batch,
+            int(max_q), int(max_kv), hq, hkv, d, float(softmax_scale), _ptr(workspace),
+            0 if workspace is None else workspace.numel(), keep=workspace)
+
+
+def qcf_shape_logits_workspace_size(n_rows, vocab):
+    return int(lib().qcf_shape_logits_workspace_size(int(n_rows), int(vocab)))
+
+
+def qcf_shape_logits(out, logits, cu_rows, history=None, prompt_len=None, hist_len=None, tokens=None, tree_mask=None,
+                     repetition=None, presence=None, frequency=None, bias_start=None, bias_token=None, bias_value=None,
+                     allowed=None, temperature=None, probabilities=True, workspace=None):
+    """Logits [rows, vocab] with penalties for the tokens said (``history`` [batch, width], of which hist_len, and the
+    pass's ``tokens`` that a row follows), biases and a mask of allowed tokens (int32 [rows, words] of bits), as
+    probabilities at each request's temperature or as logits."""
+    _dev(logits, "logits")
+    _dev(out, "out")
+    if logits.dim() != 2 or out.shape != logits.shape:
+        raise QcfError("logits and out must be [rows, vocab]")
+    n, vocab = logits.shape
+    batch = cu_rows.numel() - 1
+    if batch < 0:
+        raise QcfError("cu_rows needs batch + 1 entries")
+    ls, os_ = _row_stride(logits, "logits", vocab), _row_stride(out, "out", vocab)
+    _dev(history, "history", torch.int32)
+    if history is not None and (history.dim() != 2 or history.shape[0] != batch or (history.numel() and history.stride(1) != 1)):
+        raise QcfError("history must be [batch, width] with dense rows")
+    hs = 0 if history is None else max(history.stride(0), history.shape[1]) if batch <= 1 else history.stride(0)
+    for name, t, size in (("cu_rows", cu_rows, batch + 1), ("prompt_len", prompt_len, batch), ("hist_len", hist_len, batch),
+                          ("tokens", tokens, n), ("bias_start", bias_start, batch + 1)):
+        _one_or_none(t, name, size)
+    for name, t in (("tree_mask", tree_mask), ("allowed", allowed)):
+        _i32(t, name)
+        if t is not None and (t.dim() != 2 or t.shape[0] != n):
+            raise QcfError(f"{name} must be [rows, words]")
+    if len({x is None for x in (bias_start, bias_token, bias_value)}) > 1:
+        raise QcfError("bias_start, bias_token and bias_value go together")
+    if (history is None) != (hist_len is None) or (history is None and prompt_len is not None):
+        raise QcfError("history and hist_len go together, and prompt_len with them")
+    n_bias = 0 if bias_token is None else bias_token.numel()
+    _i32(bias_token, "bias_token")
+    for name, t, size in (("repetition", repetition, batch), ("presence", presence, batch), ("frequency", frequency, batch),
+                          ("temperature", temperature, batch), ("bias_value", bias_value, n_bias)):
+        _dev(t, name, torch.float32)
+        if t is not None and (t.numel() != size or not t.is_contiguous()):
+            raise QcfError(f"{name} must be dense with {size} entries")
+    _here("qcf_shape_logits", out=out, logits=logits, cu_rows=cu_rows, history=history, prompt_len=prompt_len,
+          hist_len=hist_len, tokens=tokens, tree_mask=tree_mask, repetition=repetition, presence=presence,
+          frequency=frequency, bias_start=bias_start, bias_token=bias_token, bias_value=bias_value, allowed=allowed,
+          temperature=temperature, workspace=workspace)
+    if history is not None and history.shape[1] == 0:  # (an empty tensor has no address)
+        history = prompt_len = hist_len = None
+    need = qcf_shape_logits_workspace_size(n, vocab) if probabilities else 0
+    if workspace is None and need > 0:
+        workspace = torch.empty(need, dtype=torch.uint8, device=out.device)
+    _invoke("qcf_shape_logits", _ptr(out), os_, _dtype(out), _ptr(logits), ls, _dtype(logits), n, vocab, batch,
+            _ptr(cu_rows), _ptr(history), hs, 0 if history is None else history.shape[1], _ptr(prompt_len),
+            _ptr(hist_len), _ptr(tokens), _ptr(tree_mask), 0 if tree_mask is None else tree_mask.shape[1],
+            _ptr(repetition), _ptr(presence), _ptr(frequency), _ptr(bias_start), _ptr(bias_token) if n_bias else None,
+            _ptr(bias_value) if n_bias else None, n_bias, _ptr(allowed), 0 if allowed is None else allowed.shape[1],
+            _ptr(temperature), int(bool(probabilities)), _ptr(workspace), 0 if workspace is None else workspace.numel(),
+            keep=workspace)
+
+
+def qcf_page_fork(table_out, kv_out, held_out, block_table, kv_len, source, free_pages, page_size, n_pages, keep_len=None,
+                  free_head=None, free_head_out=None, copy_src=None, copy_dst=None, copy_rows=None):
+    """New tables in which request b continues request source[b] (at its first keep_len[b] tokens): full pages are
+    shared, the page that it starts is its own, to be filled by qcf_copy_pages(copy_src, copy_dst, copy_rows)."""
+    batch = kv_len.numel()
+    strides = _table(table_out), _table(block_table)
+    for name, t, size in (("kv_out", kv_out, batch), ("held_out", held_out, batch), ("kv_len", kv_len, batch),
+                          ("source", source, batch), ("keep_len", keep_len, batch), ("free_head", free_head, 1),
+                          ("free_head_out", free_head_out, 1), ("copy_src", copy_src, batch),
+                          ("copy_dst", copy_dst, batch), ("copy_rows", copy_rows, batch)):
+        _one_or_none(t, name, size)
+    _i32(free_pages, "free_pages")
+    if block_table.shape[0] != batch or table_out.shape != block_table.shape:
+        raise QcfError("block_table and table_out need a row per request and the same columns")
+    if any(t is None for t in (free_head_out, copy_src, copy_dst, copy_rows)):
+        raise QcfError("qcf_page_fork needs free_head_out, copy_src, copy_dst and copy_rows")
+    _here("qcf_page_fork", table_out=table_out, kv_out=kv_out, held_out=held_out, block_table=block_table, kv_len=kv_len,
+          source=source, free_pages=free_pages, keep_len=keep_len, free_head=free_head, free_head_out=free_head_out,
+          copy_src=copy_src, copy_dst=copy_dst, copy_rows=copy_rows)
+    _invoke("qcf_page_fork", _ptr(table_out), strides[0], _ptr(kv_out), _ptr(held_out), _ptr(block_table), strides[1],
+            block_table.shape[1], batch, _ptr(kv_len), _ptr(source), _ptr(keep_len), _ptr(free_pages),
+            free_pages.numel(), _ptr(free_head), int(n_pages), int(page_size), _ptr(free_head_out), _ptr(copy_src),
+            _ptr(copy_dst), _ptr(copy_rows))
+
+
+class PoolSet:
+    """Pools [slots, heads, head_dim] of one geometry (the keys and values of a cache's layers) for
+    qcf_copy_pages: their addresses on the GPU.  Keeps the pools alive."""
+
+    def __init__(self, pools):
+        self.pools = list(pools)
+        if not self.pools:
+            raise QcfError("a PoolSet needs a pool")
+        first = self.pools[0]
+        for t in self.pools:
+            _dev(t, "pool", first.dtype)
+            if t.dim() < 2 or t.shape != first.shape or t.stride() != first.stride() or t.device != first.device:
+                raise QcfError("pools must be [slots, ...] tensors of the same shape, layout and device")
+            if t.data_ptr() % 16:
+                raise QcfError("pools must be 16-byte aligned")
+        self.n_slots = first.shape[0]
+        self.row_bytes = first.element_size() * math.prod(first.shape[1:])
+        self.row_stride = max(_rows(first, "pool") * first.element_size(), self.row_bytes if self.n_slots <= 1 else 0)
+        self.addresses = torch.tensor([t.data_ptr() for t in self.pools], dtype=torch.int64).to(first.device)
+
+
+def qcf_copy_pages(pools, src_page, dst_page, page_size, rows=None):
+    """Page src_page[i] (its first rows[i] rows) to page dst_page[i] in every pool of a PoolSet."""
+    if not isinstance(pools, PoolSet):
+        raise QcfError("qcf_copy_pages takes a PoolSet")
+    n = src_page.numel()
+    for name, t in (("src_page", src_page), ("dst_page", dst_page), ("rows", rows)):
+        _one_or_none(t, name, n)
+    _here("qcf_copy_pages", addresses=pools.addresses, src_page=src_page, dst_page=dst_page, rows=rows)
+    _invoke("qcf_copy_pages", _ptr(pools.addresses), len(pools.pools), pools.n_slots, pools.row_bytes, pools.row_stride,
+            int(page_size), _ptr(src_page), _ptr(dst_page), _ptr(rows), n, keep=pools)
+
+
+def qcf_page_release(table_before, held_before, table_after, held_after, free_pages, free_head, free_head_out, n_pages):
+    """Pages among the first held_before entries of the one table's rows and of none of the other's first held_after
+    go back in front of the free list's first free entry."""
+    batch = held_before.numel()
+    strides = _table(table_before), _table(table_after)
+    for name, t, size in (("held_before", held_before, batch), ("held_after", held_after, batch),
+                          ("free_head", free_head, 1), ("free_head_out", free_head_out, 1)):
+        if t is None:
+            raise QcfError(f"qcf_page_release needs {name}")
+        _one_or_none(t, name, size)
+    _i32(free_pages, "free_pages")
+    if table_before.shape[0] != batch or table_after.shape != table_before.shape:
+        raise QcfError("the tables need a row per request and the same columns")
+    _here("qcf_page_release", table_before=table_before, held_before=held_before, table_after=table_after,
+          held_after=held_after, free_pages=free_pages, free_head=free_head, free_head_out=free_head_out)
+    _invoke("qcf_page_release", _ptr(table_before), strides[0], _ptr(held_before), _ptr(table_after), strides[1],
+            _ptr(held_after), table_before.shape[1], batch, _ptr(free_pages), free_pages.numel(), _ptr(free_head),
+            _ptr(free_head_out), int(n_pages))

@@ -1,0 +1,459 @@
+"""Norms with rotation, shaped logits, and pages that are forked, copied and released (include/qcf_turns.h) against
+the float64 oracle, at the sizes and masks where they can go wrong.
+
+Tolerances, per element, from the roundings made (a rounding to a type is off by at most half a step:
+2^-8 of the value for bf16, 2^-24 for float32):
+  norm       the sum of d squares is at most d * 2^-24 of itself off, its root half of that; mean, root, quotient and
+             two products five more: a normed value (d / 2 + 5) * 2^-24.  A turned one then as in test_gpu_decode:
+             4 * 2^-24 * (|x1| + |x2|) more, and one rounding to the storage type.
+  logits     z passes five operations, each off by 2^-24 of the largest magnitude on the way (`size`), and one rounding to the type.
+  probabilities  x = z / T two more (the reciprocal and the product): dx = 8 * 2^-24 * size / T.  exp(x - m): dx of the
+             token and of the largest, the difference 2^-24 |x - m|, the exponential 4 * 2^-24; the sum the largest
+             of these (dx of any token that weighs) and 2^-24 for each of at most 32 + 16 + pieces additions in a row; the
+             reciprocal and a product.  So a relative 4 * max dx + (2 |x - m| + 70 + pieces) * 2^-24 and one rounding to the
+             type; below 2^-126 a result may be zero.
+  integers and copies  equal.
+"""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+from oracle import decode as D
+from oracle import turns as T
+from paper_2606_05875_amd import qcf
+from test_gpu_decode import DT, HALF, cum, host, i32, random_parents, rows_of, say, within
+
+pytestmark = pytest.mark.gpu
+E = 2.0 ** -24
+
+
+def f32(a):
+    return torch.from_numpy(np.ascontiguousarray(np.asarray(a, np.float32))).cuda()
+
+
+# -- norms -------------------------------------------------------------------------
+def _norm(rows, hq, hkv, d, dtype, R, inter, kv=True, q=True, gather=False, pad=0, magnitude=1.0, weights="shared",
+          eps=1e-6, seed=0, scale=1.0, wpad=0):
+    rng = np.random.default_rng(seed)
+    src, n_slots = rows + (9 if gather else 0), rows + 13
+    k, kh = rows_of(rng, (src, hkv, d), dtype, pad, scale)
+    v, vh = rows_of(rng, (src, hkv, d), dtype, pad)
+    x, xh = rows_of(rng, (src, hq, d), dtype, 2 * pad, scale)
+    kc, vc = rows_of(rng, (n_slots, hkv, d), dtype, 3 * pad), rows_of(rng, (n_slots, hkv, d), dtype, 3 * pad)
+    slots = rng.permutation(n_slots)[:rows]
+    idx = rng.permutation(src)[:rows]
+    if rows > 3:
+        slots[1], slots[2] = -1, n_slots                      # stored nowhere
+    if gather and rows > 5:
+        idx[3], idx[4] = -1, src                              # no such source
+    pos = rng.integers(0, 40000, rows)
+    freq = D.rope_frequencies(R, 1e4)
+    weight = lambda h: (None, None) if weights == "none" else \
+        tuple(y[0] if weights == "shared" else y for y in rows_of(rng, (h, d), dtype, wpad))
+    (qw, qwh), (kw, kwh) = weight(hq), weight(hkv)
+    out = torch.full((rows, hq, d), 3.0, dtype=DT[dtype], device="cuda")
+    more = dict(q_new=x, q_out=out, q_weight=qw) if q else {}
+    if kv:
+        more["k_weight"] = kw
+    args = (kc[0], vc[0], k, v, i32(slots)) if kv else (None,) * 5
+    qcf.qcf_norm_rope_store(*args, *((i32(pos), torch.from_numpy(freq).cuda()) if R else ()), interleaved=inter,
+                            magnitude=magnitude, src_idx=i32(idx) if gather else None, eps=eps, **more)
+    at = idx if gather else np.arange(rows)
+    ok_src = (at >= 0) & (at < src)
+    at = np.where(ok_src, at, 0)
+    eps = float(np.float32(eps))
+
+    def check(got, was, src_h, w, where, what):
+        y, size = T.norm_rope(src_h[at], pos, freq if R else [], w, eps, inter, magnitude)
+        want, bound = was.copy(), np.zeros_like(was)           # other rows keep their bits
+        ok = ok_src & (where >= 0) & (where < was.shape[0])
+        want[where[ok]] = y[ok]
+        bound[where[ok]] = (HALF[dtype] * np.abs(y) + ((d / 2 + 5) + (4 if R else 0)) * E * size * (1 + 2 ** -7))[ok]
+        within(got, want, bound, what)
+
+    if kv:
+        check(host(kc[0]), kc[1], kh, kwh, slots, "keys")
+        ok = ok_src & (slots >= 0) & (slots < n_slots)
+        want = vc[1].copy()
+        want[slots[ok]] = vh[at][ok]
+        np.testing.assert_array_equal(host(vc[0]), want)
+    if q:
+        check(host(out), np.full((rows, hq, d), 3.0), xh, qwh, np.arange(rows), "queries")
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("hq,hkv,d", [(8, 2, 64), (32, 8, 128), (16, 1, 128), (5, 5, 64), (64, 8, 128), (1, 1, 64)])
+@pytest.mark.parametrize("inter", [False, True])
+def test_norm_rope_store(dtype, hq, hkv, d, inter):
+    say("norm rope store", dtype, hq, hkv, d, inter)
+    for rows, R, kw in ((1, d, {}), (5, 16, dict(pad=8, weights="heads")), (37, d - 16, dict(gather=True, magnitude=1.25)),
+                        (300, d, dict(pad=16, weights="heads", wpad=8)), (11, 48, dict(kv=False, weights="none")),
+                        (12, 32, dict(q=False, gather=True)), (2100, d // 2, dict(gather=True, weights="heads")),
+                        (1031, 0, dict(weights="shared")), (6, d, dict(eps=0.0, scale=1e-3)), (700, 16, dict(q=False))):
+        _norm(rows, hq, hkv, d, dtype, R, inter, seed=rows, **kw)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_norms_of_any_size(dtype):
+    """Rows of very different sizes, zeros (eps decides), values that are not numbers in one head only."""
+    say("norms of any size", dtype)
+    _norm(40, 8, 2, 128, dtype, 128, False, scale=1e12, seed=2)
+    _norm(40, 8, 2, 128, dtype, 64, True, scale=1e-12, eps=1e-30, seed=3)
+    x = torch.randn(4, 2, 64, device="cuda").to(DT[dtype])
+    x[0] = 0
+    x[1, 0, 5] = math.nan
+    x[2, 0, 7] = math.inf
+    out = torch.empty_like(x)
+    call = lambda eps: qcf.qcf_norm_rope_store(None, None, None, None, None, q_new=x, q_out=out, eps=eps)
+    call(1e-6)
+    got = host(out)
+    assert (got[0] == 0).all() and np.isnan(got[1, 0]).all() and np.isfinite(got[1, 1]).all()
+    assert np.isnan(got[2, 0, 7]) and (np.delete(got[2, 0], 7) == 0).all()
+    call(0.0)
+    assert np.isnan(host(out)[0]).all() and np.isfinite(host(out)[3]).all()
+
+
+def test_norm_rope_store_refuses():
+    x = torch.randn(4, 2, 64, device="cuda")
+    out, one = torch.empty_like(x), torch.ones(64, device="cuda")
+    bad = lambda **k: pytest.raises(qcf.QcfError, qcf.qcf_norm_rope_store, None, None, None, None, None,
+                                    **{**dict(q_new=x, q_out=out), **k})
+    bad(q_weight=one[:32])
+    bad(q_weight=one.bfloat16())
+    bad(q_weight=torch.ones(3, 64, device="cuda"))
+    bad(q_weight=torch.ones(64, 2, device="cuda").T)
+    bad(k_weight=one)
+    bad(q_weight=one.cpu())
+    bad(eps=-1.0)
+    bad(eps=math.nan)
+    bad(q_weight=torch.ones(65, device="cuda")[1:])
+    bad(q_out=None, q_weight=one)
+
+
+# -- logits ------------------------------------------------------------------------
+def _shape(new, hist, vocab, dtype="f32", out="f32", penalties=True, bias=0, grammar=False, tree=False, temps=None,
+           pad=(0, 0), seed=0, probabilities=True, tokens=True, spare=2, offset=0, z=None, in_place=False, words=None,
+           width=None, rep=None, allow=None, ws=None, prompts=None):
+    rng = np.random.default_rng(seed)
+    B, n = len(new), int(sum(new))
+    cu = cum(new)
+    rows = n + spare
+    z = 4 * rng.standard_normal((rows, vocab)) if z is None else z
+    make = lambda t, p: torch.full((offset + rows * (vocab + p),), math.nan, dtype=DT[t], device="cuda")[offset:].as_strided(
+        (rows, vocab), (vocab + p, 1))
+    logits = make(dtype, pad[0])
+    logits.copy_(torch.from_numpy(z))
+    zh = host(logits)
+    o = logits if in_place else make(out, pad[1])
+    if not in_place:
+        o.fill_(7.0)
+    keep = host(o)[n:]
+    kw, width = {}, max(list(hist) + [0]) + 2 if width is None else width
+    history = rng.integers(-2, min(vocab + 2, 60), (B, width))
+    if width > 5:
+        history[:, 3] = vocab - 1
+    prompt = np.array([int(h * rng.random()) for h in hist]) if prompts is None else np.array(prompts)
+    toks = rng.integers(-1, min(vocab + 1, 70), rows)
+    if penalties:
+        kw.update(history=i32(history), hist_len=i32(hist), prompt_len=i32(prompt))
+        pen = [f32(x) for x in (rng.uniform(0.7, 1.6, B) if rep is None else rep, rng.uniform(-1, 1, B), rng.uniform(-0.2, 0.5, B))]
+        kw.update(repetition=pen[0], presence=pen[1], frequency=pen[2])
+        if tokens:
+            kw["tokens"] = i32(toks)
+    parents = random_parents(rng, new) if tree else None
+    bits = None
+    if tree:
+        words = (max(list(new) + [1]) + 31) // 32 if words is None else words
+        bits = np.zeros((rows, 32 * words), bool)
+        for b, m in enumerate(new):
+            for i in range(m):
+                a = i
+                while a >= 0:
+                    bits[cu[b] + i, a] = True
+                    a = parents[cu[b] + a]
+                bits[cu[b] + i, m:] = rng.random(32 * words - m) < 0.5      # beyond the request: not followed
+        if penalties and tokens:
+            kw["tree_mask"] = i32(D.pack_bits(bits))
+    entries = [[] for _ in new]
+    if bias:
+        each = [int(rng.integers(0, bias + 1)) for _ in new]
+        tok, val = rng.integers(-2, min(vocab + 3, 40 + bias), sum(each)), rng.normal(0, 3, sum(each)).astype(np.float32)
+        s = cum(each)
+        entries = [list(zip(tok[s[b]:s[b + 1]].tolist(), val[s[b]:s[b + 1]].astype(np.float64).tolist())) for b in range(B)]
+        kw.update(bias_start=i32(s), bias_token=i32(tok), bias_value=f32(val))
+    allowed = None
+    if grammar:
+        aw = (vocab + 31) // 32 + 1
+        a = rng.random((rows, aw * 32)) < rng.choice([0.02, 0.5, 1.0], (rows, 1))
+        if n:
+            a[0, :vocab] = False                               # nothing is allowed
+        if n > 1:
+            a[1, :vocab] = False
+            a[1, vocab - 1] = True
+        if allow is not None:
+            a[:] = allow
+        allowed = a[:, :vocab]
+        kw["allowed"] = i32(D.pack_bits(a))
+    temps = rng.uniform(0.3, 2.0, B) if temps is None else np.asarray(temps)
+    t32 = temps.astype(np.float32)
+    if probabilities:
+        kw["temperature"] = f32(temps)
+    qcf.qcf_shape_logits(o, logits, i32(cu), probabilities=probabilities, workspace=ws, **kw)
+    got = host(o)
+    np.testing.assert_array_equal(got[n:], keep)               # rows behind the last request
+    pieces = -(-vocab // 1024)
+    half = HALF[out if not in_place else dtype]
+    for b, m in enumerate(new):
+        for i in range(m):
+            r = int(cu[b]) + i
+            follows = [j for j in range(m) if bits[r, j]] if tree and j_in(bits) else list(range(i + 1))
+            follows = [j for j in range(m) if bits[r, j]] if tree else follows
+            pr, an = T.said_by(r, b, history if penalties else None, prompt[b], hist[b], toks if penalties and tokens else None,
+                               int(cu[b]), follows)
+            p64 = [float(kw[x][b]) for x in ("repetition", "presence", "frequency")] if penalties else [1.0, 0.0, 0.0]
+            want, size = T.shape_logits(zh[r], pr, an, p64[0], p64[1], p64[2], entries[b],
+                                        None if allowed is None else allowed[r])
+            if not probabilities:
+                tol = 5 * E * size + half * np.abs(np.where(np.isfinite(want), want, 0))
+                same = ~np.isfinite(want)
+                np.testing.assert_array_equal(got[r][same], want[same])
+                within(got[r][~same], want[~same], tol[~same], f"row {r}")
+                continue
+            temp = float(t32[b])
+            p, _ = T.shape_logits(zh[r], pr, an, p64[0], p64[1], p64[2], entries[b], None if allowed is None else allowed[r], temp)
+            if np.isnan(p).any() or temp == 0 or not p.any():
+                np.testing.assert_array_equal(got[r], p)
+                continue
+            x = want / temp
+            live = np.isfinite(x)
+            dx = 8 * E * np.where(live, size, 0).max() / temp
+            gapx = np.where(live, x.max() - x, 0)
+            tol = p * (4 * dx + (2 * gapx + 70 + pieces) * E) * (1 + 1e-3) + half * p + 2.0 ** -125
+            within(got[r], p, tol, f"row {r}")
+    return o
+
+
+def j_in(bits):
+    return bits is not None
+
+
+@pytest.mark.parametrize("dtype,out", [("f32", "f32"), ("bf16", "f32"), ("bf16", "bf16"), ("f32", "bf16")])
+@pytest.mark.parametrize("probabilities", [True, False])
+def test_shape_logits(dtype, out, probabilities):
+    say("shape logits", dtype, out, probabilities)
+    kw = dict(dtype=dtype, out=out, probabilities=probabilities)
+    _shape([1], [5], 1, **kw)
+    _shape([1, 1, 1], [0, 40, 7], 1000, **kw)
+    _shape([3, 0, 2, 5], [9, 3, 0, 100], 777, pad=(3, 1), bias=30, grammar=True, **kw)
+    _shape([4, 9], [30, 0], 2049, tree=True, bias=5, pad=(0, 5), seed=2, **kw)
+    _shape([40, 3], [300, 20], 500, tree=True, grammar=True, words=3, seed=3, **kw)
+    _shape([2, 1], [2000, 1], 20011, bias=300, grammar=True, offset=1, seed=4, **kw)
+    _shape([1, 2], [100, 50], 70003, tree=True, bias=100, pad=(1, 0), offset=3, seed=5, **kw)
+    _shape([2], [50], 33000, penalties=False, seed=6, **kw)
+    _shape([2, 2], [50, 9], 9000, tokens=False, seed=7, **kw)
+    _shape([1], [40], 8192, seed=8, **kw)
+    _shape([1], [40], 8193, seed=9, grammar=True, allow=True, **kw)
+    _shape([2, 1], [0, 0], 16384, seed=10, width=0, **kw)
+    _shape([1, 1], [9, 9], 300, seed=11, prompts=[-4, 100], **kw)
+
+
+def test_shape_logits_in_place_and_many_requests():
+    say("shape logits in place, many requests")
+    _shape([3, 2], [30, 50], 30001, in_place=True, bias=9, grammar=True)
+    _shape([3, 2], [30, 50], 30001, dtype="bf16", in_place=True, probabilities=False)
+    _shape([1, 0, 2] * 200, [3, 0, 9] * 200, 50, seed=3, bias=4)
+    _shape([0, 0], [1, 2], 100, spare=3)
+    _shape([1], [0], 150001, seed=4)
+    need = qcf.qcf_shape_logits_workspace_size(7, 30001)
+    ws = torch.full((need + 256,), 0xFF, dtype=torch.uint8, device="cuda")
+    a = _shape([3, 2], [30, 50], 30001, ws=ws)
+    assert torch.equal(a, _shape([3, 2], [30, 50], 30001, ws=ws))
+
+
+def test_shape_logits_cold_and_odd_values():
+    """T = 0 takes the largest, the lowest of equal ones; infinities and NaN where nothing is allowed stay out, and
+    where they are allowed make the row NaN."""
+    say("shape logits, cold and odd values")
+    rng = np.random.default_rng(3)
+    for vocab in (500, 40000):
+        z = np.round(2 * rng.standard_normal((8, vocab)))                # many equal ones
+        _shape([2, 1, 3], [5, 0, 9], vocab, z=z, temps=[0.0, 1.0, 0.0], grammar=True, seed=1)
+        z = z.copy()
+        z[2, 7], z[3, 9], z[4, vocab - 1] = math.nan, math.inf, -math.inf
+        z[5] = -math.inf
+        _shape([1, 1, 1, 1, 1, 1], [0] * 6, vocab, z=z, temps=[1.0, 0.5, 1.0, 1.0, 0.7, 1.0])
+        a = np.ones((8, ((vocab + 31) // 32 + 1) * 32), bool)
+        a[2, 7] = a[3, 9] = False
+        _shape([1, 1, 1, 1, 1, 1], [0] * 6, vocab, z=z, grammar=True, allow=a, temps=[1.0, 0.5, 1.0, 1.0, 0.7, 0.0])
+        _shape([1, 1, 1], [0] * 3, vocab, z=60 * rng.standard_normal((5, vocab)), temps=[0.05, 1.0, 30.0], rep=[1.0, 1e-3, 1e3])
+
+
+def test_shape_logits_feeds_verification():
+    """The probabilities are qcf_verify_drafts' target: a token is drawn where something is allowed, none (-1) where nothing is."""
+    say("shape logits, verification")
+    vocab, B = 9000, 2
+    logits = torch.randn(2, vocab, device="cuda")
+    allowed = torch.zeros((2, (vocab + 31) // 32), dtype=torch.int32, device="cuda")
+    allowed[0, 100] = 1 << 5
+    cu, out = i32([0, 1, 2]), torch.empty_like(logits)
+    qcf.qcf_shape_logits(out, logits, cu, allowed=allowed)
+    n_out, path, toks = i32([0, 0]), i32([[0], [0]]), i32([[0], [0]])
+    qcf.qcf_verify_drafts(n_out, path, toks, out, i32([1, 1]), cu, f32([0.5, 0.5]), f32([0.9, 0.1]))
+    assert toks.cpu().tolist() == [[3205], [-1]]
+
+
+# -- pages -------------------------------------------------------------------------
+def _paged(kv, ps, seed=0, held=None, cols=None, spare=9, share=()):
+    rng = np.random.default_rng(seed)
+    need = [-(-max(k, 0) // ps) for k in kv] if held is None else held
+    cols = max(list(need) + [0]) + 2 if cols is None else cols
+    pages = sum(need) + spare
+    order = rng.permutation(pages)
+    table, at = np.full((len(kv), cols), -5), 0
+    for b, h in enumerate(need):
+        h = min(h, cols)
+        table[b, :h] = order[at:at + h]
+        at += h
+    for a, b, n in share:                                       # b's first n pages are a's
+        table[b, :n] = table[a, :n]
+    return table, order, at, pages, need
+
+
+def _fork(kv, ps, source, keep=None, seed=0, free=None, head=None, cols=None, share=(), held=None, heads=2, layers=2, no_head=False):
+    table, order, at, pages, _ = _paged(kv, ps, seed, held, cols, spare=len(kv) + 4, share=share)
+    B, cols = table.shape
+    full = lambda *shape: torch.full(shape, -9, dtype=torch.int32, device="cuda")
+    wide = full(B, cols + 3)
+    out, kvo, ho, fo, cs, cd, cr = wide[:, :cols], full(B), full(B), full(1), full(B), full(B), full(B)
+    free = order if free is None else free(order, pages)
+    head = at if head is None else head
+    qcf.qcf_page_fork(out, kvo, ho, i32(table) if B else full(0, cols), i32(kv), i32(source), i32(free), ps, pages,
+                      keep_len=None if keep is None else i32(keep), free_head=None if no_head else i32([head]), free_head_out=fo,
+                      copy_src=cs, copy_dst=cd, copy_rows=cr)
+    want = T.page_fork(table, kv, source, free, ps, pages, keep, 0 if no_head else head)
+    got = [host(x).astype(np.int64) for x in (out, kvo, ho)]
+    for g, w, name in zip(got, want[:3], ("table", "lengths", "held")):
+        np.testing.assert_array_equal(g, w, err_msg=name)
+    assert int(fo[0]) == want[3]
+    np.testing.assert_array_equal(np.stack([host(x) for x in (cs, cd, cr)], 1).reshape(-1, 3), np.array(want[4]).reshape(-1, 3))
+    assert (wide[:, cols:] == -9).all()
+    return cs, cd, cr, want[4], pages
+
+
+@pytest.mark.parametrize("ps", [1, 2, 16, 128])
+def test_page_fork(ps):
+    say("page fork", ps)
+    rng = np.random.default_rng(ps)
+    _fork([7], ps, [0])
+    _fork([0, 5 * ps, 5 * ps + 1, 3], ps, [1, 2, 2, 2])
+    _fork([0, 5 * ps, 5 * ps + 1, 3], ps, [3, 1, 0, 2])                     # everyone another's
+    _fork([9, 20, 33], ps, [-1, 3, 1])                                       # the first two end
+    _fork([9, 20, 33, 50], ps, [1, 1, 2, 3], keep=[15, 3, 100, 0])
+    _fork([9, 20, 33, 50], ps, [0, 1, 2, 3], keep=[9, 19, 32, -4], share=[(2, 3, 2)] if ps < 16 else ())
+    _fork([-3, 20], ps, [0, 1])
+    kv = rng.integers(0, 300, 700)
+    _fork(kv, ps, rng.integers(-1, 701, 700), keep=rng.integers(0, 300, 700))   # several rounds of counting
+    _fork([30, 9], ps, [0, 1], held=[60, 40])                                # more pages than tokens
+
+
+def test_page_fork_runs_out():
+    say("page fork runs out")
+    _fork([9, 9, 9, 9], 4, [0, 0, 0, 0], free=lambda f, n: f[:14])
+    _fork([9, 9, 9, 9], 4, [0, 0, 0, 0], free=lambda f, n: np.where(np.arange(f.size) % 2 == 0, n + 3, f))
+    _fork([9, 9, 9, 9], 4, [0, 0, 0, 0], free=lambda f, n: np.where(np.arange(f.size) % 2 == 0, -2, f))
+    _fork([9, 9], 4, [1, 0], free=lambda f, n: f[:0], head=0)
+    _fork([9, 9], 4, [1, 0], head=10 ** 6)
+    _fork([9, 9], 4, [1, 0], head=-1)
+    _fork([9, 9], 4, [1, 0], no_head=True)
+    _fork([9, 30], 4, [1, 0], cols=3)                                        # the table ends
+    _fork([9, 30], 4, [1, 0], cols=8, held=[1, 7])                           # a source's page is not there
+    _fork([], 4, [], cols=4)
+
+
+@pytest.mark.parametrize("dtype,heads,d,pad,ps,layers", [("bf16", 8, 128, 128, 16, 3), ("f32", 1, 64, 0, 1, 2), ("bf16", 5, 64, 8, 64, 1),
+                                                         ("f32", 8, 128, 4, 128, 2), ("bf16", 64, 128, 0, 4, 1), ("bf16", 1, 8, 0, 2, 5)])
+def test_copy_pages(dtype, heads, d, pad, ps, layers):
+    say("copy pages", dtype, heads, d, pad, ps, layers)
+    rng = np.random.default_rng(4)
+    pages = 23
+    pools = [torch.from_numpy(rng.standard_normal((pages * ps + (ps > 1), heads * d + pad))).to(DT[dtype]).cuda() for _ in range(2 * layers)]
+    views = [x[:, :heads * d].view(-1, heads, d) for x in pools]
+    order = rng.permutation(pages)
+    src, dst = order[:8].copy(), order[8:16].copy()
+    rows = rng.integers(0, ps + 1, 8)
+    rows[0], rows[1], rows[2] = ps, ps + 5, -3
+    src[3], dst[4], src[5], dst[6] = -1, -1, pages, pages
+    src[7] = dst[7]
+    for r in (rows, None):
+        want = [x.clone() for x in pools]
+        for i in range(8):
+            n = ps if r is None else min(max(int(r[i]), 0), ps)
+            if 0 <= src[i] < pages and 0 <= dst[i] < pages:
+                for x in want:
+                    x[dst[i] * ps:dst[i] * ps + n, :heads * d] = x[src[i] * ps:src[i] * ps + n, :heads * d].clone()
+        qcf.qcf_copy_pages(qcf.PoolSet(views), i32(src), i32(dst), ps, rows=None if r is None else i32(r))
+        for a, b in zip(pools, want):
+            assert torch.equal(a, b)
+    qcf.qcf_copy_pages(qcf.PoolSet(views), i32([]), i32([]), ps)
+
+
+def test_pool_sets_are_checked():
+    a = torch.zeros(32, 2, 64, device="cuda")
+    for bad in ([a, a.bfloat16()], [a, a[:16]], [a, torch.zeros(32, 3, 64, device="cuda")[:, :2]], [a, a.cpu()],
+                [a.view(-1)[1:1 + 31 * 128].view(31, 2, 64)]):
+        with pytest.raises(qcf.QcfError):
+            qcf.PoolSet(bad)
+    i = i32([0])
+    with pytest.raises(qcf.QcfError):
+        qcf.qcf_copy_pages(qcf.PoolSet([a]), i, i, 24)
+    with pytest.raises(qcf.QcfError):
+        qcf.qcf_copy_pages(qcf.PoolSet([a]), i, i32([1, 2]), 16)
+    with pytest.raises(qcf.QcfError):
+        qcf.qcf_copy_pages(qcf.PoolSet([torch.zeros(32, 3, device="cuda")]), i, i, 16)   # rows of 12 bytes
+
+
+def _release(before, hb, after, ha, free, head, pages):
+    fl, fo = i32(free), i32([-9])
+    same = after is before
+    t = i32(before)
+    qcf.qcf_page_release(t, i32(hb), t if same else i32(after), i32(ha), fl, i32([head]), fo, pages)
+    want, at = T.page_release(before, hb, after, ha, free, head, pages)
+    np.testing.assert_array_equal(host(fl), want)
+    assert int(fo[0]) == at
+
+
+@pytest.mark.parametrize("B,most,pages_more", [(1, 3, 5), (3, 200, 9), (40, 70, 40), (300, 20, 0), (2, 9000, 100), (1100, 5, 3)])
+def test_page_release(B, most, pages_more):
+    say("page release", B, most, pages_more)
+    rng = np.random.default_rng(B)
+    held = rng.integers(0, most + 1, B)
+    table, order, at, pages, _ = _paged([0] * B, 16, B, held=held, spare=pages_more)
+    for b in range(1, B):
+        n = min(held[b], held[b - 1]) // 2
+        if b % 3:
+            table[b, :n] = table[b - 1, :n]                                  # shared contexts
+    _release(table, held, table, np.zeros(B, int), order, at, pages)         # all end
+    _release(table, held, table, held, order, at, pages)                     # none does
+    shorter = (held * rng.random(B)).astype(int)
+    _release(table, held, table, shorter, order, at, pages)
+    moved = table[rng.integers(0, B, B)]
+    _release(table, held, moved, shorter, order, at, pages)
+    _release(table, held + 5, moved, shorter - 3, order, at, pages)          # columns that hold nothing, negative lengths
+    _release(table, held, moved, shorter, order[:max(at - 1, 0)], at + 7, pages)   # the list had run out
+    _release(table, held, table, np.zeros(B, int), order, at // 2, pages)    # more than were taken
+    _release(table, held, table, np.zeros(B, int), order, -1, pages)
+
+
+def test_page_release_large_pools():
+    """Pools of more pages than one go marks."""
+    say("page release, large pools")
+    rng = np.random.default_rng(1)
+    pages = 3 * (1 << 19) + 77
+    table = rng.choice(pages, (30, 400), replace=False)
+    held, after = np.full(30, 400), rng.integers(0, 401, 30)
+    _release(table, held, table, after, np.arange(20000), 15000, pages)
+    _release(np.zeros((0, 4), int), [], np.zeros((0, 4), int), [], np.arange(5), 3, 10)
+    _release(np.zeros((3, 0), int), [1, 0, 2], np.zeros((3, 0), int), [0, 0, 0], np.arange(5), 3, 10)
+    _release(np.zeros((1, 4), int), [2], np.zeros((1, 4), int), [0], np.arange(5), 3, 0)
