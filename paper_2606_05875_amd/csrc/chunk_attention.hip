@@ -54,8 +54,8 @@ __global__ __launch_bounds__(kW * 64, 2) void chunk_attn_kernel(ChunkAttn p, Chu
 
   chunk_walk<kW * 64>(p, cut, ws, lg, [&](int b, const TreeRequest& rq, int g, int tile, int first, int n, int slot) {
     const int32_t* table = p.block_table + b * p.table_stride;
-    const uint16_t* kc = static_cast<const uint16_t*>(p.k_cache) + (int64_t)g * D;
-    const uint16_t* vc = static_cast<const uint16_t*>(p.v_cache) + (int64_t)g * D;
+    const char* kc = static_cast<const char*>(p.k_cache) + (int64_t)g * RB;
+    const char* vc = static_cast<const char*>(p.v_cache) + (int64_t)g * RB;
     const bool pool = p.n_pages > 0;
     const int t_first = first * kT;
     // Page numbers of a tile's groups: lane i (i < 4) looks up group i
@@ -74,14 +74,15 @@ __global__ __launch_bounds__(kW * 64, 2) void chunk_attn_kernel(ChunkAttn p, Chu
     // stand in and are not seen
     auto base_of = [&](int t, int page) {
       const int t0 = t_first + t * kT + 16 * w;
-      return (page < 0 ? 0 : ((int64_t)page << p.page_log2) + (t0 & ((1 << p.page_log2) - 1))) * p.kv_stride;
+      const uint32_t row = page < 0 ? 0u : ((uint32_t)page << p.page_log2) + (t0 & ((1 << p.page_log2) - 1));
+      return (uint64_t)row * row_b;
     };
-    auto copy_k = [&](int t, int64_t at, int i) {
+    auto copy_k = [&](int t, uint64_t at, int i) {
       asm volatile("" : "+v"(coff), "+v"(kx));  // (formed anew: every copy's offset kept is a register each)
       const uint32_t c = kx ^ (i * 64);
       copy16(kc + at, coff + i * RPC * row_b + c, k_lds + (t & 1) * TB + (w * GC + i) * 1024);
     };
-    auto copy_v = [&](int t, int64_t at, int i) {
+    auto copy_v = [&](int t, uint64_t at, int i) {
       asm volatile("" : "+v"(coff));
       copy16(vc + at, coff + i * RPC * row_b + vx, v_lds + (t & 1) * TB + (w * GC + i) * 1024);
     };
@@ -124,7 +125,7 @@ __global__ __launch_bounds__(kW * 64, 2) void chunk_attn_kernel(ChunkAttn p, Chu
 #pragma unroll
       for (int st = 0; st < D / 16; ++st) asm volatile("" : "+v"(qreg[st]));
       if (pool) {
-        const int64_t a0 = base_of(0, page0), a1 = base_of(1, page1);
+        const uint64_t a0 = base_of(0, page0), a1 = base_of(1, page1);
 #pragma unroll
         for (int i = 0; i < GC; ++i) copy_k(0, a0, i);
 #pragma unroll
@@ -189,7 +190,7 @@ __global__ __launch_bounds__(kW * 64, 2) void chunk_attn_kernel(ChunkAttn p, Chu
     // read four groups ahead, a group's arguments, exponentials and sums in three groups in turn, and the copies of
     // K(t+2) and V(t+1) in between
     auto weights = [&](auto next_s, const uint8_t* kn, f32x16 (&sn)[2], f32x16 (&s)[2], bf16x8 (&pb)[2][2], int t,
-                       int64_t ak, int64_t av) {
+                       uint64_t ak, uint64_t av) {
       constexpr bool kNext = decltype(next_s)::value;
       constexpr int NM = 2 * NS, EG = 32 / NM, PF = 4, DSTEP = NM / (2 * GC);
       const float nm = -finite(m), sc = big ? 1.f : scale2;
@@ -222,7 +223,7 @@ __global__ __launch_bounds__(kW * 64, 2) void chunk_attn_kernel(ChunkAttn p, Chu
           if (i + PF < NM) kf[i + PF] = k_frag(kn, i + PF);
           if (i % DSTEP == 0) {
             if (i / DSTEP < GC) {
-              if (t + 2 < n) copy_k(t + 2, ak, i / DSTEP);
+              copy_k(t + 2, ak, i / DSTEP);  // (behind the last tile from the pool's first rows, for nobody)
             } else {
               copy_v(t + 1, av, i / DSTEP - GC);
             }
@@ -308,11 +309,37 @@ __global__ __launch_bounds__(kW * 64, 2) void chunk_attn_kernel(ChunkAttn p, Chu
 
     // the wave has a row that sees a token of the tile at t0
     auto uses = [&](int t0) { return busy && t0 < w_hi && t0 + kT > w_lo; };
-    // step t: tile t's softmax and O, S of tile t + 1 (into sn)
-    auto step = [&](int t, f32x16 (&s)[2], f32x16 (&sn)[2]) {
+    auto on = [&](int t) {  // the page numbers move up
+      there0 = there1;
+      there1 = there2;
+      page1 = page2;
+      there2 = pages_of(t + 3, next, page2);
+    };
+    // a tile that all rows of the block see, its next S (into sn) beside it
+    auto plain_step = [&](int t, f32x16 (&s)[2], f32x16 (&sn)[2]) {
+      next = look(t + 3);
+      bf16x8 pb[2][2];
+      const uint64_t ak = base_of(t + 2, page2), av = base_of(t + 1, page1);
+      maximum(s, true);
+      __builtin_amdgcn_s_setprio(1);
+      weights(std::true_type{}, k_ring + ((t + 1) & 1) * TB, sn, s, pb, t, ak, av);
+      __builtin_amdgcn_s_setprio(0);
+      products_o(v_ring + (t & 1) * TB, pb);
+      meet();
+      on(t);
+    };
+    // any tile, its next S (into s) after it
+    auto other_step = [&](int t, f32x16 (&s)[2]) {
       const int t0 = t_first + t * kT;
       const bool now = uses(t0), then = t + 1 < n && uses(t0 + kT);
       next = look(t + 3);
+      const uint64_t ak = base_of(t + 2, page2), av = base_of(t + 1, page1);
+      if (t + 2 < n)
+#pragma unroll
+        for (int i = 0; i < GC; ++i) copy_k(t + 2, ak, i);
+      if (t + 1 < n)
+#pragma unroll
+        for (int i = 0; i < GC; ++i) copy_v(t + 1, av, i);
       uint64_t held = ~0ull, loose = 0;
       if (t0 + kT > plain_hi || t0 < plain_lo || there0 != 15) {
         held = 0;
@@ -322,62 +349,52 @@ __global__ __launch_bounds__(kW * 64, 2) void chunk_attn_kernel(ChunkAttn p, Chu
         if (rq.end - t0 < kT) held &= rq.end > t0 ? (1ull << (rq.end - t0)) - 1ull : 0ull;
         loose = clean(t, held);
       }
-      uint64_t sees = ~0ull;
-      if (now && (t0 + kT > all_hi || t0 < all_lo || held != ~0ull)) {
-        const int from = min(max(r_lo - t0, 0), kT), to = min(max(r_hi - t0, 0), kT);
-        sees = held & (to < kT ? (1ull << to) - 1ull : ~0ull) & (from < kT ? ~0ull << from : 0ull);
+      if (now) {
+        uint64_t sees = ~0ull;
+        if (t0 + kT > all_hi || t0 < all_lo || held != ~0ull) {
+          const int from = min(max(r_lo - t0, 0), kT), to = min(max(r_hi - t0, 0), kT);
+          sees = held & (to < kT ? (1ull << to) - 1ull : ~0ull) & (from < kT ? ~0ull << from : 0ull);
 #pragma unroll
-        for (int hb = 0; hb < 2; ++hb) {
-          const uint32_t mine = (uint32_t)(sees >> (32 * hb)) >> (4 * hi);
+          for (int hb = 0; hb < 2; ++hb) {
+            const uint32_t mine = (uint32_t)(sees >> (32 * hb)) >> (4 * hi);
 #pragma unroll
-          for (int v = 0; v < 16; ++v)
-            if (!(mine >> (8 * (v >> 2) + (v & 3)) & 1)) s[hb][v] = -INFINITY;
+            for (int v = 0; v < 16; ++v)
+              if (!(mine >> (8 * (v >> 2) + (v & 3)) & 1)) s[hb][v] = -INFINITY;
+          }
         }
-      }
-      bf16x8 pb[2][2];
-      const int64_t ak = base_of(t + 2, page2), av = base_of(t + 1, page1);
-      if (!then) {
-#pragma unroll
-        for (int i = 0; i < GC; ++i)
-          if (t + 2 < n) copy_k(t + 2, ak, i);
-#pragma unroll
-        for (int i = 0; i < GC; ++i)
-          if (t + 1 < n) copy_v(t + 1, av, i);
-      }
-      if (now) maximum(s, sees != 0);
-      const uint8_t* kn = k_ring + ((t + 1) & 1) * TB;
-      if (then && now) {
-        weights(std::true_type{}, kn, sn, s, pb, t, ak, av);
-      } else if (now) {
-        weights(std::false_type{}, kn, sn, s, pb, t, ak, av);
-      } else if (then) {  // (the first tile of a window's)
-#pragma unroll
-        for (int i = 0; i < GC; ++i)
-          if (t + 2 < n) copy_k(t + 2, ak, i);
-#pragma unroll
-        for (int i = 0; i < GC; ++i) copy_v(t + 1, av, i);
-        products(kn, sn);
-      }
-      if (loose) {
-        if (now) add_loose(t, loose, sees, s);
+        maximum(s, sees != 0);
+        bf16x8 pb[2][2];
+        weights(std::false_type{}, k_ring, s, s, pb, t, ak, av);
+        if (loose) {
+          add_loose(t, loose, sees, s);
+          take_out(t, loose);
+        }
+        products_o(v_ring + (t & 1) * TB, pb);
+      } else if (loose) {
         take_out(t, loose);
       }
-      if (now) products_o(v_ring + (t & 1) * TB, pb);
+      if (then) products(k_ring + ((t + 1) & 1) * TB, s);
       meet();
-      there0 = there1;
-      there1 = there2;
-      page1 = page2;
-      there2 = pages_of(t + 3, next, page2);
+      on(t);
     };
 
     if (pool) {
+      // tiles from plain_at on before plain_end are seen by all rows of the block
+      const int plain_end = min((plain_hi - t_first) >> 6, n), plain_at = (max(plain_lo - t_first, 0) + kT - 1) >> 6;
       f32x16 sa[2], sb[2];
       meet();
       if (uses(t_first)) products(k_ring, sa);
       meet();  // K(0) has been read before K(2) takes its place
-      for (int t = 0; t < n; t += 2) {
-        step(t, sa, sb);
-        if (t + 1 < n) step(t + 1, sb, sa);
+      for (int t = 0; t < n;) {
+        if (busy && t >= plain_at) {
+          const int end = min(plain_end - 1, n - 2);
+          for (; t < end; t += 2) {
+            if ((there0 & there1) != 15) break;
+            plain_step(t, sa, sb);
+            plain_step(t + 1, sb, sa);
+          }
+        }
+        other_step(t++, sa);
       }
     }
     ls += __shfl_xor(ls, 32, 64);
@@ -413,9 +430,8 @@ hipError_t launch_bf16(const ChunkAttn& p, void* workspace, hipStream_t stream) 
   const int lg = log2_of(p.hq / p.hkv);
   const ChunkCut c = chunk_cut(p.batch, p.max_q, p.max_kv, p.hq, p.hkv, true);
   const ChunkWs ws = chunk_ws(c, D, workspace);
-  const int64_t blocks = c.blocks ? c.blocks : (int64_t)p.batch * p.hkv * c.tiles;
-  chunk_attn_kernel<D><<<dim3((unsigned)blocks), kW * 64, 0, stream>>>(p, c, ws, lg);
-  if (c.blocks) launch_chunk_merge<uint16_t, D>(p, c, ws, lg, stream);
+  chunk_attn_kernel<D><<<dim3((unsigned)c.blocks), kW * 64, 0, stream>>>(p, c, ws, lg);
+  launch_chunk_merge<uint16_t, D>(p, c, ws, lg, stream);
   return hipGetLastError();
 }
 
@@ -424,7 +440,7 @@ hipError_t launch_bf16(const ChunkAttn& p, void* workspace, hipStream_t stream) 
 bool chunk_attn_fits(int batch, int max_q, int max_kv, int hq, int hkv, bool bf16) {
   const ChunkCut c = chunk_cut(batch, max_q, max_kv, hq, hkv, bf16);
   const int64_t units = (int64_t)hkv * c.tiles;
-  return batch == 0 || units <= (c.blocks ? INT32_MAX : (1 << kGridLog2) - 1) / batch;
+  return batch == 0 || units <= INT32_MAX / batch;
 }
 
 size_t chunk_attn_workspace(int batch, int max_q, int max_kv, int hq, int hkv, int head_dim, bool bf16) {

@@ -265,9 +265,8 @@ hipError_t launch_t(const ChunkAttn& p, void* workspace, hipStream_t stream) {
   const int lg = log2_of(p.hq / p.hkv);
   const ChunkCut c = chunk_cut(p.batch, p.max_q, p.max_kv, p.hq, p.hkv, false);
   const ChunkWs ws = chunk_ws(c, D, workspace);
-  const int64_t blocks = c.blocks ? c.blocks : (int64_t)p.batch * p.hkv * c.tiles;
-  chunk_attn_f32_kernel<D><<<dim3((unsigned)blocks), kW * 64, 0, stream>>>(p, c, ws, lg);
-  if (c.blocks) launch_chunk_merge<float, D>(p, c, ws, lg, stream);
+  chunk_attn_f32_kernel<D><<<dim3((unsigned)c.blocks), kW * 64, 0, stream>>>(p, c, ws, lg);
+  launch_chunk_merge<float, D>(p, c, ws, lg, stream);
   return hipGetLastError();
 }
 

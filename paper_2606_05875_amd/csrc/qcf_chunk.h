@@ -19,7 +19,7 @@ constexpr int kChunkStep = 64;  // tokens per step
 
 struct ChunkCut {
   int vt_log2;  // query vectors per unit
-  int blocks;   // blocks that share the steps, 0: one block per unit
+  int blocks;   // blocks that share the steps
   int start;    // what beginning a unit counts as, in steps
   int tiles;    // units of the longest request per KV head
 };
@@ -80,17 +80,6 @@ struct ChunkCost {
 template <int NT, typename F>
 __device__ __forceinline__ void chunk_walk(const ChunkAttn& p, const ChunkCut& cut, const ChunkWs& ws, int lg,
                                            F&& unit) {
-  if (cut.blocks == 0) {
-    const int g = blockIdx.x % p.hkv, rest = blockIdx.x / p.hkv;
-    // the longest tiles first
-    const int tile = cut.tiles - 1 - rest % cut.tiles, b = rest / cut.tiles;
-    const TreeRequest q = tree_request_uni(p, b);
-    const ChunkCost c(p, q, lg, cut);
-    if (tile >= c.tiles) return;
-    const int s0 = (int)c.first(tile);
-    unit(b, q, g, tile, uni(s0), uni((int)c.last(tile) - s0), -1);
-    return;
-  }
   __shared__ int64_t sum_l[NT + 1];  // steps before each thread's requests
   __shared__ int64_t wave_l[NT / 64];
   const int tid = threadIdx.x, lane = tid & 63;
@@ -165,67 +154,66 @@ __device__ __forceinline__ void chunk_walk(const ChunkAttn& p, const ChunkCut& c
 
 namespace {
 
-// The partial results of the units that are cut, in the blocks' order: one wave per query vector of the unit that
-// a block begins.  Lane j first takes the maximum and sum of partial j, then 64 / (D / 4) partials at a time are
-// read and summed, whose sums meet at the end.  Bound: the partials' bytes.
-constexpr int kChunkMergeWaves = 4;
+// The partial results of the units that are cut, in the blocks' order.  A block takes 32 query vectors of the unit that
+// block x0 begins; a thread sums four columns of a vector, for several vectors at a time, so that many
+// partials are asked for at once.  Bound: the partials' bytes.
+constexpr int kMergeThreads = 256, kMergeVecs = 32;
 template <typename T, int D>
-__global__ __launch_bounds__(kChunkMergeWaves * 64) void chunk_merge_kernel(ChunkAttn p, ChunkCut cut, ChunkWs ws, int lg) {
-  constexpr int LPR = D / 4, RPW = 64 / LPR, U = 8;
-  const int l = threadIdx.x & 63, lc = l % LPR, lr = l / LPR;
+__global__ __launch_bounds__(kMergeThreads) void chunk_merge_kernel(ChunkAttn p, ChunkCut cut, ChunkWs ws, int lg) {
+  constexpr int LPR = D / 4, VP = kMergeThreads / LPR, U = kMergeVecs / VP;  // vectors side by side, and in turn
   const int x0 = blockIdx.x;
   const int4 c = ws.cut[x0];
   const int b = uni(c.x), g = uni(c.y), tile = uni(c.z), x1 = uni(c.w);
   if (b < 0) return;
   const TreeRequest q = tree_request_uni(p, b);
-  const int v = blockIdx.y * kChunkMergeWaves + uni((int)threadIdx.x >> 6);
-  const int64_t vec = ((int64_t)tile << cut.vt_log2) + v;
-  const int i = (int)(vec >> lg), h = (g << lg) + (int)(vec & ((1 << lg) - 1));
-  if (i >= q.rows) return;
-  auto slot = [&](int x) { return ((int64_t)(2 * x + (x == x0 ? 1 : 0)) << cut.vt_log2) + v; };
+  const int lc = threadIdx.x % LPR, v0 = blockIdx.y * kMergeVecs + threadIdx.x / LPR;
   const float4* part = reinterpret_cast<const float4*>(ws.o);
-  float mx = -INFINITY, lt = 0.f;
-  float4 a = make_float4(0.f, 0.f, 0.f, 0.f);
-  for (int xb = x0; xb <= x1; xb += 64) {
-    const int n = min(64, x1 - xb + 1);
-    const float2 ml = ws.ml[slot(min(xb + l, x1))];
-    const float m1 = l < n ? ml.x : -INFINITY, l1 = l < n ? ml.y : 0.f;
-    const float mn = fmaxf(mx, wave_max(m1));
-    const float f = __builtin_amdgcn_exp2f(gap(m1, mn)), fa = __builtin_amdgcn_exp2f(gap(mx, mn));
-    lt = lt * fa + wave_sum(l1 * f);
-    mx = mn;
-    a.x *= fa;
-    a.y *= fa;
-    a.z *= fa;
-    a.w *= fa;
-    for (int j0 = 0; j0 < n; j0 += U * RPW) {
-      float4 o[U];
+  float mx[U], lt[U];
+  float4 a[U];
 #pragma unroll
-      for (int k = 0; k < U; ++k) o[k] = part[slot(xb + min(j0 + k * RPW + lr, n - 1)) * LPR + lc];
+  for (int k = 0; k < U; ++k) {
+    mx[k] = -INFINITY;
+    lt[k] = 0.f;
+    a[k] = make_float4(0.f, 0.f, 0.f, 0.f);
+  }
+  for (int x = x0; x <= x1; x += 2) {
+    float2 ml[2][U];
+    float4 o[2][U];
+#pragma unroll
+    for (int j = 0; j < 2; ++j)
 #pragma unroll
       for (int k = 0; k < U; ++k) {
-        const int j = j0 + k * RPW + lr;
-        const float fo = __shfl(f, min(j, 63), 64);
-        if (j >= n) continue;
-        a.x = fmaf(o[k].x, fo, a.x);
-        a.y = fmaf(o[k].y, fo, a.y);
-        a.z = fmaf(o[k].z, fo, a.z);
-        a.w = fmaf(o[k].w, fo, a.w);
+        const int y = min(x + j, x1);
+        const int64_t at = ((int64_t)(2 * y + (y == x0 ? 1 : 0)) << cut.vt_log2) + v0 + k * VP;
+        ml[j][k] = ws.ml[at];
+        o[j][k] = part[at * LPR + lc];
+      }
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+      if (x + j > x1) break;
+#pragma unroll
+      for (int k = 0; k < U; ++k) {
+        const float mn = fmaxf(mx[k], ml[j][k].x);
+        const float fa = __builtin_amdgcn_exp2f(gap(mx[k], mn)), fo = __builtin_amdgcn_exp2f(gap(ml[j][k].x, mn));
+        mx[k] = mn;
+        lt[k] = fmaf(lt[k], fa, ml[j][k].y * fo);
+        a[k].x = fmaf(a[k].x, fa, o[j][k].x * fo);
+        a[k].y = fmaf(a[k].y, fa, o[j][k].y * fo);
+        a[k].z = fmaf(a[k].z, fa, o[j][k].z * fo);
+        a[k].w = fmaf(a[k].w, fa, o[j][k].w * fo);
       }
     }
   }
 #pragma unroll
-  for (int m = LPR; m < 64; m <<= 1) {
-    a.x += __shfl_xor(a.x, m, 64);
-    a.y += __shfl_xor(a.y, m, 64);
-    a.z += __shfl_xor(a.z, m, 64);
-    a.w += __shfl_xor(a.w, m, 64);
+  for (int k = 0; k < U; ++k) {
+    const int64_t vec = ((int64_t)tile << cut.vt_log2) + v0 + k * VP;
+    const int i = (int)(vec >> lg), h = (g << lg) + (int)(vec & ((1 << lg) - 1));
+    if (i >= q.rows) continue;
+    const float inv = row_scale(mx[k], lt[k]);
+    const int64_t at = (q.r0 + i) * p.hq + h;
+    store4(static_cast<T*>(p.out) + at * D + 4 * lc, make_float4(a[k].x * inv, a[k].y * inv, a[k].z * inv, a[k].w * inv));
+    if (p.lse && lc == 0) p.lse[at] = row_lse(mx[k], lt[k]);
   }
-  const float inv = row_scale(mx, lt);
-  const int64_t at = (q.r0 + i) * p.hq + h;
-  if (lr == 0)
-    store4(static_cast<T*>(p.out) + at * D + 4 * lc, make_float4(a.x * inv, a.y * inv, a.z * inv, a.w * inv));
-  if (p.lse && l == 0) p.lse[at] = row_lse(mx, lt);
 }
 
 // How a call is cut, from its bounds (lengths are on the device): tiles of 128 vectors (float32: 32), as many
@@ -247,7 +235,6 @@ struct ChunkWsLayout {
 inline ChunkWsLayout chunk_ws_layout(const ChunkCut& c, int d) {
   const auto up = [](size_t x) { return (x + 255) / 256 * 256; };
   ChunkWsLayout w{};
-  if (c.blocks == 0) return w;
   w.ml = up((size_t)c.blocks * sizeof(int4));
   w.o = w.ml + up(((size_t)2 * c.blocks << c.vt_log2) * 8);
   w.total = w.o + up(((size_t)2 * c.blocks << c.vt_log2) * d * 4);
@@ -263,7 +250,7 @@ inline ChunkWs chunk_ws(const ChunkCut& c, int d, void* workspace) {
 
 template <typename T, int D>
 inline void launch_chunk_merge(const ChunkAttn& p, const ChunkCut& c, const ChunkWs& ws, int lg, hipStream_t stream) {
-  chunk_merge_kernel<T, D><<<dim3((unsigned)c.blocks, (1u << c.vt_log2) / kChunkMergeWaves), kChunkMergeWaves * 64, 0, stream>>>(p, c, ws, lg);
+  chunk_merge_kernel<T, D><<<dim3((unsigned)c.blocks, (1u << c.vt_log2) / kMergeVecs), kMergeThreads, 0, stream>>>(p, c, ws, lg);
 }
 
 }  // namespace
