@@ -98,8 +98,8 @@ qcf_status qcf_chunk_attn(void* out, float* lse, const void* q, int64_t n_rows,
  * request's first tokens 0 .. prompt_len[b] - 1 were said as well, outside the answer.
  * With T = 0 the probability is 1 for the largest z (the lowest such token) and 0 elsewhere.  A row without a z
  * above -infinity gives zeros (qcf_verify_drafts: token -1); a NaN z or one of +infinity makes a
- * row of probabilities NaN (T = 0: a NaN z is passed over).  z is formed in float32 in this order, z / T
- * as z times the float32 reciprocal of T, sums are float32.
+ * row of probabilities NaN (T = 0: a NaN z is passed over).  Everything is float32: the quotient by the repetition is the
+ * product with its reciprocal, the exponential of z / T 2 to the power of z log2(e) / T, the quotient rounded once.
  *   out        [n_rows, vocab], rows out_stride elements apart, of type out_dtype; may be the logits
  *              themselves (same type and stride).  Rows at and behind cu_rows[batch] are neither read nor written
  *   logits     [n_rows, vocab], rows logits_stride elements apart (any stride >= vocab), of type dtype.
@@ -204,15 +204,20 @@ qcf_status qcf_copy_pages(void* const* pools, int n_pools, int64_t n_slots, int6
  *                same (lengths alone differ)
  *   held_before, held_after  int32 [batch] (negative ones count as 0, those beyond max_pages as that)
  *   free_pages   int32 [n_free], in and out; free_head, free_head_out int32 [1], different ones
+ *   workspace    >= qcf_page_release_workspace_size(...) bytes (may be 0), 256-byte aligned: marks of
+ *                pages for large tables.  No initialisation; calls that overlap in time need separate
+ *                ones.  The size covers every call whose three values do not exceed those given
  * Entries outside [0, n_pages) are no pages.
- * Errors: null pointers, sizes, n_pages beyond int32, free_head_out that is free_head.
+ * Errors: null pointers, sizes, n_pages beyond int32, free_head_out that is free_head, 2^22 pieces of 1024
+ * entries and more (UNSUPPORTED), workspace.
  */
+size_t qcf_page_release_workspace_size(int batch, int max_pages, int64_t n_pages);
 qcf_status qcf_page_release(const int32_t* table_before, int64_t before_stride,
                             const int32_t* held_before, const int32_t* table_after,
                             int64_t after_stride, const int32_t* held_after, int max_pages,
                             int batch, int32_t* free_pages, int64_t n_free,
                             const int32_t* free_head, int32_t* free_head_out, int64_t n_pages,
-                            hipStream_t stream);
+                            void* workspace, size_t workspace_bytes, hipStream_t stream);
 
 #ifdef __cplusplus
 }

@@ -193,15 +193,22 @@ qcf_status qcf_copy_pages(void* const* pools, int n_pools, int64_t n_slots, int6
   return hip_status(qcf::launch_copy_pages(p, stream));
 }
 
+size_t qcf_page_release_workspace_size(int batch, int max_pages, int64_t n_pages) {
+  if (batch <= 0 || max_pages <= 0 || n_pages <= 0 || n_pages > INT32_MAX) return 0;
+  return qcf::page_release_workspace(batch, max_pages, n_pages);
+}
+
 qcf_status qcf_page_release(const int32_t* table_before, int64_t before_stride,
                             const int32_t* held_before, const int32_t* table_after,
                             int64_t after_stride, const int32_t* held_after, int max_pages,
                             int batch, int32_t* free_pages, int64_t n_free,
                             const int32_t* free_head, int32_t* free_head_out, int64_t n_pages,
-                            hipStream_t stream) {
+                            void* workspace, size_t workspace_bytes, hipStream_t stream) {
   if (batch < 0 || max_pages < 0 || before_stride < max_pages || after_stride < max_pages || n_free < 0 ||
       n_free > INT32_MAX || n_pages < 0 || n_pages > INT32_MAX)
     return QCF_ERR_INVALID_ARG;
+  // (a block per 1024 entries of a row of either table)
+  if (batch >= 1 << 22 || (int64_t)batch * (((int64_t)max_pages + 1023) / 1024) >= 1 << 22) return QCF_ERR_UNSUPPORTED;
   const bool none = batch == 0, no_table = none || max_pages == 0;
   if (!index_ok(table_before, no_table) || !index_ok(table_after, no_table) || !index_ok(held_before, none) ||
       !index_ok(held_after, none) || !index_ok(free_pages, n_free == 0) || !index_ok(free_head, false) ||
@@ -210,9 +217,11 @@ qcf_status qcf_page_release(const int32_t* table_before, int64_t before_stride,
   const void* in[] = {table_before, table_after, held_before, held_after, free_head};
   for (const void* x : in)
     if (x && (x == free_head_out || x == free_pages)) return QCF_ERR_INVALID_ARG;
+  const size_t need = qcf_page_release_workspace_size(batch, max_pages, n_pages);
+  if (workspace_bytes < need || (need > 0 && (!workspace || !aligned256(workspace)))) return QCF_ERR_WORKSPACE;
   const qcf::PageRelease p{table_before, before_stride, held_before, table_after, after_stride, held_after, max_pages,
                            batch, free_pages, n_free, free_head, free_head_out, n_pages};
-  return hip_status(qcf::launch_page_release(p, stream));
+  return hip_status(qcf::launch_page_release(p, workspace, stream));
 }
 
 }  // extern "C"

@@ -16,126 +16,129 @@ constexpr int kThreads = 256;
 constexpr int kAhead = 3;    // units of a thread that are asked for before the angles are formed
 constexpr int kMaxRows = 8;  // rows of a block
 
-// 2^rows_log2 rows per block, for rows of few units
-template <typename T, int D, bool kInter>
-__global__ __launch_bounds__(kThreads) void norm_rope_store_kernel(NormRopeStore p, int rows_log2) {
+// 2^rows_log2 rows per block (kMulti: more than one, for rows of few units)
+template <typename T, int D, bool kInter, bool kMulti>
+__global__ __launch_bounds__(kThreads, 4) void norm_rope_store_kernel(NormRopeStore p, int rows_log2) {
   constexpr int VEC = Vec16<T>::N;
   constexpr int UPH = D / (2 * VEC);  // units per head
-  __shared__ float2 cs[kMaxRows * (D / 2)];
-  const int64_t r0 = ((int64_t)blockIdx.y << kGridLog2 | blockIdx.x) << rows_log2;
+  static_assert(kThreads % UPH == 0, "a thread's units are the same part of their heads");
+  __shared__ float2 cs[(kMulti ? kMaxRows : 1) * (D / 2)];
+  const int64_t block = (int64_t)blockIdx.y << kGridLog2 | blockIdx.x;
+  const int64_t r0 = kMulti ? block << rows_log2 : block;
   if (r0 >= p.n_rows) return;
-  const int rows = (int)min((int64_t)1 << rows_log2, p.n_rows - r0);
+  const int rows = kMulti ? (int)min((int64_t)1 << rows_log2, p.n_rows - r0) : 1;
   const int half = p.rotary_dim / 2;
   const int nq = p.q_out ? p.hq : 0, nkv = p.k_cache ? p.hkv : 0;
   const int per_row = (nq + 2 * nkv) * UPH, units = per_row * rows;
+  // this thread's part of every head: 16-byte vectors at ia and ib (values: va and vb)
+  const int c = threadIdx.x % UPH;
+  const bool turned = p.positions != nullptr && c * 2 * VEC < p.rotary_dim;
+  const int va = c * 2 * VEC, vb = va + VEC;
+  const int ia = turned && !kInter ? c * VEC : va, ib = turned && !kInter ? ia + half : vb;
+  auto row_of = [&](int u) { return kMulti ? u / per_row : 0; };
+  auto head_of = [&](int u, int i) { return (u - i * per_row) / UPH; };
   struct Unit {
-    uint4 a, b, wa, wb;
-    T* dst;  // NULL: nothing is stored
-    int ia, ib, cs0;
-    bool norm, turn;
+    uint4 a, b;
   };
   auto load = [&](int u) {
-    Unit x;
-    const int i = rows_log2 ? u / per_row : 0;
-    const int v = u - i * per_row, h = v / UPH, c = v % UPH;
-    const int64_t r = r0 + i;
-    const int64_t from = p.src_idx ? (int64_t)p.src_idx[r] : r;
-    const bool there = from >= 0 && from < p.n_src_rows;
-    const int64_t s = there ? from : 0;
-    const T *src, *w = nullptr;
-    x.norm = true;
-    if (h < nq) {
-      src = static_cast<const T*>(p.q_new) + s * p.q_stride + h * D;
-      x.dst = static_cast<T*>(p.q_out) + (r * p.hq + h) * D;
-      if (p.q_weight) w = static_cast<const T*>(p.q_weight) + h * p.q_weight_stride;
-    } else {
-      const int64_t slot = p.slots[r];
-      const bool is_k = h < nq + nkv;
-      const int g = h - nq - (is_k ? 0 : nkv);
-      src = static_cast<const T*>(is_k ? p.k_new : p.v_new) + s * p.new_stride + g * D;
-      x.dst = slot >= 0 && slot < p.n_slots ? static_cast<T*>(is_k ? p.k_cache : p.v_cache) + slot * p.cache_stride + g * D
-                                            : nullptr;
-      if (is_k && p.k_weight) w = static_cast<const T*>(p.k_weight) + g * p.k_weight_stride;
-      x.norm = is_k;
-    }
-    if (!there) x.dst = nullptr;
-    x.turn = x.norm && p.positions != nullptr && c * 2 * VEC < p.rotary_dim;
-    x.cs0 = i * (D / 2);
-    x.ia = x.turn && !kInter ? c * VEC : c * 2 * VEC;
-    x.ib = x.turn && !kInter ? x.ia + half : x.ia + VEC;
-    x.a = ld16(src + x.ia);
-    x.b = ld16(src + x.ib);
+    const int i = row_of(u), h = head_of(u, i);
+    const int64_t from = p.src_idx ? (int64_t)p.src_idx[r0 + i] : r0 + i;
+    const int64_t s = from >= 0 && from < p.n_src_rows ? from : 0;
+    const T* src = h < nq         ? static_cast<const T*>(p.q_new) + s * p.q_stride + h * D
+                   : h < nq + nkv ? static_cast<const T*>(p.k_new) + s * p.new_stride + (h - nq) * D
+                                  : static_cast<const T*>(p.v_new) + s * p.new_stride + (h - nq - nkv) * D;
+    const bool v = h >= nq + nkv;
+    return Unit{ld16(src + (v ? va : ia)), ld16(src + (v ? vb : ib))};
+  };
+  // weights that all heads share are read once
+  struct Weight {
+    uint4 a, b;
+  };
+  auto weight = [&](const void* w, int64_t stride, int h) {
     if (w) {
-      x.wa = ld16(w + x.ia);
-      x.wb = ld16(w + x.ib);
-    } else {
-      float one[VEC];
-#pragma unroll
-      for (int e = 0; e < VEC; ++e) one[e] = 1.f;
-      x.wa = x.wb = Vec16<T>::pack(one);
+      const T* x = static_cast<const T*>(w) + h * stride;
+      return Weight{ld16(x + ia), ld16(x + ib)};
     }
-    return x;
+    float one[VEC];
+#pragma unroll
+    for (int e = 0; e < VEC; ++e) one[e] = 1.f;
+    return Weight{Vec16<T>::pack(one), Vec16<T>::pack(one)};
   };
   // (all of a head's lanes come here together)
-  auto finish = [&](const Unit& u) {
-    uint4 va = u.a, vb = u.b;
+  auto finish = [&](int u, const Unit& unit, const Weight& qw, const Weight& kw) {
+    const int i = row_of(u), h = head_of(u, i);
+    const int64_t r = r0 + i;
+    const bool is_q = h < nq, is_v = h >= nq + nkv;
     float x[VEC], y[VEC];
-    Vec16<T>::unpack(va, x);
-    Vec16<T>::unpack(vb, y);
+    Vec16<T>::unpack(unit.a, x);
+    Vec16<T>::unpack(unit.b, y);
     float sum = 0.f;
 #pragma unroll
     for (int e = 0; e < VEC; ++e) sum = fmaf(x[e], x[e], fmaf(y[e], y[e], sum));
 #pragma unroll
     for (int o = UPH / 2; o > 0; o >>= 1) sum += __shfl_xor(sum, o, 64);
-    if (u.norm) {
+    Unit out = unit;
+    if (!is_v) {
       const float scale = 1.f / sqrtf(sum * (1.f / D) + p.eps);
+      Weight w = is_q ? qw : kw;
+      if (is_q && p.q_weight_stride) w = weight(p.q_weight, p.q_weight_stride, h);
+      if (!is_q && p.k_weight_stride) w = weight(p.k_weight, p.k_weight_stride, h - nq);
       float wx[VEC], wy[VEC];
-      Vec16<T>::unpack(u.wa, wx);
-      Vec16<T>::unpack(u.wb, wy);
+      Vec16<T>::unpack(w.a, wx);
+      Vec16<T>::unpack(w.b, wy);
 #pragma unroll
       for (int e = 0; e < VEC; ++e) {
         x[e] = x[e] * scale * wx[e];
         y[e] = y[e] * scale * wy[e];
       }
-      if (u.turn) {
+      if (turned) {
         float xo[VEC], yo[VEC];
-        const float2* c = cs + u.cs0;
+        const float2* t = cs + i * (D / 2);
         if (kInter) {
 #pragma unroll
           for (int e = 0; e < VEC; e += 2) {
-            rope_pair(x[e], x[e + 1], c[(u.ia + e) / 2], xo[e], xo[e + 1]);
-            rope_pair(y[e], y[e + 1], c[(u.ib + e) / 2], yo[e], yo[e + 1]);
+            rope_pair(x[e], x[e + 1], t[(ia + e) / 2], xo[e], xo[e + 1]);
+            rope_pair(y[e], y[e + 1], t[(ib + e) / 2], yo[e], yo[e + 1]);
           }
         } else {
 #pragma unroll
-          for (int e = 0; e < VEC; ++e) rope_pair(x[e], y[e], c[u.ia + e], xo[e], yo[e]);
+          for (int e = 0; e < VEC; ++e) rope_pair(x[e], y[e], t[ia + e], xo[e], yo[e]);
         }
-        va = Vec16<T>::pack(xo);
-        vb = Vec16<T>::pack(yo);
+        out = Unit{Vec16<T>::pack(xo), Vec16<T>::pack(yo)};
       } else {
-        va = Vec16<T>::pack(x);
-        vb = Vec16<T>::pack(y);
+        out = Unit{Vec16<T>::pack(x), Vec16<T>::pack(y)};
       }
     }
-    if (u.dst) {
-      st16(u.dst + u.ia, va);
-      st16(u.dst + u.ib, vb);
+    const int64_t from = p.src_idx ? (int64_t)p.src_idx[r] : r;
+    T* dst = nullptr;
+    if (is_q) {
+      dst = static_cast<T*>(p.q_out) + (r * p.hq + h) * D;
+    } else {
+      const int64_t slot = p.slots[r];
+      if (slot >= 0 && slot < p.n_slots)
+        dst = static_cast<T*>(is_v ? p.v_cache : p.k_cache) + slot * p.cache_stride + (is_v ? h - nq - nkv : h - nq) * D;
+    }
+    if (dst && from >= 0 && from < p.n_src_rows) {
+      st16(dst + (is_v ? va : ia), out.a);
+      st16(dst + (is_v ? vb : ib), out.b);
     }
   };
   Unit x[kAhead];
 #pragma unroll
   for (int k = 0; k < kAhead; ++k)
-    if (k * kThreads < units) x[k] = load(min((int)threadIdx.x + k * kThreads, units - 1));
+    if (k * kThreads < units) x[k] = load(min((int)threadIdx.x + k * kThreads, units - UPH + c));
   if (p.positions)
     for (int t = threadIdx.x; t < rows * half; t += kThreads) {
-      const int i = rows_log2 ? t / half : 0, j = t - i * half;
+      const int i = kMulti ? t / half : 0, j = t - i * half;
       cs[i * (D / 2) + j] = angle_cs<true, true>((double)p.positions[r0 + i] * p.freq[j], (double)p.magnitude);
     }
+  const Weight qw = weight(p.q_weight_stride ? nullptr : p.q_weight, 0, 0);
+  const Weight kw = weight(p.k_weight_stride ? nullptr : p.k_weight, 0, 0);
   __syncthreads();
 #pragma unroll
   for (int k = 0; k < kAhead; ++k)
-    if ((int)threadIdx.x + k * kThreads < units) finish(x[k]);
-  for (int u = threadIdx.x + kAhead * kThreads; u < units; u += kThreads) finish(load(u));
+    if ((int)threadIdx.x + k * kThreads < units) finish(threadIdx.x + k * kThreads, x[k], qw, kw);
+  for (int u = threadIdx.x + kAhead * kThreads; u < units; u += kThreads) finish(u, load(u), qw, kw);
 }
 
 template <typename T, int D>
@@ -144,10 +147,13 @@ hipError_t launch_t(const NormRopeStore& p, bool interleaved, hipStream_t stream
   int lg = 0;
   while ((2 << lg) <= kMaxRows && ((int64_t)units << (lg + 1)) <= kThreads && (p.n_rows >> lg) > 512) ++lg;
   const dim3 grid = grid_of(((p.n_rows - 1) >> lg) + 1);
-  if (interleaved)
-    norm_rope_store_kernel<T, D, true><<<grid, kThreads, 0, stream>>>(p, lg);
-  else
-    norm_rope_store_kernel<T, D, false><<<grid, kThreads, 0, stream>>>(p, lg);
+  if (lg > 0) {
+    if (interleaved) norm_rope_store_kernel<T, D, true, true><<<grid, kThreads, 0, stream>>>(p, lg);
+    else norm_rope_store_kernel<T, D, false, true><<<grid, kThreads, 0, stream>>>(p, lg);
+  } else {
+    if (interleaved) norm_rope_store_kernel<T, D, true, false><<<grid, kThreads, 0, stream>>>(p, lg);
+    else norm_rope_store_kernel<T, D, false, false><<<grid, kThreads, 0, stream>>>(p, lg);
+  }
   return hipGetLastError();
 }
 

@@ -3,6 +3,8 @@
 // Pages have no holders' counts: a page is held by whoever's table names it, and what nobody's names any
 // more is found by marking the pages of the tables before and after a change in two bit sets.  There is
 // nothing to keep in step, and no result hangs on the order of blocks.
+#include <algorithm>
+
 #include "qcf_device.h"
 #include "qcf_turns_launch.h"
 
@@ -10,6 +12,7 @@ namespace qcf {
 namespace {
 
 constexpr int kThreads = 256;
+constexpr int64_t kReleaseSmall = 8192;  // entries of a table
 
 // ---------------------------------------------------------------------------
 // fork: one block per request, which counts the pages that the requests before it take on its own (three
@@ -127,16 +130,27 @@ __global__ __launch_bounds__(kThreads) void copy_pages_kernel(CopyPages p, int r
 }
 
 // ---------------------------------------------------------------------------
-// release: one block, which marks the pages of both tables in LDS (two bits per page; larger pools in
-// several goes) and writes those that are only in the first.  Bound: latency, and for large tables what one
-// compute unit reads.
+// release.  Row i < batch is a request's row of the table before, row batch + i of the one after.
 // ---------------------------------------------------------------------------
+struct ReleaseRow {
+  const int32_t* pages;
+  int held;
+};
+__device__ __forceinline__ ReleaseRow release_row(const PageRelease& p, int i) {
+  const bool after = i >= p.batch;
+  const int b = after ? i - p.batch : i;
+  const int held = after ? p.held_after[b] : p.held_before[b];
+  return ReleaseRow{after ? p.after + b * p.after_stride : p.before + b * p.before_stride, min(max(held, 0), p.max_pages)};
+}
+
+// Small tables: one block marks the pages of both tables in LDS (two bits per page; larger pools in several goes)
+// and writes those that are only in the first.  Bound: latency.
 constexpr int kRelThreads = 1024;
 constexpr int kRelWords = 1 << 14;  // of 32 pages, per bit set
 
 __global__ __launch_bounds__(kRelThreads) void page_release_kernel(PageRelease p) {
   __shared__ uint32_t was_l[kRelWords], is_l[kRelWords];
-  __shared__ int32_t first_l[kRelThreads + 1];  // 64-entry pieces before each request of a go
+  __shared__ int32_t first_l[kRelThreads];  // 64-entry pieces before each row of a go
   __shared__ int wave_l[kRelThreads / 64];
   const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
   constexpr int kWaves = kRelThreads / 64;
@@ -155,54 +169,15 @@ __global__ __launch_bounds__(kRelThreads) void page_release_kernel(PageRelease p
     __syncthreads();
     if (lane == 63) wave_l[w] = sum;
     __syncthreads();
+    const int part = lane < kWaves ? wave_l[lane] : 0;
     all = 0;
+#pragma unroll
     for (int i = 0; i < kWaves; ++i) {
-      if (i < w) sum += wave_l[i];
-      all += wave_l[i];
+      const int x1 = __builtin_amdgcn_readlane(part, i);
+      if (i < w) sum += x1;
+      all += x1;
     }
     return sum;
-  };
-  // marks the pages p0 .. p0 + kPages - 1 of a table
-  auto mark = [&](const int32_t* table, int64_t stride, const int32_t* held, uint32_t* bits, int64_t p0) {
-    for (int b0 = 0; b0 < p.batch; b0 += kRelThreads) {
-      const int mine = b0 + tid < p.batch ? min(max(held[b0 + tid], 0), p.max_pages) : 0;
-      int all;
-      const int pieces = (mine + 63) >> 6;
-      const int sum = scan(pieces, all);
-      first_l[tid] = sum - pieces;
-      if (tid == 0) first_l[kRelThreads] = all;
-      __syncthreads();
-      // a wave takes 64 pieces at a time; each lane looks up one of them
-      for (int i0 = w * 64; i0 < all; i0 += kWaves * 64) {
-        const int mine_i = min(i0 + lane, all - 1);
-        int lo = 0, hi = kRelThreads;
-        while (hi - lo > 1) {
-          const int mid = (lo + hi) >> 1;
-          if (first_l[mid] <= mine_i) lo = mid; else hi = mid;
-        }
-        const int64_t row = (int64_t)(b0 + lo) * stride;
-        const int col = (mine_i - first_l[lo]) * 64;
-        const int n_row = min(max(held[b0 + lo], 0), p.max_pages);
-        const int n = min(64, all - i0);
-        constexpr int U = 8;
-        for (int k0 = 0; k0 < n; k0 += U) {
-          int x[U];
-#pragma unroll
-          for (int k = 0; k < U; ++k) {
-            const int from = min(k0 + k, n - 1);
-            const int64_t r = __shfl(row, from, 64);
-            const int c = __shfl(col, from, 64), end = __shfl(n_row, from, 64);
-            x[k] = table[r + min(c + lane, end - 1)];
-          }
-#pragma unroll
-          for (int k = 0; k < U; ++k) {
-            const int64_t at = (int64_t)x[k] - p0;
-            if (x[k] >= 0 && x[k] < p.n_pages && at >= 0 && at < kPages) atomicOr(&bits[at >> 5], 1u << (at & 31));
-          }
-        }
-      }
-      __syncthreads();
-    }
   };
   // marks go g's pages of both tables; own: how many of this thread's are released, before: of the threads' before
   // it; returns the number of all
@@ -212,13 +187,50 @@ __global__ __launch_bounds__(kRelThreads) void page_release_kernel(PageRelease p
     words = (int)((min(p.n_pages - p0, kPages) + 31) >> 5);
     __syncthreads();
     for (int i = tid; i < words; i += kRelThreads) was_l[i] = is_l[i] = 0;
-    __syncthreads();
-    mark(p.before, p.before_stride, p.held_before, was_l, p0);
-    mark(p.after, p.after_stride, p.held_after, is_l, p0);
+    for (int i0 = 0; i0 < 2 * p.batch; i0 += kRelThreads) {
+      const int mine = i0 + tid < 2 * p.batch ? release_row(p, i0 + tid).held : 0;
+      int all;
+      const int pieces = (mine + 63) >> 6;
+      const int sum = scan(pieces, all);
+      first_l[tid] = sum - pieces;
+      __syncthreads();
+      // the waves share the pieces evenly; each lane looks up one of up to 64 at a time
+      const int to = (int)((int64_t)all * (w + 1) / kWaves);
+      for (int k0 = (int)((int64_t)all * w / kWaves); k0 < to; k0 += 64) {
+        const int piece = min(k0 + lane, to - 1);
+        int lo = 0, hi = kRelThreads;
+        while (hi - lo > 1) {
+          const int mid = (lo + hi) >> 1;
+          if (first_l[mid] <= piece) lo = mid; else hi = mid;
+        }
+        const ReleaseRow row = release_row(p, i0 + lo);
+        const int64_t from = reinterpret_cast<int64_t>(row.pages + (piece - first_l[lo]) * 64);
+        const int left = row.held - (piece - first_l[lo]) * 64;
+        const int which = i0 + lo >= p.batch ? 1 : 0, n = min(64, to - k0);
+        constexpr int U = 8;
+        for (int k = 0; k < n; k += U) {
+          int x[U], set[U];
+#pragma unroll
+          for (int u = 0; u < U; ++u) {
+            const int j = min(k + u, n - 1);
+            const int32_t* at = reinterpret_cast<const int32_t*>(__shfl(from, j, 64));
+            x[u] = at[min(lane, __shfl(left, j, 64) - 1)];
+            set[u] = __shfl(which, j, 64);
+          }
+#pragma unroll
+          for (int u = 0; u < U; ++u) {
+            const int64_t at = (int64_t)x[u] - p0;
+            if (x[u] >= 0 && x[u] < p.n_pages && at >= 0 && at < kPages)
+              atomicOr(&(set[u] ? is_l : was_l)[at >> 5], 1u << (at & 31));
+          }
+        }
+      }
+      __syncthreads();
+    }
     const int per = (words + kRelThreads - 1) / kRelThreads;
-    const int i0 = min(tid * per, words), i1 = min(i0 + per, words);
+    const int w0 = min(tid * per, words), w1 = min(w0 + per, words);
     own = 0;
-    for (int i = i0; i < i1; ++i) own += __popc(was_l[i] & ~is_l[i]);
+    for (int i = w0; i < w1; ++i) own += __popc(was_l[i] & ~is_l[i]);
     int all;
     before = scan(own, all) - own;
     return all;
@@ -230,14 +242,100 @@ __global__ __launch_bounds__(kRelThreads) void page_release_kernel(PageRelease p
   for (int g = 0; g < goes; ++g) {
     const int all = goes > 1 ? go(g) : (int)n;  // (a single one's marks are still there)
     const int per = (words + kRelThreads - 1) / kRelThreads;
-    const int i0 = min(tid * per, words), i1 = min(i0 + per, words);
+    const int w0 = min(tid * per, words), w1 = min(w0 + per, words);
     int64_t at = put + before;
-    for (int i = i0; i < i1; ++i)
+    for (int i = w0; i < w1; ++i)
       for (uint32_t left = was_l[i] & ~is_l[i]; left; left &= left - 1, ++at)
         if (at >= 0) p.free_pages[at] = (int)(g * kPages + i * 32 + __builtin_ctz(left));
     put += all;
   }
 }
+
+// Large tables: a byte per page and table in the workspace, set to zero, marked by a block per 1024 entries of a row
+// (the same value from everywhere), and gone through by blocks of 16384 pages, each of which counts those before it.
+constexpr int kMarkEntries = 1024;
+
+__global__ __launch_bounds__(kThreads) void release_zero_kernel(uint4* marks, int64_t n) {
+  const int64_t i = (int64_t)blockIdx.x * kThreads + threadIdx.x;
+  if (i < n) marks[i] = make_uint4(0, 0, 0, 0);
+}
+
+__global__ __launch_bounds__(kThreads) void release_mark_kernel(PageRelease p, uint8_t* marks, int64_t set_bytes, int pieces) {
+  const int i = blockIdx.x / pieces, c0 = (blockIdx.x - i * pieces) * kMarkEntries;
+  const ReleaseRow row = release_row(p, i);
+  if (c0 >= row.held) return;
+  uint8_t* set = marks + (i >= p.batch ? set_bytes : 0);
+  constexpr int U = kMarkEntries / kThreads;
+  int x[U];
+#pragma unroll
+  for (int u = 0; u < U; ++u) x[u] = row.pages[min(c0 + (int)threadIdx.x + u * kThreads, row.held - 1)];
+#pragma unroll
+  for (int u = 0; u < U; ++u)
+    if (x[u] >= 0 && x[u] < p.n_pages) set[x[u]] = 1;
+}
+
+__global__ __launch_bounds__(kRelThreads) void release_list_kernel(PageRelease p, const uint8_t* marks, int64_t set_bytes) {
+  __shared__ int sum_l[2][kRelThreads / 64];
+  const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
+  const uint4* was = reinterpret_cast<const uint4*>(marks);
+  const uint4* is = reinterpret_cast<const uint4*>(marks + set_bytes);
+  const int64_t n = set_bytes / 16, mine = (int64_t)blockIdx.x * kRelThreads + tid;
+  auto gone = [&](int64_t i) {  // bytes that are 1: released pages 16 i .. 16 i + 15
+    const uint4 a = was[i], b = is[i];
+    return make_uint4(a.x & ~b.x, a.y & ~b.y, a.z & ~b.z, a.w & ~b.w);
+  };
+  auto count = [](const uint4& x) { return __popc(x.x) + __popc(x.y) + __popc(x.z) + __popc(x.w); };
+  const int64_t head = min(max((int64_t)p.free_head[0], (int64_t)0), p.n_free);
+  const uint4 own = mine < n ? gone(mine) : make_uint4(0, 0, 0, 0);
+  // pages released in front of this block's, and all
+  int before = 0, all = 0;
+  constexpr int U = 4;
+  for (int64_t i0 = tid; i0 < n; i0 += kRelThreads * U) {
+    uint4 x[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) x[u] = gone(min(i0 + u * kRelThreads, n - 1));
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int64_t i = i0 + u * kRelThreads;
+      const int c = i < n ? count(x[u]) : 0;
+      all += c;
+      if (i < (int64_t)blockIdx.x * kRelThreads) before += c;
+    }
+  }
+  const int mine_n = count(own);
+  int sum = mine_n;  // of the wave's threads up to this one
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) {
+    const int y = __shfl_up(sum, o, 64);
+    if (lane >= o) sum += y;
+  }
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) {
+    before += __shfl_xor(before, o, 64);
+    all += __shfl_xor(all, o, 64);
+  }
+  // a wave's threads up to its last, behind what lies before the block
+  __shared__ int own_l[kRelThreads / 64];
+  if (lane == 63) own_l[w] = sum;
+  if (lane == 0) sum_l[0][w] = before, sum_l[1][w] = all;
+  __syncthreads();
+  before = all = 0;
+  for (int i = 0; i < kRelThreads / 64; ++i) {
+    before += sum_l[0][i] + (i < w ? own_l[i] : 0);
+    all += sum_l[1][i];
+  }
+  const int64_t put = head - all;
+  if (blockIdx.x == 0 && tid == 0) p.free_head_out[0] = (int)max(put, (int64_t)0);
+  int64_t at = put + before + sum - mine_n;
+  const uint32_t words[4] = {own.x, own.y, own.z, own.w};
+#pragma unroll
+  for (int k = 0; k < 4; ++k)
+    for (uint32_t left = words[k]; left; left &= left - 1, ++at)
+      if (at >= 0) p.free_pages[at] = (int)(16 * mine + 4 * k + (__builtin_ctz(left) >> 3));
+}
+
+// One block's time grows with the tables, three launches do not.
+inline bool release_small(const PageRelease& p) { return (int64_t)p.batch * p.max_pages <= kReleaseSmall; }
 
 }  // namespace
 
@@ -262,8 +360,24 @@ hipError_t launch_copy_pages(const CopyPages& p, hipStream_t stream) {
   return hipGetLastError();
 }
 
-hipError_t launch_page_release(const PageRelease& p, hipStream_t stream) {
-  page_release_kernel<<<dim3(1), kRelThreads, 0, stream>>>(p);
+size_t page_release_workspace(int batch, int max_pages, int64_t n_pages) {
+  if ((int64_t)batch * max_pages <= kReleaseSmall) return 0;
+  return (size_t)((n_pages + 255) / 256 * 256) * 2;
+}
+
+hipError_t launch_page_release(const PageRelease& p, void* ws, hipStream_t stream) {
+  if (release_small(p)) {
+    page_release_kernel<<<dim3(1), kRelThreads, 0, stream>>>(p);
+    return hipGetLastError();
+  }
+  const int64_t set_bytes = (p.n_pages + 255) / 256 * 256, vecs = set_bytes * 2 / 16;
+  uint8_t* marks = static_cast<uint8_t*>(ws);
+  const int pieces = (p.max_pages + kMarkEntries - 1) / kMarkEntries;
+  if (vecs > 0)
+    release_zero_kernel<<<dim3((unsigned)((vecs + kThreads - 1) / kThreads)), kThreads, 0, stream>>>(reinterpret_cast<uint4*>(marks), vecs);
+  release_mark_kernel<<<dim3((unsigned)((int64_t)2 * p.batch * pieces)), kThreads, 0, stream>>>(p, marks, set_bytes, pieces);
+  const int64_t blocks = std::max<int64_t>((set_bytes / 16 + kRelThreads - 1) / kRelThreads, 1);
+  release_list_kernel<<<dim3((unsigned)blocks), kRelThreads, 0, stream>>>(p, marks, set_bytes);
   return hipGetLastError();
 }
 

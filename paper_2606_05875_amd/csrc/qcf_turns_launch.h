@@ -86,6 +86,7 @@ struct PageRelease {
   int32_t* free_head_out;
   int64_t n_pages;
 };
-hipError_t launch_page_release(const PageRelease& p, hipStream_t stream);
+size_t page_release_workspace(int batch, int max_pages, int64_t n_pages);
+hipError_t launch_page_release(const PageRelease& p, void* ws, hipStream_t stream);
 
 }  // namespace qcf

@@ -1,12 +1,14 @@
 // Logits with penalties for what was said, biases and masks, as logits or as probabilities (qcf_shape_logits).
 //
 // A block takes a piece of one row.  How often each of the piece's tokens was said is counted in LDS from the
-// request's history and the drafted tokens that the row follows (32 bits per token: bit 0 said at all, the
-// count in the answer above it; whole numbers, so the order of the additions is of no account), and which
+// request's history and the drafted tokens that the row follows (32 bits per token: the count in the answer, and
+// whether the prompt has it; whole numbers, so the order of the additions is of no account), and which
 // entry of the bias list is a token's last beside it.  Probabilities take two launches: a piece's maximum and its sum
 // of exponentials, then the row's from all of them (in the pieces' order) and the values; a row
 // of one piece takes one.  z is formed the same way both times, so nothing is stored in between.
 // Bound: HBM and the scan of the history by every block.
+#include <algorithm>
+
 #include "qcf_device.h"
 #include "qcf_turns_launch.h"
 
@@ -14,295 +16,366 @@ namespace qcf {
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int kVec = 8;                              // tokens of a thread at a time
-constexpr int kVecs = 4;                             // times
-constexpr int kPiece = kThreads * kVec * kVecs;      // tokens of a block
+constexpr int kVec = 8;  // tokens of a thread at a time
 constexpr int kWaves = kThreads / 64;
+// Tokens of a block's piece: 32 KB of LDS for what is looked up of them
+constexpr int piece_of(bool bias) { return bias ? 4096 : 8192; }
+constexpr int64_t kShapeBlocks = 2048;
+
+constexpr uint32_t kSaid = 1u << 31;  // of a token's count: it was said in the prompt
 
 enum Mode { kLogits, kStats, kWrite, kWhole };
 
+// Of a part of a row.  With c = log2(e) / T in float32, exp(z / T) is exp2(z c) but for c's rounding, and exp2(z c - m) with
+// one fused multiply-add keeps that product exact, so that a token near the maximum is hardly off at all.
 struct Stat {
-  float m, s;  // maximum, sum of exp(x - m)
+  float m, s;  // the maximum times c, sum of exp2(z c - m); T = 0: the maximum
   int at;      // lowest token with the maximum (T = 0)
   int pad;
 };
 
-// exp(y), y <= 0 (or NaN): the product's rounding error goes into the result, which is off by 2^-23 or so for any
-// y where 2^(y log2 e) alone is off by |y| 2^-24
-__device__ __forceinline__ float exp_of(float y) {
-  y = y < -200.f ? -200.f : y;  // (0 already)
-  const float t = y * kLog2e;
-  const float e = __builtin_amdgcn_exp2f(t);
-  return fmaf(e, fmaf(y, kLog2e, -t) * kLn2, e);
+__device__ __forceinline__ float finite(float m) { return m == -INFINITY ? 0.f : m; }
+
+// two parts of a row, the first's tokens before the second's
+__device__ __forceinline__ Stat both(const Stat& a, const Stat& b, bool cold) {
+  Stat r{fmaxf(a.m, b.m), 0.f, INT32_MAX, 0};
+  if (cold) {
+    r.at = min(a.m == r.m ? a.at : INT32_MAX, b.m == r.m ? b.at : INT32_MAX);
+  } else {
+    const float ref = finite(r.m);
+    r.s = a.s * __builtin_amdgcn_exp2f(a.m - ref) + b.s * __builtin_amdgcn_exp2f(b.m - ref);
+  }
+  return r;
 }
 
-template <typename T>
-__device__ __forceinline__ void load8(const T* p, float (&x)[kVec]) {  // (aligned as its elements are)
-  T v[kVec];
-  __builtin_memcpy(v, p, sizeof v);
-#pragma unroll
-  for (int e = 0; e < kVec; ++e) x[e] = sizeof(T) == 2 ? bf2f((uint16_t)v[e]) : (float)v[e];
+// Between the phases of a row only LDS is handed on: loads of the next ones stay in flight
+__device__ __forceinline__ void meet() {
+  asm volatile("" ::: "memory");
+  __builtin_amdgcn_s_waitcnt(0xc07f);  // lgkmcnt(0)
+  __builtin_amdgcn_s_barrier();
+  asm volatile("" ::: "memory");
 }
-__device__ __forceinline__ void load8(const float* p, float (&x)[kVec]) { __builtin_memcpy(x, p, sizeof x); }
-__device__ __forceinline__ float as_float(uint16_t x) { return bf2f(x); }
-__device__ __forceinline__ float as_float(float x) { return x; }
+
 __device__ __forceinline__ void put(uint16_t* p, float x) { *p = f2bf(x); }
 __device__ __forceinline__ void put(float* p, float x) { *p = x; }
-__device__ __forceinline__ void store8(uint16_t* p, const float (&x)[kVec]) {
-  const uint4 v = Vec16<uint16_t>::pack(x);
-  __builtin_memcpy(p, &v, sizeof v);
-}
-__device__ __forceinline__ void store8(float* p, const float (&x)[kVec]) { __builtin_memcpy(p, x, sizeof x); }
 
+// 16 bytes at an address that is aligned as its elements are
+typedef uint32_t v4_at2 __attribute__((ext_vector_type(4), aligned(2)));
+typedef uint32_t v4_at4 __attribute__((ext_vector_type(4), aligned(4)));
+template <typename T> struct Loose { typedef v4_at4 V; };
+template <> struct Loose<uint16_t> { typedef v4_at2 V; };
+template <typename T>
+__device__ __forceinline__ uint4 load16(const T* p) {
+  const typename Loose<T>::V x = *reinterpret_cast<const typename Loose<T>::V*>(p);
+  return make_uint4(x[0], x[1], x[2], x[3]);
+}
+template <typename T>
+__device__ __forceinline__ void store16(T* p, const uint4& x) {
+  *reinterpret_cast<typename Loose<T>::V*>(p) = typename Loose<T>::V{x.x, x.y, x.z, x.w};
+}
+template <typename T>
+__device__ __forceinline__ void store8(T* p, const float (&x)[kVec]) {
+#pragma unroll
+  for (int i = 0; i < kVec; i += Vec16<T>::N) store16(p + i, Vec16<T>::pack(x + i));
+}
+
+// One piece of `per` consecutive rows.  A row's loads all go out before anything waits.
 template <typename In, typename Out, int kMode, bool kBias>
-__global__ __launch_bounds__(kThreads) void shape_kernel(ShapeLogits p, Stat* stats, int pieces) {
+__global__ __launch_bounds__(kThreads, 4) void shape_kernel(ShapeLogits p, Stat* stats, int pieces, int per) {
+  constexpr int kPiece = piece_of(kBias), kVecs = kPiece / (kThreads * kVec);
   __shared__ __attribute__((aligned(16))) uint32_t said_l[kPiece];
   __shared__ __attribute__((aligned(16))) uint32_t bias_l[kBias ? kPiece : 4];
-  __shared__ float red_l[kWaves];
-  __shared__ int redi_l[kWaves];
+  __shared__ Stat red_l[kWaves];
   const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
   const int64_t block = (int64_t)blockIdx.y << kGridLog2 | blockIdx.x;
-  const int64_t r = block / pieces;
-  if (r >= p.n_rows) return;
-  const int piece = (int)(block - r * pieces), p0 = piece * kPiece;
-  auto sum_i = [&](int x) {
-#pragma unroll
-    for (int o = 32; o > 0; o >>= 1) x += __shfl_xor(x, o, 64);
-    __syncthreads();
-    if (lane == 0) redi_l[w] = x;
-    __syncthreads();
-    x = 0;
-#pragma unroll
-    for (int i = 0; i < kWaves; ++i) x += redi_l[i];
-    return x;
-  };
-  auto min_i = [&](int x) {
-    x = wave_min_i(x);
-    __syncthreads();
-    if (lane == 0) redi_l[w] = x;
-    __syncthreads();
-    x = redi_l[0];
-#pragma unroll
-    for (int i = 1; i < kWaves; ++i) x = min(x, redi_l[i]);
-    return x;
-  };
-  auto max_f = [&](float x) {
-    x = wave_max(x);
-    __syncthreads();
-    if (lane == 0) red_l[w] = x;
-    __syncthreads();
-    x = red_l[0];
-#pragma unroll
-    for (int i = 1; i < kWaves; ++i) x = fmaxf(x, red_l[i]);
-    return x;
-  };
-  auto sum_f = [&](float x) {
-    x = wave_sum(x);
-    __syncthreads();
-    if (lane == 0) red_l[w] = x;
-    __syncthreads();
-    x = 0.f;
-#pragma unroll
-    for (int i = 0; i < kWaves; ++i) x += red_l[i];
-    return x;
-  };
-  // the row's request: as many end at or before it
-  int before = 0;
-  for (int i = tid; i < p.batch; i += kThreads) before += (int64_t)p.cu_rows[i + 1] <= r ? 1 : 0;
-  const int b = sum_i(before);
-  if (b >= p.batch) return;
+  const int64_t group = block / pieces;
+  const int64_t r_first = group * per, r_end = min(r_first + per, p.n_rows);
+  if (r_first >= r_end) return;
+  const int piece = (int)(block - group * pieces), p0 = piece * kPiece;
+  const bool inside = p0 + kPiece <= p.vocab;
 
-  // what was said of the piece's tokens
-  for (int i = tid; i < kPiece / 4; i += kThreads) {
-    reinterpret_cast<uint4*>(said_l)[i] = make_uint4(0, 0, 0, 0);
-    if (kBias) reinterpret_cast<uint4*>(bias_l)[i] = make_uint4(0, 0, 0, 0);
-  }
-  __syncthreads();
-  if (p.history) {
-    const int n = min(max(p.hist_len[b], 0), p.max_history);
-    const int prompt = p.prompt_len ? p.prompt_len[b] : 0;
-    const int32_t* h = p.history + (int64_t)b * p.history_stride;
-    constexpr int U = 8;
-    for (int i0 = tid; i0 < n; i0 += kThreads * U) {
-      int t[U];
+  auto clear = [&]() {
+    for (int i = tid; i < kPiece / 4; i += kThreads) {
+      reinterpret_cast<uint4*>(said_l)[i] = make_uint4(0, 0, 0, 0);
+      if (kBias) reinterpret_cast<uint4*>(bias_l)[i] = make_uint4(0, 0, 0, 0);
+    }
+  };
+  clear();
+  // the first row's request: as many end at or before it (every wave looks for itself)
+  int b = 0;
+  for (int i0 = 0; i0 < p.batch; i0 += 256) {
+    int end[4];
 #pragma unroll
-      for (int k = 0; k < U; ++k) t[k] = h[min(i0 + k * kThreads, n - 1)];
+    for (int k = 0; k < 4; ++k) end[k] = p.cu_rows[min(i0 + 64 * k + lane, p.batch - 1) + 1];
+#pragma unroll
+    for (int k = 0; k < 4; ++k)
+      b += __builtin_popcountll(__ballot(i0 + 64 * k + lane < p.batch && (int64_t)end[k] <= r_first));
+  }
+  // everything that is one number per request comes by one load, a lane each
+  const int32_t* param = p.cu_rows;  // lane 0: where the request begins; 1: and ends
+  int instead = 0;
+  const auto lane_is = [&](int i, const void* x, int none) {
+    if (lane == i) {
+      param = static_cast<const int32_t*>(x);
+      instead = none;
+    }
+  };
+  lane_is(2, p.hist_len, 0);
+  lane_is(3, p.prompt_len, 0);
+  lane_is(4, p.repetition, __float_as_int(1.f));
+  lane_is(5, p.presence, 0);
+  lane_is(6, p.frequency, 0);
+  lane_is(7, p.temperature, __float_as_int(1.f));
+  lane_is(8, p.bias_start, 0);
+  lane_is(9, p.bias_start, 0);
+  const int second = lane == 1 || lane == 9 ? 1 : 0;
+
+  int counted = -1;             // the request whose history is counted
+  int64_t first = 0, last = 0;  // its rows
+  float rep = 1.f, inv_rep = 1.f, pres = 0.f, freq = 0.f, c = 1.f;
+  bool cold = false;
+  int64_t bias0 = 0;
+  // adds (1) or takes back (-1) the drafted tokens that row r follows
+  auto drafts = [&](int64_t r, uint32_t what) {
+    const uint32_t* m = p.tree_mask ? p.tree_mask + r * p.mask_words : nullptr;
+    const int end = m ? (int)min(last - first, (int64_t)p.mask_words * 32) : (int)(r - first) + 1;
+    for (int j = tid; j < end; j += kThreads) {
+      const uint32_t at = (uint32_t)p.tokens[first + j] - (uint32_t)p0;
+      if (at < (uint32_t)kPiece && (!m || (m[j >> 5] >> (j & 31) & 1))) atomicAdd(&said_l[at], what);
+    }
+  };
+  // the history's tokens from .. to - 1: `count` is given the place of each that lies in the piece
+  auto scan = [&](const int32_t* h, int from, int to, auto count) {
+    if (to - from < 4) {
+      if (tid < to - from) {
+        const uint32_t at = (uint32_t)h[from + tid] - (uint32_t)p0;
+        if (at < (uint32_t)kPiece) count(at);
+      }
+      return;
+    }
+    constexpr int U = 4;
+#pragma unroll 1
+    for (int i0 = from + tid * 4; i0 < to; i0 += kThreads * 4 * U) {
+      uint4 t[U];
+#pragma unroll
+      for (int k = 0; k < U; ++k) t[k] = load16(h + min(i0 + k * kThreads * 4, to - 4));
 #pragma unroll
       for (int k = 0; k < U; ++k) {
-        const int i = i0 + k * kThreads;
-        const uint32_t x = (uint32_t)t[k] - (uint32_t)p0;
-        if (i < n && t[k] >= 0 && x < (uint32_t)kPiece) {
-          if (i < prompt) atomicOr(&said_l[x], 1u);
-          else atomicAdd(&said_l[x], 2u);
+        // (the last four overlap the four before: those are left out)
+        const int i = i0 + k * kThreads * 4, over = i - min(i, to - 4);
+        const uint32_t a0 = t[k].x - p0, a1 = t[k].y - p0, a2 = t[k].z - p0, a3 = t[k].w - p0;
+        if (a0 < (uint32_t)kPiece && over < 1) count(a0);
+        if (a1 < (uint32_t)kPiece && over < 2) count(a1);
+        if (a2 < (uint32_t)kPiece && over < 3) count(a2);
+        if (a3 < (uint32_t)kPiece && over < 4) count(a3);
+      }
+    }
+  };
+  // vector k of a row's tokens, as they are stored (behind the vocabulary its last one), and its word of the mask
+  struct Raw {
+    uint4 q[sizeof(In) * kVec / 16];
+    uint32_t allowed;
+  };
+  // (the thread's number, formed anew: offsets that are kept from row to row would be a register each)
+  auto self = [&]() {
+    int i = threadIdx.x;
+    asm volatile("" : "+v"(i));
+    return i;
+  };
+  auto load = [&](int64_t r, int k) {
+    const In* in = static_cast<const In*>(p.logits) + r * p.logits_stride;
+    const int t0 = p0 + (self() + k * kThreads) * kVec;
+    Raw x;
+    if (p.vocab >= kVec) {
+      // (aligned as its elements are; behind the vocabulary's last vector that one stands in, and the one that
+      // it ends in is read again by elements)
+      const int over = max(t0 + kVec - p.vocab, 0);
+#pragma unroll
+      for (int i = 0; i < (int)(sizeof x.q / 16); ++i) x.q[i] = load16(in + t0 - over + i * Vec16<In>::N);
+      if (!inside && over > 0 && over < kVec) {
+        In v[kVec];
+#pragma unroll
+        for (int e = 0; e < kVec; ++e) v[e] = in[min(t0 + e, p.vocab - 1)];
+        __builtin_memcpy(x.q, v, sizeof x.q);
+      }
+    } else {
+      In v[kVec];
+#pragma unroll
+      for (int e = 0; e < kVec; ++e) v[e] = in[min(t0 + e, p.vocab - 1)];
+      __builtin_memcpy(x.q, v, sizeof x.q);
+    }
+    x.allowed = p.allowed ? p.allowed[r * p.allowed_words + (min(t0, p.vocab - 1) >> 5)] : ~0u;
+    return x;
+  };
+  // its z; -infinity behind the vocabulary
+  const bool masked = !inside || p.allowed;
+  auto shaped = [&](const Raw& raw, int k, float (&x)[kVec]) {
+    const int at = (self() + k * kThreads) * kVec, t0 = p0 + at;
+    uint32_t said[kVec];
+    *reinterpret_cast<uint4*>(said) = *reinterpret_cast<const uint4*>(said_l + at);
+    *reinterpret_cast<uint4*>(said + 4) = *reinterpret_cast<const uint4*>(said_l + at + 4);
+#pragma unroll
+    for (int i = 0; i < (int)(sizeof raw.q / 16); ++i) Vec16<In>::unpack(raw.q[i], &x[i * Vec16<In>::N]);
+    if ((said[0] | said[1]) | (said[2] | said[3]) | (said[4] | said[5]) | (said[6] | said[7])) {
+#pragma unroll
+      for (int e = 0; e < kVec; ++e) {
+        const float n = (float)(said[e] & ~kSaid), z = x[e];
+        const float by = said[e] ? z > 0.f ? inv_rep : rep : 1.f;
+        x[e] = fmaf(z, by, -fmaf(freq, n, n > 0.f ? pres : 0.f));
+      }
+    }
+    if (kBias) {
+      uint32_t bias[kVec];
+      *reinterpret_cast<uint4*>(bias) = *reinterpret_cast<const uint4*>(bias_l + at);
+      *reinterpret_cast<uint4*>(bias + 4) = *reinterpret_cast<const uint4*>(bias_l + at + 4);
+      if ((bias[0] | bias[1]) | (bias[2] | bias[3]) | (bias[4] | bias[5]) | (bias[6] | bias[7])) {
+#pragma unroll
+        for (int e = 0; e < kVec; ++e)
+          if (bias[e]) x[e] += p.bias_value[bias0 + bias[e] - 1];
+      }
+    }
+    if (masked) {
+      uint32_t bits = raw.allowed >> (t0 & 31) & 0xffu;
+      bits &= t0 + kVec <= p.vocab ? 0xffu : t0 < p.vocab ? (1u << (p.vocab - t0)) - 1u : 0u;
+#pragma unroll
+      for (int e = 0; e < kVec; ++e) x[e] = bits >> e & 1 ? x[e] : -INFINITY;
+    }
+  };
+
+  for (int64_t r = r_first; r < r_end; ++r) {
+    Raw raw[kVecs];
+#pragma unroll
+    for (int k = 0; k < kVecs; ++k) raw[k] = load(r, k);
+    if (r > r_first) {
+      while (b < p.batch && (int64_t)p.cu_rows[b + 1] <= r) ++b;
+      meet();  // the last row's counts have been read
+    }
+    if (b >= p.batch) return;
+    if (b != counted) {
+      const int x = *(param ? param + b + second : p.cu_rows);
+      const auto of = [&](int i) { return __builtin_amdgcn_readlane(param ? x : instead, i); };
+      if (counted >= 0) clear();
+      counted = b;
+      first = of(0);
+      last = min((int64_t)of(1), p.n_rows);
+      rep = __int_as_float(of(4));
+      inv_rep = 1.f / rep;
+      pres = __int_as_float(of(5));
+      freq = __int_as_float(of(6));
+      const float temp = kMode == kLogits ? 1.f : __int_as_float(of(7));
+      cold = temp == 0.f;
+      c = cold ? 1.f : kLog2e / temp;
+      meet();  // (the counts are zero)
+      if (p.history) {
+        const int n = min(max(of(2), 0), p.max_history), prompt = min(max(of(3), 0), n);
+        const int32_t* h = p.history + (int64_t)b * p.history_stride;
+        scan(h, 0, prompt, [&](uint32_t at) { atomicOr(&said_l[at], kSaid); });
+        scan(h, prompt, n, [&](uint32_t at) { atomicAdd(&said_l[at], 1u); });
+      }
+      if (kBias) {
+        bias0 = max(of(8), 0);
+        const int64_t bias1 = min((int64_t)of(9), p.n_bias);
+        for (int64_t e = bias0 + tid; e < bias1; e += kThreads) {
+          const uint32_t at = (uint32_t)p.bias_token[e] - (uint32_t)p0;
+          if (at < (uint32_t)kPiece) atomicMax(&bias_l[at], (uint32_t)(e - bias0) + 1u);
+        }
+      }
+    } else if (p.tokens) {
+      drafts(r - 1, (uint32_t)-1);
+    }
+    if (p.tokens) drafts(r, 1u);
+    meet();
+
+    Stat all{-INFINITY, 0.f, INT32_MAX, 0};
+    if (kMode == kStats || kMode == kWhole) {
+      // the waves', each with its own maximum, then the block's in the waves' order
+      float x[kVecs][kVec], m = -INFINITY;
+#pragma unroll
+      for (int k = 0; k < kVecs; ++k) {
+        shaped(raw[k], k, x[k]);
+#pragma unroll
+        for (int e = 0; e < kVec; ++e) m = fmaxf(m, x[k][e]);
+      }
+      m = wave_max(m);
+      Stat wave{cold ? m : m * c, 0.f, INT32_MAX, 0};
+      if (cold) {
+        const int id = self();
+#pragma unroll
+        for (int k = kVecs - 1; k >= 0; --k)
+#pragma unroll
+          for (int e = kVec - 1; e >= 0; --e)
+            if (x[k][e] == m && m > -INFINITY) wave.at = p0 + (id + k * kThreads) * kVec + e;
+        wave.at = wave_min_i(wave.at);
+      } else {
+        const float ref = finite(wave.m);
+#pragma unroll
+        for (int k = 0; k < kVecs; ++k) {
+          float s = 0.f;
+#pragma unroll
+          for (int e = 0; e < kVec; ++e) s += __builtin_amdgcn_exp2f(fmaf(x[k][e], c, -ref));
+          wave.s += s;
+        }
+        wave.s = wave_sum(wave.s);
+      }
+      if (lane == 0) red_l[w] = wave;
+      meet();
+#pragma unroll 1
+      for (int i = 0; i < kWaves; ++i) all = both(all, red_l[i], cold);
+      if (kMode == kStats && tid == 0) stats[r * pieces + piece] = all;
+    } else if (kMode == kWrite) {
+      // the row's: pieces in their order, 64 at a time
+      const Stat* st = stats + r * pieces;
+#pragma unroll 1
+      for (int i0 = 0; i0 < pieces; i0 += 64) {
+        Stat one = st[min(i0 + lane, pieces - 1)];
+        const bool there = i0 + lane < pieces;
+        const float m = wave_max(there ? one.m : -INFINITY);
+        Stat some{m, 0.f, INT32_MAX, 0};
+        if (cold) some.at = wave_min_i(there && one.m == m ? one.at : INT32_MAX);
+        else some.s = wave_sum(there ? one.s * __builtin_amdgcn_exp2f(one.m - finite(m)) : 0.f);
+        all = both(all, some, cold);
+      }
+    }
+    if (kMode != kStats) {
+      const float ref = finite(all.m), inv = all.s == 0.f ? 0.f : 1.f / all.s;
+      Out* out = static_cast<Out*>(p.out) + r * p.out_stride;
+#pragma unroll
+      for (int k = 0; k < kVecs; ++k) {
+        const int t0 = p0 + (self() + k * kThreads) * kVec;
+        float x[kVec];
+        shaped(raw[k], k, x);
+        if (kMode != kLogits) {
+#pragma unroll
+          for (int e = 0; e < kVec; ++e) x[e] = cold ? (t0 + e == all.at ? 1.f : 0.f) : __builtin_amdgcn_exp2f(fmaf(x[e], c, -ref)) * inv;
+        }
+        if (t0 + kVec <= p.vocab) {
+          store8(out + t0, x);
+        } else if (!inside) {
+#pragma unroll
+          for (int e = 0; e < kVec; ++e)
+            if (t0 + e < p.vocab) put(out + t0 + e, x[e]);
         }
       }
     }
   }
-  if (p.tokens) {
-    const int64_t first = p.cu_rows[b];
-    const int own = (int)(r - first);
-    const int64_t last = min((int64_t)p.cu_rows[b + 1], p.n_rows);
-    const int rows = (int)(last - first);
-    const uint32_t* m = p.tree_mask ? p.tree_mask + r * p.mask_words : nullptr;
-    const int end = m ? (int)min((int64_t)rows, (int64_t)p.mask_words * 32) : own + 1;
-    for (int j = tid; j < end; j += kThreads) {
-      const int t = p.tokens[first + j];
-      const uint32_t x = (uint32_t)t - (uint32_t)p0;
-      if (t >= 0 && x < (uint32_t)kPiece && (!m || (m[j >> 5] >> (j & 31) & 1))) atomicAdd(&said_l[x], 2u);
-    }
-  }
-  int64_t bias0 = 0;
-  if (kBias) {
-    bias0 = max((int64_t)p.bias_start[b], (int64_t)0);
-    const int64_t bias1 = min((int64_t)p.bias_start[b + 1], p.n_bias);
-    for (int64_t e = bias0 + tid; e < bias1; e += kThreads) {
-      const int t = p.bias_token[e];
-      const uint32_t x = (uint32_t)t - (uint32_t)p0;
-      if (t >= 0 && x < (uint32_t)kPiece) atomicMax(&bias_l[x], (uint32_t)(e - bias0) + 1u);
-    }
-  }
-  __syncthreads();
-
-  const float rep = p.repetition ? p.repetition[b] : 1.f, pres = p.presence ? p.presence[b] : 0.f;
-  const float freq = p.frequency ? p.frequency[b] : 0.f;
-  const float temp = kMode != kLogits && p.temperature ? p.temperature[b] : 1.f;
-  const bool cold = temp == 0.f;
-  const float inv_t = cold ? 1.f : 1.f / temp;
-  const In* in = static_cast<const In*>(p.logits) + r * p.logits_stride;
-  Out* out = static_cast<Out*>(p.out) + r * p.out_stride;
-  const uint32_t* allowed = p.allowed ? p.allowed + r * p.allowed_words : nullptr;
-
-  // x = z / T of the thread's tokens, -infinity behind the vocabulary
-  float x[kVecs][kVec];
-#pragma unroll
-  for (int k = 0; k < kVecs; ++k) {
-    const int at = (tid + k * kThreads) * kVec, t0 = p0 + at;
-    if (t0 + kVec <= p.vocab) {
-      load8(in + t0, x[k]);
-    } else {
-#pragma unroll
-      for (int e = 0; e < kVec; ++e) x[k][e] = t0 + e < p.vocab ? as_float(in[t0 + e]) : -INFINITY;
-    }
-  }
-#pragma unroll
-  for (int k = 0; k < kVecs; ++k) {
-    const int at = (tid + k * kThreads) * kVec, t0 = p0 + at;
-    const uint32_t bits = !allowed ? 0xffu : t0 < p.vocab ? allowed[t0 >> 5] >> (t0 & 31) & 0xffu : 0u;
-    uint32_t said[kVec], bias[kVec];
-    *reinterpret_cast<uint4*>(said) = *reinterpret_cast<const uint4*>(said_l + at);
-    *reinterpret_cast<uint4*>(said + 4) = *reinterpret_cast<const uint4*>(said_l + at + 4);
-    if (kBias) {
-      *reinterpret_cast<uint4*>(bias) = *reinterpret_cast<const uint4*>(bias_l + at);
-      *reinterpret_cast<uint4*>(bias + 4) = *reinterpret_cast<const uint4*>(bias_l + at + 4);
-    }
-#pragma unroll
-    for (int e = 0; e < kVec; ++e) {
-      float z = x[k][e];
-      if (said[e]) {
-        const float c = (float)(said[e] >> 1);
-        z = z > 0.f ? z / rep : z * rep;
-        z = fmaf(-freq, c, z);
-        if (c > 0.f) z -= pres;
-      }
-      if (kBias && bias[e]) z += p.bias_value[bias0 + bias[e] - 1];
-      if (!(bits >> e & 1) || t0 + e >= p.vocab) z = -INFINITY;
-      x[k][e] = kMode == kLogits ? z : z * inv_t;
-    }
-  }
-  auto store = [&](int k) {
-    const int t0 = p0 + (tid + k * kThreads) * kVec;
-    if (t0 + kVec <= p.vocab) {
-      store8(out + t0, x[k]);
-    } else {
-#pragma unroll
-      for (int e = 0; e < kVec; ++e)
-        if (t0 + e < p.vocab) put(out + t0 + e, x[k][e]);
-    }
-  };
-  if (kMode == kLogits) {
-#pragma unroll
-    for (int k = 0; k < kVecs; ++k) store(k);
-    return;
-  }
-  Stat all;
-  if (kMode != kWrite) {
-    float m = -INFINITY;
-#pragma unroll
-    for (int k = 0; k < kVecs; ++k)
-#pragma unroll
-      for (int e = 0; e < kVec; ++e) m = fmaxf(m, x[k][e]);
-    m = max_f(m);
-    int at = INT32_MAX;
-    float s = 0.f;
-    if (cold) {
-#pragma unroll
-      for (int k = 0; k < kVecs; ++k)
-#pragma unroll
-        for (int e = 0; e < kVec; ++e)
-          if (x[k][e] == m && m > -INFINITY) at = min(at, p0 + (tid + k * kThreads) * kVec + e);
-      at = min_i(at);
-    } else {
-      const float ref = m == -INFINITY ? 0.f : m;
-#pragma unroll
-      for (int k = 0; k < kVecs; ++k)
-#pragma unroll
-        for (int e = 0; e < kVec; ++e) s += exp_of(x[k][e] - ref);
-      s = sum_f(s);
-    }
-    all = Stat{m, s, at, 0};
-    if (kMode == kStats) {
-      if (tid == 0) stats[r * pieces + piece] = all;
-      return;
-    }
-  } else {
-    // the row's: pieces in their order, 64 at a time
-    const Stat* st = stats + r * pieces;
-    all = Stat{-INFINITY, 0.f, INT32_MAX, 0};
-    for (int i0 = 0; i0 < pieces; i0 += 64) {
-      const Stat one = st[min(i0 + lane, pieces - 1)];
-      const bool there = i0 + lane < pieces;
-      const float m = wave_max(there ? one.m : -INFINITY), mn = fmaxf(all.m, m);
-      if (cold) {
-        const int at = wave_min_i(there && one.m == mn ? one.at : INT32_MAX);
-        all.at = all.m == mn ? min(all.at, at) : at;
-      } else {
-        const float ref = mn == -INFINITY ? 0.f : mn;
-        all.s = all.s * exp_of(all.m - ref) + wave_sum(there ? one.s * exp_of(one.m - ref) : 0.f);
-      }
-      all.m = mn;
-    }
-  }
-  if (cold) {
-#pragma unroll
-    for (int k = 0; k < kVecs; ++k)
-#pragma unroll
-      for (int e = 0; e < kVec; ++e) x[k][e] = p0 + (tid + k * kThreads) * kVec + e == all.at ? 1.f : 0.f;
-  } else {
-    const float ref = all.m == -INFINITY ? 0.f : all.m;
-    const float inv = all.s == 0.f ? 0.f : 1.f / all.s;
-#pragma unroll
-    for (int k = 0; k < kVecs; ++k)
-#pragma unroll
-      for (int e = 0; e < kVec; ++e) x[k][e] = exp_of(x[k][e] - ref) * inv;
-  }
-#pragma unroll
-  for (int k = 0; k < kVecs; ++k) store(k);
 }
 
-inline int pieces_of(int vocab) { return (vocab + kPiece - 1) / kPiece; }
+inline int pieces_of(int vocab, bool bias) { return (vocab + piece_of(bias) - 1) / piece_of(bias); }
 
 template <typename In, typename Out, bool kBias>
 hipError_t launch_t(const ShapeLogits& p, bool probabilities, void* ws, hipStream_t stream) {
-  const int pieces = pieces_of(p.vocab);
-  const dim3 grid = grid_of(p.n_rows * pieces);
+  const int pieces = pieces_of(p.vocab, kBias);
+  // rows of a block: more share one count of the history, as long as the blocks fill the chip twice
+  const int per = (int)std::min<int64_t>(std::max<int64_t>(p.n_rows * pieces / kShapeBlocks, 1), 16);
+  const dim3 grid = grid_of((p.n_rows + per - 1) / per * pieces);
   Stat* stats = static_cast<Stat*>(ws);
   if (!probabilities) {
-    shape_kernel<In, Out, kLogits, kBias><<<grid, kThreads, 0, stream>>>(p, stats, pieces);
+    shape_kernel<In, Out, kLogits, kBias><<<grid, kThreads, 0, stream>>>(p, stats, pieces, per);
   } else if (pieces == 1) {
-    shape_kernel<In, Out, kWhole, kBias><<<grid, kThreads, 0, stream>>>(p, stats, pieces);
+    shape_kernel<In, Out, kWhole, kBias><<<grid, kThreads, 0, stream>>>(p, stats, pieces, per);
   } else {
-    shape_kernel<In, Out, kStats, kBias><<<grid, kThreads, 0, stream>>>(p, stats, pieces);
-    shape_kernel<In, Out, kWrite, kBias><<<grid, kThreads, 0, stream>>>(p, stats, pieces);
+    shape_kernel<In, Out, kStats, kBias><<<grid, kThreads, 0, stream>>>(p, stats, pieces, per);
+    shape_kernel<In, Out, kWrite, kBias><<<grid, kThreads, 0, stream>>>(p, stats, pieces, per);
   }
   return hipGetLastError();
 }
@@ -316,7 +389,8 @@ hipError_t launch_b(const ShapeLogits& p, bool probabilities, void* ws, hipStrea
 }  // namespace
 
 size_t shape_logits_workspace(int64_t n_rows, int vocab) {
-  return pieces_of(vocab) > 1 ? (size_t)n_rows * pieces_of(vocab) * sizeof(Stat) : 0;
+  const int pieces = pieces_of(vocab, true);  // (the smaller pieces)
+  return pieces > 1 ? (size_t)n_rows * pieces * sizeof(Stat) : 0;
 }
 
 hipError_t launch_shape_logits(const ShapeLogits& p, bool in_bf16, bool out_bf16, bool probabilities, void* ws,

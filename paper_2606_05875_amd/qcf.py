@@ -26,7 +26,8 @@ __all__ = [
     "qcf_page_plan", "qcf_rope_frequencies", "rope_frequencies", "qcf_rope_store", "qcf_tree_attn_workspace_size",
     "qcf_tree_attn", "qcf_verify_drafts_workspace_size", "qcf_verify_drafts",
     "qcf_norm_rope_store", "qcf_chunk_attn_workspace_size", "qcf_chunk_attn", "qcf_shape_logits_workspace_size",
-    "qcf_shape_logits", "qcf_page_fork", "PoolSet", "qcf_copy_pages", "qcf_page_release",
+    "qcf_shape_logits", "qcf_page_fork", "PoolSet", "qcf_copy_pages",
+    "qcf_page_release_workspace_size", "qcf_page_release",
     "EXPORTS", "Prepared", "prepare",
 ]
 
@@ -95,7 +96,8 @@ EXPORTS = {
                               _P, _P, _P, _P, _I64, _P, _I64, _P, _I, _P, _SZ, _P]),
     "qcf_page_fork": (_I, [_P, _I64, _P, _P, _P, _I64, _I, _I, _P, _P, _P, _P, _I64, _P, _I64, _I, _P, _P, _P, _P, _P]),
     "qcf_copy_pages": (_I, [_P, _I, _I64, _I64, _I64, _I, _P, _P, _P, _I64, _P]),
-    "qcf_page_release": (_I, [_P, _I64, _P, _P, _I64, _P, _I, _I, _P, _I64, _P, _P, _I64, _P]),
+    "qcf_page_release_workspace_size": (_SZ, [_I, _I, _I64]),
+    "qcf_page_release": (_I, [_P, _I64, _P, _P, _I64, _P, _I, _I, _P, _I64, _P, _P, _I64, _P, _SZ, _P]),
 }
 
 
@@ -1051,7 +1053,12 @@ def qcf_copy_pages(pools, src_page, dst_page, page_size, rows=None):
             int(page_size), _ptr(src_page), _ptr(dst_page), _ptr(rows), n, keep=pools)
 
 
-def qcf_page_release(table_before, held_before, table_after, held_after, free_pages, free_head, free_head_out, n_pages):
+def qcf_page_release_workspace_size(batch, max_pages, n_pages):
+    return int(lib().qcf_page_release_workspace_size(int(batch), int(max_pages), int(n_pages)))
+
+
+def qcf_page_release(table_before, held_before, table_after, held_after, free_pages, free_head, free_head_out, n_pages,
+                     workspace=None):
     """Pages among the first held_before entries of the one table's rows and of none of the other's first held_after
     go back in front of the free list's first free entry."""
     batch = held_before.numel()
@@ -1065,7 +1072,11 @@ def qcf_page_release(table_before, held_before, table_after, held_after, free_pa
     if table_before.shape[0] != batch or table_after.shape != table_before.shape:
         raise QcfError("the tables need a row per request and the same columns")
     _here("qcf_page_release", table_before=table_before, held_before=held_before, table_after=table_after,
-          held_after=held_after, free_pages=free_pages, free_head=free_head, free_head_out=free_head_out)
+          held_after=held_after, free_pages=free_pages, free_head=free_head, free_head_out=free_head_out,
+          workspace=workspace)
+    need = qcf_page_release_workspace_size(batch, table_before.shape[1], n_pages)
+    if workspace is None and need > 0:
+        workspace = torch.empty(need, dtype=torch.uint8, device=free_pages.device)
     _invoke("qcf_page_release", _ptr(table_before), strides[0], _ptr(held_before), _ptr(table_after), strides[1],
             _ptr(held_after), table_before.shape[1], batch, _ptr(free_pages), free_pages.numel(), _ptr(free_head),
-            _ptr(free_head_out), int(n_pages))
+            _ptr(free_head_out), int(n_pages), _ptr(workspace), 0 if workspace is None else workspace.numel(), keep=workspace)

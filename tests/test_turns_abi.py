@@ -28,7 +28,7 @@ def test_declared_and_bound(L):
             for m in re.finditer(r"\b(?:qcf_status|size_t)\s+(qcf_\w+)\s*\(([^;]*?)\)\s*;", text, re.S)}
     assert set(decl) == {"qcf_norm_rope_store", "qcf_chunk_attn_workspace_size", "qcf_chunk_attn",
                          "qcf_shape_logits_workspace_size", "qcf_shape_logits", "qcf_page_fork", "qcf_copy_pages",
-                         "qcf_page_release"}
+                         "qcf_page_release_workspace_size", "qcf_page_release"}
     for name, nargs in decl.items():
         assert hasattr(L, name) and len(qcf.EXPORTS[name][1]) == nargs, name
         assert name in qcf.__all__, name
@@ -151,15 +151,23 @@ def test_copy_pages_refusals(L):
 
 
 def test_page_release_refusals(L):
+    need = L.qcf_page_release_workspace_size(400, 1000, 100000)
+    assert need > 0 and L.qcf_page_release_workspace_size(4, 10, 100) == 0 and L.qcf_page_release_workspace_size(0, 10, 5) == 0
+    assert need <= L.qcf_page_release_workspace_size(401, 1001, 100001)
+
     def call(**k):
         g = k.get
-        return L.qcf_page_release(g("tb", A), g("bs", 10), g("hb", A + 64), g("ta", A), g("as_", 10), g("ha", A + 128),
-                                  g("cols", 10), g("batch", 4), g("free", B), g("n_free", 8), g("head", C),
-                                  g("fo", C + 64), g("pages", 100), None)
+        return L.qcf_page_release(g("tb", A), g("bs", 1000), g("hb", A + 64), g("ta", A), g("as_", 1000), g("ha", A + 128),
+                                  g("cols", 1000), g("batch", 400), g("free", B), g("n_free", 8), g("head", C),
+                                  g("fo", C + 64), g("pages", 100000), g("ws", B + 256), g("wsb", need), None)
     for bad in (dict(tb=None), dict(hb=None), dict(ta=None), dict(ha=None), dict(free=None), dict(head=None),
-                dict(fo=None), dict(bs=9), dict(as_=9), dict(batch=-1), dict(cols=-1), dict(n_free=-1), dict(pages=-1),
+                dict(fo=None), dict(bs=999), dict(as_=999), dict(batch=-1), dict(cols=-1), dict(n_free=-1), dict(pages=-1),
                 dict(pages=1 << 31), dict(fo=C), dict(free=A), dict(hb=MIS + 1), dict(free=C)):
         assert call(**bad) == INVALID, bad
+    for bad in (dict(batch=1 << 22), dict(batch=1 << 12, cols=1 << 21, bs=1 << 21, as_=1 << 21)):
+        assert call(**bad) == UNSUPPORTED, bad
+    for bad in (dict(ws=None), dict(ws=B + 16), dict(wsb=need - 1)):
+        assert call(**bad) == WORKSPACE, bad
 
 
 def test_the_binding_refuses_host_tensors():
