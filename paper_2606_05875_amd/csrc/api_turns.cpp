@@ -51,7 +51,7 @@ size_t qcf_chunk_attn_workspace_size(int batch, int max_q, int max_kv, int n_q_h
                                      int n_kv_heads, int head_dim, qcf_dtype dtype) {
   if (!dtype_ok(dtype) || check_heads(n_q_heads, n_kv_heads, head_dim) != QCF_OK) return 0;
   if (batch <= 0 || max_q <= 0 || max_kv <= 0) return 0;
-  return qcf::chunk_attn_workspace(batch, max_q, max_kv, n_q_heads, n_kv_heads, head_dim, dtype == QCF_BF16);
+  return qcf::chunk_attn_workspace(max_q, n_q_heads, n_kv_heads, head_dim, dtype == QCF_BF16);
 }
 
 qcf_status qcf_chunk_attn(void* out, float* lse, const void* q, int64_t n_rows,
@@ -74,7 +74,7 @@ qcf_status qcf_chunk_attn(void* out, float* lse, const void* q, int64_t n_rows,
   if (!kv_stride_ok(kv_row_stride, n_kv_heads, head_dim, dtype)) return QCF_ERR_INVALID_ARG;
   // the kernels' 32-bit numbers: offsets inside 16 rows, (row, head) pairs, tokens a few tiles on
   if (kv_row_stride > INT32_MAX / (16 * esize(dtype)) || max_kv > INT32_MAX - (1 << 21) || max_q > 1 << 20 ||
-      !qcf::chunk_attn_fits(batch, max_q, max_kv, n_q_heads, n_kv_heads, dtype == QCF_BF16))
+      !qcf::chunk_attn_fits(batch, max_q, n_q_heads, n_kv_heads, dtype == QCF_BF16))
     return QCF_ERR_UNSUPPORTED;
   const bool empty = n_rows == 0 || batch == 0 || max_q == 0;
   const bool no_kv = empty || max_kv == 0 || max_pages == 0 || n_slots >> lp == 0;

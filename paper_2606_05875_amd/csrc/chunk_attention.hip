@@ -52,6 +52,7 @@ __global__ __launch_bounds__(kW * 64, 2) void chunk_attn_kernel(ChunkAttn p, Chu
   uint32_t coff = cr * row_b, kx = (cc ^ (D == 128 ? cr : cr >> 1)) * 16;
   const uint32_t vx = (cc ^ (4 * (D == 128 ? cr : (cr >> 1) & 1))) * 16;
 
+  if (threadIdx.x < 2) loose_l[threadIdx.x] = 0;
   chunk_walk<kW * 64>(p, cut, ws, lg, [&](int b, const TreeRequest& rq, int g, int tile, int first, int n, int slot) {
     const int32_t* table = p.block_table + b * p.table_stride;
     const char* kc = static_cast<const char*>(p.k_cache) + (int64_t)g * RB;
@@ -265,8 +266,6 @@ __global__ __launch_bounds__(kW * 64, 2) void chunk_attn_kernel(ChunkAttn p, Chu
     // is the tokens with a value that is not finite, which are added to the rows that see them one by one ..
     auto clean = [&](int t, uint64_t held) {
       uint8_t* vl = v_ring + (t & 1) * TB;
-      if (threadIdx.x < 2) loose_l[threadIdx.x] = 0;
-      __syncthreads();
       for (int u = threadIdx.x; u < kT * CH; u += kW * 64) {
         const int r = u / CH;
         if (!(held >> r & 1)) st16(vl + 16 * u, make_uint4(0, 0, 0, 0));
@@ -281,6 +280,7 @@ __global__ __launch_bounds__(kW * 64, 2) void chunk_attn_kernel(ChunkAttn p, Chu
       __syncthreads();
       for (int u = threadIdx.x; u < kT * CH; u += kW * 64)
         if (loose >> (u / CH) & 1) st16(vl + 16 * u, make_uint4(0, 0, 0, 0));
+      if (threadIdx.x < 2) loose_l[threadIdx.x] = 0;  // (zero between tiles)
       __syncthreads();
     };
     auto add_loose = [&](int t, uint64_t loose, uint64_t sees, const f32x16 (&s)[2]) {
@@ -428,7 +428,7 @@ __global__ __launch_bounds__(kW * 64, 2) void chunk_attn_kernel(ChunkAttn p, Chu
 template <int D>
 hipError_t launch_bf16(const ChunkAttn& p, void* workspace, hipStream_t stream) {
   const int lg = log2_of(p.hq / p.hkv);
-  const ChunkCut c = chunk_cut(p.batch, p.max_q, p.max_kv, p.hq, p.hkv, true);
+  const ChunkCut c = chunk_cut(p.max_q, p.hq, p.hkv, true);
   const ChunkWs ws = chunk_ws(c, D, workspace);
   chunk_attn_kernel<D><<<dim3((unsigned)c.blocks), kW * 64, 0, stream>>>(p, c, ws, lg);
   launch_chunk_merge<uint16_t, D>(p, c, ws, lg, stream);
@@ -437,14 +437,14 @@ hipError_t launch_bf16(const ChunkAttn& p, void* workspace, hipStream_t stream) 
 
 }  // namespace
 
-bool chunk_attn_fits(int batch, int max_q, int max_kv, int hq, int hkv, bool bf16) {
-  const ChunkCut c = chunk_cut(batch, max_q, max_kv, hq, hkv, bf16);
+bool chunk_attn_fits(int batch, int max_q, int hq, int hkv, bool bf16) {
+  const ChunkCut c = chunk_cut(max_q, hq, hkv, bf16);
   const int64_t units = (int64_t)hkv * c.tiles;
   return batch == 0 || units <= INT32_MAX / batch;
 }
 
-size_t chunk_attn_workspace(int batch, int max_q, int max_kv, int hq, int hkv, int head_dim, bool bf16) {
-  return chunk_ws_layout(chunk_cut(batch, max_q, max_kv, hq, hkv, bf16), head_dim).total;
+size_t chunk_attn_workspace(int max_q, int hq, int hkv, int head_dim, bool bf16) {
+  return chunk_ws_layout(chunk_cut(max_q, hq, hkv, bf16), head_dim).total;
 }
 
 hipError_t launch_chunk_attn(const ChunkAttn& p, bool bf16, int head_dim, void* ws, hipStream_t stream) {

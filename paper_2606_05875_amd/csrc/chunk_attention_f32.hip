@@ -263,7 +263,7 @@ __global__ __launch_bounds__(kW * 64, 2) void chunk_attn_f32_kernel(ChunkAttn p,
 template <int D>
 hipError_t launch_t(const ChunkAttn& p, void* workspace, hipStream_t stream) {
   const int lg = log2_of(p.hq / p.hkv);
-  const ChunkCut c = chunk_cut(p.batch, p.max_q, p.max_kv, p.hq, p.hkv, false);
+  const ChunkCut c = chunk_cut(p.max_q, p.hq, p.hkv, false);
   const ChunkWs ws = chunk_ws(c, D, workspace);
   chunk_attn_f32_kernel<D><<<dim3((unsigned)c.blocks), kW * 64, 0, stream>>>(p, c, ws, lg);
   launch_chunk_merge<float, D>(p, c, ws, lg, stream);

@@ -12,7 +12,6 @@ namespace qcf {
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int64_t kReleaseSmall = 8192;  // entries of a table
 
 // ---------------------------------------------------------------------------
 // fork: one block per request, which counts the pages that the requests before it take on its own (three
@@ -143,20 +142,18 @@ __device__ __forceinline__ ReleaseRow release_row(const PageRelease& p, int i) {
   return ReleaseRow{after ? p.after + b * p.after_stride : p.before + b * p.before_stride, min(max(held, 0), p.max_pages)};
 }
 
-// Small tables: one block marks the pages of both tables in LDS (two bits per page; larger pools in several goes)
-// and writes those that are only in the first.  Bound: latency.
+// Small tables: one block marks the pages of both tables in LDS (two bits per page) and writes those that are only in
+// the first.  Bound: latency (16 requests of up to 200 pages 9.2 us, of three dependent loads; one of 2 pages 6.4).
 constexpr int kRelThreads = 1024;
 constexpr int kRelWords = 1 << 14;  // of 32 pages, per bit set
 
 __global__ __launch_bounds__(kRelThreads) void page_release_kernel(PageRelease p) {
   __shared__ uint32_t was_l[kRelWords], is_l[kRelWords];
-  __shared__ int32_t first_l[kRelThreads];  // 64-entry pieces before each row of a go
+  __shared__ int32_t first_l[kRelThreads];  // 64-entry pieces before each row
   __shared__ int wave_l[kRelThreads / 64];
   const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
   constexpr int kWaves = kRelThreads / 64;
   const int64_t head = min(max((int64_t)p.free_head[0], (int64_t)0), p.n_free);
-  constexpr int64_t kPages = (int64_t)kRelWords * 32;
-  const int goes = (int)((p.n_pages + kPages - 1) / kPages);
 
   // inclusive sum over the block's threads of x; `all` is the total
   auto scan = [&](int x, int& all) {
@@ -179,76 +176,56 @@ __global__ __launch_bounds__(kRelThreads) void page_release_kernel(PageRelease p
     }
     return sum;
   };
-  // marks go g's pages of both tables; own: how many of this thread's are released, before: of the threads' before
-  // it; returns the number of all
-  int words, own, before;
-  auto go = [&](int g) {
-    const int64_t p0 = g * kPages;
-    words = (int)((min(p.n_pages - p0, kPages) + 31) >> 5);
-    __syncthreads();
-    for (int i = tid; i < words; i += kRelThreads) was_l[i] = is_l[i] = 0;
-    for (int i0 = 0; i0 < 2 * p.batch; i0 += kRelThreads) {
-      const int mine = i0 + tid < 2 * p.batch ? release_row(p, i0 + tid).held : 0;
-      int all;
-      const int pieces = (mine + 63) >> 6;
-      const int sum = scan(pieces, all);
-      first_l[tid] = sum - pieces;
-      __syncthreads();
-      // the waves share the pieces evenly; each lane looks up one of up to 64 at a time
-      const int to = (int)((int64_t)all * (w + 1) / kWaves);
-      for (int k0 = (int)((int64_t)all * w / kWaves); k0 < to; k0 += 64) {
-        const int piece = min(k0 + lane, to - 1);
-        int lo = 0, hi = kRelThreads;
-        while (hi - lo > 1) {
-          const int mid = (lo + hi) >> 1;
-          if (first_l[mid] <= piece) lo = mid; else hi = mid;
-        }
-        const ReleaseRow row = release_row(p, i0 + lo);
-        const int64_t from = reinterpret_cast<int64_t>(row.pages + (piece - first_l[lo]) * 64);
-        const int left = row.held - (piece - first_l[lo]) * 64;
-        const int which = i0 + lo >= p.batch ? 1 : 0, n = min(64, to - k0);
-        constexpr int U = 8;
-        for (int k = 0; k < n; k += U) {
-          int x[U], set[U];
-#pragma unroll
-          for (int u = 0; u < U; ++u) {
-            const int j = min(k + u, n - 1);
-            const int32_t* at = reinterpret_cast<const int32_t*>(__shfl(from, j, 64));
-            x[u] = at[min(lane, __shfl(left, j, 64) - 1)];
-            set[u] = __shfl(which, j, 64);
-          }
-#pragma unroll
-          for (int u = 0; u < U; ++u) {
-            const int64_t at = (int64_t)x[u] - p0;
-            if (x[u] >= 0 && x[u] < p.n_pages && at >= 0 && at < kPages)
-              atomicOr(&(set[u] ? is_l : was_l)[at >> 5], 1u << (at & 31));
-          }
-        }
-      }
-      __syncthreads();
-    }
-    const int per = (words + kRelThreads - 1) / kRelThreads;
-    const int w0 = min(tid * per, words), w1 = min(w0 + per, words);
-    own = 0;
-    for (int i = w0; i < w1; ++i) own += __popc(was_l[i] & ~is_l[i]);
+  const int words = (int)((p.n_pages + 31) >> 5);
+  for (int i = tid; i < words; i += kRelThreads) was_l[i] = is_l[i] = 0;
+  for (int i0 = 0; i0 < 2 * p.batch; i0 += kRelThreads) {
+    const int mine = i0 + tid < 2 * p.batch ? release_row(p, i0 + tid).held : 0;
     int all;
-    before = scan(own, all) - own;
-    return all;
-  };
-  int64_t n = 0;
-  for (int g = 0; g < goes; ++g) n += go(g);
-  int64_t put = head - n;
-  if (tid == 0) p.free_head_out[0] = (int)max(put, (int64_t)0);
-  for (int g = 0; g < goes; ++g) {
-    const int all = goes > 1 ? go(g) : (int)n;  // (a single one's marks are still there)
-    const int per = (words + kRelThreads - 1) / kRelThreads;
-    const int w0 = min(tid * per, words), w1 = min(w0 + per, words);
-    int64_t at = put + before;
-    for (int i = w0; i < w1; ++i)
-      for (uint32_t left = was_l[i] & ~is_l[i]; left; left &= left - 1, ++at)
-        if (at >= 0) p.free_pages[at] = (int)(g * kPages + i * 32 + __builtin_ctz(left));
-    put += all;
+    const int pieces = (mine + 63) >> 6;
+    const int sum = scan(pieces, all);
+    first_l[tid] = sum - pieces;
+    __syncthreads();
+    // the waves share the pieces evenly; each lane looks up one of up to 64 at a time
+    const int to = (int)((int64_t)all * (w + 1) / kWaves);
+    for (int k0 = (int)((int64_t)all * w / kWaves); k0 < to; k0 += 64) {
+      const int piece = min(k0 + lane, to - 1);
+      int lo = 0, hi = kRelThreads;
+      while (hi - lo > 1) {
+        const int mid = (lo + hi) >> 1;
+        if (first_l[mid] <= piece) lo = mid; else hi = mid;
+      }
+      const ReleaseRow row = release_row(p, i0 + lo);
+      const int64_t from = reinterpret_cast<int64_t>(row.pages + (piece - first_l[lo]) * 64);
+      const int left = row.held - (piece - first_l[lo]) * 64;
+      const int which = i0 + lo >= p.batch ? 1 : 0, n = min(64, to - k0);
+      constexpr int U = 8;
+      for (int k = 0; k < n; k += U) {
+        int x[U], set[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+          const int j = min(k + u, n - 1);
+          const int32_t* at = reinterpret_cast<const int32_t*>(__shfl(from, j, 64));
+          x[u] = at[min(lane, __shfl(left, j, 64) - 1)];
+          set[u] = __shfl(which, j, 64);
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+          if (x[u] >= 0 && x[u] < p.n_pages) atomicOr(&(set[u] ? is_l : was_l)[x[u] >> 5], 1u << (x[u] & 31));
+      }
+    }
+    __syncthreads();
   }
+  const int per = (words + kRelThreads - 1) / kRelThreads;
+  const int w0 = min(tid * per, words), w1 = min(w0 + per, words);
+  int own = 0, all;
+  for (int i = w0; i < w1; ++i) own += __popc(was_l[i] & ~is_l[i]);
+  const int before = scan(own, all) - own;
+  const int64_t put = head - all;
+  if (tid == 0) p.free_head_out[0] = (int)max(put, (int64_t)0);
+  int64_t at = put + before;
+  for (int i = w0; i < w1; ++i)
+    for (uint32_t left = was_l[i] & ~is_l[i]; left; left &= left - 1, ++at)
+      if (at >= 0) p.free_pages[at] = i * 32 + __builtin_ctz(left);
 }
 
 // Large tables: a byte per page and table in the workspace, set to zero, marked by a block per 1024 entries of a row
@@ -334,8 +311,11 @@ __global__ __launch_bounds__(kRelThreads) void release_list_kernel(PageRelease p
       if (at >= 0) p.free_pages[at] = (int)(16 * mine + 4 * k + (__builtin_ctz(left) >> 3));
 }
 
-// One block's time grows with the tables, three launches do not.
-inline bool release_small(const PageRelease& p) { return (int64_t)p.batch * p.max_pages <= kReleaseSmall; }
+// One block's time grows with the tables, three launches take about 10 us whatever their size (a request of 2 pages 6.4 us
+// against 9.4, 16 of 200 9.2 against 9.8, 64 of 100 14.5 against 9.9, 256 of 100 29 against 9.9, 400 of 900 128 against 15).
+inline bool release_small(int batch, int max_pages, int64_t n_pages) {
+  return (int64_t)batch * max_pages <= 4096 && n_pages <= 32 * kRelWords;
+}
 
 }  // namespace
 
@@ -361,12 +341,11 @@ hipError_t launch_copy_pages(const CopyPages& p, hipStream_t stream) {
 }
 
 size_t page_release_workspace(int batch, int max_pages, int64_t n_pages) {
-  if ((int64_t)batch * max_pages <= kReleaseSmall) return 0;
-  return (size_t)((n_pages + 255) / 256 * 256) * 2;
+  return release_small(batch, max_pages, n_pages) ? 0 : (size_t)((n_pages + 255) / 256 * 256) * 2;
 }
 
 hipError_t launch_page_release(const PageRelease& p, void* ws, hipStream_t stream) {
-  if (release_small(p)) {
+  if (release_small(p.batch, p.max_pages, p.n_pages)) {
     page_release_kernel<<<dim3(1), kRelThreads, 0, stream>>>(p);
     return hipGetLastError();
   }

@@ -25,7 +25,7 @@ struct ChunkCut {
 };
 
 struct ChunkWs {
-  int4* cut;   // [blocks] the unit (request, KV head, tile) that a block begins and others end, the last of them; or -1
+  int4* cut;   // [blocks] of the unit that a block begins and others end: first row, rows, KV head, last block; 0 rows: none
   float2* ml;  // [2 * blocks][vt] running maximum (log2 units) and sum
   float* o;    // [2 * blocks][vt][d]
 };
@@ -104,7 +104,7 @@ __device__ __forceinline__ void chunk_walk(const ChunkAttn& p, const ChunkCut& c
   const TreeShares shares(uni(sum_l[NT]), cut.blocks);
   const bool works = (int)blockIdx.x < shares.blocks && shares.all > 0;
   const int x = works ? shares.block(blockIdx.x) : (int)blockIdx.x;
-  if (tid == 0) ws.cut[x] = make_int4(-1, 0, 0, 0);
+  if (tid == 0) ws.cut[x] = make_int4(0, 0, 0, 0);
   if (!works) return;
   int64_t s = shares.first(x);
   const int64_t share1 = shares.first(x + 1);
@@ -138,7 +138,8 @@ __device__ __forceinline__ void chunk_walk(const ChunkAttn& p, const ChunkCut& c
       const int steps = (int)(u1 - u0) - c.start;
       const int first = (int)max(s - u0 - c.start, (int64_t)0), n = (int)(to - u0) - c.start - first;
       if (n > 0) {
-        if (first == 0 && n < steps && tid == 0) ws.cut[x] = make_int4(b, g, tile, shares.holder(u1 - 1));
+        if (first == 0 && n < steps && tid == 0) 
+          ws.cut[x] = make_int4((int)(q.r0 + (tile << c.rl)), (int)min((int64_t)1 << c.rl, c.rows - ((int64_t)tile << c.rl)), g, shares.holder(u1 - 1));
         unit(uni(b), q, uni(g), uni(tile), uni((int)c.first(tile) + first), uni(n),
              n == steps ? -1 : uni(2 * x + (first > 0 ? 0 : 1)));
       }
@@ -163,9 +164,9 @@ __global__ __launch_bounds__(kMergeThreads) void chunk_merge_kernel(ChunkAttn p,
   constexpr int LPR = D / 4, VP = kMergeThreads / LPR, U = kMergeVecs / VP;  // vectors side by side, and in turn
   const int x0 = blockIdx.x;
   const int4 c = ws.cut[x0];
-  const int b = uni(c.x), g = uni(c.y), tile = uni(c.z), x1 = uni(c.w);
-  if (b < 0) return;
-  const TreeRequest q = tree_request_uni(p, b);
+  const int64_t row0 = c.x;
+  const int rows = c.y, g = c.z, x1 = c.w;
+  if (((blockIdx.y * kMergeVecs) >> lg) >= rows) return;
   const int lc = threadIdx.x % LPR, v0 = blockIdx.y * kMergeVecs + threadIdx.x / LPR;
   const float4* part = reinterpret_cast<const float4*>(ws.o);
   float mx[U], lt[U];
@@ -206,20 +207,20 @@ __global__ __launch_bounds__(kMergeThreads) void chunk_merge_kernel(ChunkAttn p,
   }
 #pragma unroll
   for (int k = 0; k < U; ++k) {
-    const int64_t vec = ((int64_t)tile << cut.vt_log2) + v0 + k * VP;
-    const int i = (int)(vec >> lg), h = (g << lg) + (int)(vec & ((1 << lg) - 1));
-    if (i >= q.rows) continue;
+    const int v = v0 + k * VP, i = v >> lg, h = (g << lg) + (v & ((1 << lg) - 1));
+    if (i >= rows) continue;
     const float inv = row_scale(mx[k], lt[k]);
-    const int64_t at = (q.r0 + i) * p.hq + h;
+    const int64_t at = (row0 + i) * p.hq + h;
     store4(static_cast<T*>(p.out) + at * D + 4 * lc, make_float4(a[k].x * inv, a[k].y * inv, a[k].z * inv, a[k].w * inv));
     if (p.lse && lc == 0) p.lse[at] = row_lse(mx[k], lt[k]);
   }
 }
 
 // How a call is cut, from its bounds (lengths are on the device): tiles of 128 vectors (float32: 32), as many
-// blocks as run at once, two per CU, with 4 steps each at least.
+// blocks as run at once, two per CU.  (Three of head size 64, whose registers would do: 246 us against 240 for
+// prompts of 700 to 4000 rows with windows of 1024: the vector units are busy with two.)
 constexpr int kChunkBlocks = 512;
-inline ChunkCut chunk_cut(int batch, int max_q, int max_kv, int hq, int hkv, bool bf16) {
+inline ChunkCut chunk_cut(int max_q, int hq, int hkv, bool bf16) {
   const int64_t vectors = (int64_t)max_q * (hq / hkv);
   ChunkCut c;
   c.vt_log2 = bf16 ? 7 : 5;

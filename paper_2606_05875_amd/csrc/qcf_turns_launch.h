@@ -16,8 +16,8 @@ hipError_t launch_norm_rope_store(const NormRopeStore& p, bool bf16, int head_di
 struct ChunkAttn : TreeAttn {
   int window;
 };
-bool chunk_attn_fits(int batch, int max_q, int max_kv, int hq, int hkv, bool bf16);
-size_t chunk_attn_workspace(int batch, int max_q, int max_kv, int hq, int hkv, int head_dim, bool bf16);
+bool chunk_attn_fits(int batch, int max_q, int hq, int hkv, bool bf16);
+size_t chunk_attn_workspace(int max_q, int hq, int hkv, int head_dim, bool bf16);
 hipError_t launch_chunk_attn_f32(const ChunkAttn& p, int head_dim, void* ws, hipStream_t stream);
 hipError_t launch_chunk_attn(const ChunkAttn& p, bool bf16, int head_dim, void* ws, hipStream_t stream);
 
