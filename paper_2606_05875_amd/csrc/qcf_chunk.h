@@ -10,6 +10,8 @@
 // shares.  A block has at most two partial results: of a unit that others began (slot 2 x) and of one
 // that it begins (slot 2 x + 1), which it enters in a list for the merge.
 #pragma once
+#include <type_traits>
+
 #include "qcf_tree.h"
 #include "qcf_turns_launch.h"
 
@@ -155,65 +157,53 @@ __device__ __forceinline__ void chunk_walk(const ChunkAttn& p, const ChunkCut& c
 
 namespace {
 
-// The partial results of the units that are cut, in the blocks' order.  A block takes 32 query vectors of the unit that
-// block x0 begins; a thread sums four columns of a vector, for several vectors at a time, so that many
-// partials are asked for at once.  Bound: the partials' bytes.
-constexpr int kMergeThreads = 256, kMergeVecs = 32;
+// The partial results of the units that are cut, in the blocks' order.  A thread sums four columns of one query vector of
+// the unit that block x0 begins; the first two partials (most units have no more) go out at once, then eight at a time.
+// Bound: the partials' bytes, or latency.
+constexpr int kMergeThreads = 256;
 template <typename T, int D>
 __global__ __launch_bounds__(kMergeThreads) void chunk_merge_kernel(ChunkAttn p, ChunkCut cut, ChunkWs ws, int lg) {
-  constexpr int LPR = D / 4, VP = kMergeThreads / LPR, U = kMergeVecs / VP;  // vectors side by side, and in turn
-  const int x0 = blockIdx.x;
+  constexpr int LPR = D / 4, VP = kMergeThreads / LPR;  // vectors of a block
+  const int x0 = blockIdx.y;  // (the vectors along x: units are begun by blocks of one XCD where they are cut alike)
   const int4 c = ws.cut[x0];
   const int64_t row0 = c.x;
   const int rows = c.y, g = c.z, x1 = c.w;
-  if (((blockIdx.y * kMergeVecs) >> lg) >= rows) return;
-  const int lc = threadIdx.x % LPR, v0 = blockIdx.y * kMergeVecs + threadIdx.x / LPR;
+  const int lc = threadIdx.x % LPR, v = blockIdx.x * VP + threadIdx.x / LPR;
+  const int i = v >> lg, h = (g << lg) + (v & ((1 << lg) - 1));
+  if (i >= rows) return;
   const float4* part = reinterpret_cast<const float4*>(ws.o);
-  float mx[U], lt[U];
-  float4 a[U];
+  float mx = -INFINITY, lt = 0.f;
+  float4 a = make_float4(0.f, 0.f, 0.f, 0.f);
+  auto add = [&](auto count, int x) {
+    constexpr int J = decltype(count)::value;
+    float2 ml[J];
+    float4 o[J];
 #pragma unroll
-  for (int k = 0; k < U; ++k) {
-    mx[k] = -INFINITY;
-    lt[k] = 0.f;
-    a[k] = make_float4(0.f, 0.f, 0.f, 0.f);
-  }
-  for (int x = x0; x <= x1; x += 2) {
-    float2 ml[2][U];
-    float4 o[2][U];
-#pragma unroll
-    for (int j = 0; j < 2; ++j)
-#pragma unroll
-      for (int k = 0; k < U; ++k) {
-        const int y = min(x + j, x1);
-        const int64_t at = ((int64_t)(2 * y + (y == x0 ? 1 : 0)) << cut.vt_log2) + v0 + k * VP;
-        ml[j][k] = ws.ml[at];
-        o[j][k] = part[at * LPR + lc];
-      }
-#pragma unroll
-    for (int j = 0; j < 2; ++j) {
-      if (x + j > x1) break;
-#pragma unroll
-      for (int k = 0; k < U; ++k) {
-        const float mn = fmaxf(mx[k], ml[j][k].x);
-        const float fa = __builtin_amdgcn_exp2f(gap(mx[k], mn)), fo = __builtin_amdgcn_exp2f(gap(ml[j][k].x, mn));
-        mx[k] = mn;
-        lt[k] = fmaf(lt[k], fa, ml[j][k].y * fo);
-        a[k].x = fmaf(a[k].x, fa, o[j][k].x * fo);
-        a[k].y = fmaf(a[k].y, fa, o[j][k].y * fo);
-        a[k].z = fmaf(a[k].z, fa, o[j][k].z * fo);
-        a[k].w = fmaf(a[k].w, fa, o[j][k].w * fo);
-      }
+    for (int j = 0; j < J; ++j) {
+      const int y = min(x + j, x1);
+      const int64_t at = ((int64_t)(2 * y + (y == x0 ? 1 : 0)) << cut.vt_log2) + v;
+      ml[j] = ws.ml[at];
+      o[j] = part[at * LPR + lc];
     }
-  }
 #pragma unroll
-  for (int k = 0; k < U; ++k) {
-    const int v = v0 + k * VP, i = v >> lg, h = (g << lg) + (v & ((1 << lg) - 1));
-    if (i >= rows) continue;
-    const float inv = row_scale(mx[k], lt[k]);
-    const int64_t at = (row0 + i) * p.hq + h;
-    store4(static_cast<T*>(p.out) + at * D + 4 * lc, make_float4(a[k].x * inv, a[k].y * inv, a[k].z * inv, a[k].w * inv));
-    if (p.lse && lc == 0) p.lse[at] = row_lse(mx[k], lt[k]);
-  }
+    for (int j = 0; j < J; ++j) {
+      if (x + j > x1) break;
+      const float mn = fmaxf(mx, ml[j].x);
+      const float fa = __builtin_amdgcn_exp2f(gap(mx, mn)), fo = __builtin_amdgcn_exp2f(gap(ml[j].x, mn));
+      mx = mn;
+      lt = fmaf(lt, fa, ml[j].y * fo);
+      a.x = fmaf(a.x, fa, o[j].x * fo);
+      a.y = fmaf(a.y, fa, o[j].y * fo);
+      a.z = fmaf(a.z, fa, o[j].z * fo);
+      a.w = fmaf(a.w, fa, o[j].w * fo);
+    }
+  };
+  add(std::integral_constant<int, 2>{}, x0);
+  for (int x = x0 + 2; x <= x1; x += 8) add(std::integral_constant<int, 8>{}, x);
+  const float inv = row_scale(mx, lt);
+  const int64_t at = (row0 + i) * p.hq + h;
+  store4(static_cast<T*>(p.out) + at * D + 4 * lc, make_float4(a.x * inv, a.y * inv, a.z * inv, a.w * inv));
+  if (p.lse && lc == 0) p.lse[at] = row_lse(mx, lt);
 }
 
 // How a call is cut, from its bounds (lengths are on the device): tiles of 128 vectors (float32: 32), as many
@@ -251,7 +241,7 @@ inline ChunkWs chunk_ws(const ChunkCut& c, int d, void* workspace) {
 
 template <typename T, int D>
 inline void launch_chunk_merge(const ChunkAttn& p, const ChunkCut& c, const ChunkWs& ws, int lg, hipStream_t stream) {
-  chunk_merge_kernel<T, D><<<dim3((unsigned)c.blocks, (1u << c.vt_log2) / kMergeVecs), kMergeThreads, 0, stream>>>(p, c, ws, lg);
+  chunk_merge_kernel<T, D><<<dim3((1u << c.vt_log2) / (kMergeThreads / (D / 4)), (unsigned)c.blocks), kMergeThreads, 0, stream>>>(p, c, ws, lg);
 }
 
 }  // namespace
