@@ -18,11 +18,15 @@ namespace {
 constexpr int kThreads = 256;
 constexpr int kVec = 8;  // tokens of a thread at a time
 constexpr int kWaves = kThreads / 64;
+// Where the biases' entries are kept: nowhere, in the upper half of the tokens' counts, or, for long lists and histories
+// whose counts could pass 15 bits, beside them
+enum Bias { kNone, kPacked, kBeside };
 // Tokens of a block's piece: 32 KB of LDS for what is looked up of them
-constexpr int piece_of(bool bias) { return bias ? 4096 : 8192; }
+constexpr int piece_of(int bias) { return bias == kBeside ? 4096 : 8192; }
 constexpr int64_t kShapeBlocks = 2048;
 
-constexpr uint32_t kSaid = 1u << 31;  // of a token's count: it was said in the prompt
+// Of a token's word: it was said in the prompt; its count; where its bias begins (kPacked)
+constexpr uint32_t said_bit(int bias) { return bias == kPacked ? 1u << 15 : 1u << 31; }
 
 enum Mode { kLogits, kStats, kWrite, kWhole };
 
@@ -79,16 +83,17 @@ __device__ __forceinline__ void store8(T* p, const float (&x)[kVec]) {
   for (int i = 0; i < kVec; i += Vec16<T>::N) store16(p + i, Vec16<T>::pack(x + i));
 }
 
-// One piece of `per` consecutive rows.  A row's loads all go out before anything waits.
-template <typename In, typename Out, int kMode, bool kBias>
+// One piece of `per` consecutive rows.  A row's loads go out while the row before it is still worked on.
+template <typename In, typename Out, int kMode, int kBias>
 __global__ __launch_bounds__(kThreads, 4) void shape_kernel(ShapeLogits p, Stat* stats, int pieces, int per) {
   constexpr int kPiece = piece_of(kBias), kVecs = kPiece / (kThreads * kVec);
   __shared__ __attribute__((aligned(16))) uint32_t said_l[kPiece];
-  __shared__ __attribute__((aligned(16))) uint32_t bias_l[kBias ? kPiece : 4];
+  __shared__ __attribute__((aligned(16))) uint32_t bias_l[kBias == kBeside ? kPiece : 4];
+  constexpr uint32_t kSaid = said_bit(kBias), kCount = kSaid - 1;
   __shared__ Stat red_l[kWaves];
   const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
   const int64_t block = (int64_t)blockIdx.y << kGridLog2 | blockIdx.x;
-  const int64_t group = block / pieces;
+  const int64_t group = (uint64_t)block >> 32 ? block / pieces : (int64_t)((uint32_t)block / (uint32_t)pieces);
   const int64_t r_first = group * per, r_end = min(r_first + per, p.n_rows);
   if (r_first >= r_end) return;
   const int piece = (int)(block - group * pieces), p0 = piece * kPiece;
@@ -97,7 +102,7 @@ __global__ __launch_bounds__(kThreads, 4) void shape_kernel(ShapeLogits p, Stat*
   auto clear = [&]() {
     for (int i = tid; i < kPiece / 4; i += kThreads) {
       reinterpret_cast<uint4*>(said_l)[i] = make_uint4(0, 0, 0, 0);
-      if (kBias) reinterpret_cast<uint4*>(bias_l)[i] = make_uint4(0, 0, 0, 0);
+      if (kBias == kBeside) reinterpret_cast<uint4*>(bias_l)[i] = make_uint4(0, 0, 0, 0);
     }
   };
   clear();
@@ -219,12 +224,13 @@ __global__ __launch_bounds__(kThreads, 4) void shape_kernel(ShapeLogits p, Stat*
     if ((said[0] | said[1]) | (said[2] | said[3]) | (said[4] | said[5]) | (said[6] | said[7])) {
 #pragma unroll
       for (int e = 0; e < kVec; ++e) {
-        const float n = (float)(said[e] & ~kSaid), z = x[e];
-        const float by = said[e] ? z > 0.f ? inv_rep : rep : 1.f;
+        const float n = (float)(said[e] & kCount), z = x[e];
+        const float by = said[e] & (kSaid | kCount) ? z > 0.f ? inv_rep : rep : 1.f;
         x[e] = fmaf(z, by, -fmaf(freq, n, n > 0.f ? pres : 0.f));
+        if (kBias == kPacked && said[e] >> 16) x[e] += p.bias_value[bias0 + (said[e] >> 16) - 1];
       }
     }
-    if (kBias) {
+    if (kBias == kBeside) {
       uint32_t bias[kVec];
       *reinterpret_cast<uint4*>(bias) = *reinterpret_cast<const uint4*>(bias_l + at);
       *reinterpret_cast<uint4*>(bias + 4) = *reinterpret_cast<const uint4*>(bias_l + at + 4);
@@ -242,10 +248,12 @@ __global__ __launch_bounds__(kThreads, 4) void shape_kernel(ShapeLogits p, Stat*
     }
   };
 
-  for (int64_t r = r_first; r < r_end; ++r) {
-    Raw raw[kVecs];
+  Raw raw[kVecs], next[kVecs];
 #pragma unroll
-    for (int k = 0; k < kVecs; ++k) raw[k] = load(r, k);
+  for (int k = 0; k < kVecs; ++k) next[k] = load(r_first, k);
+  for (int64_t r = r_first; r < r_end; ++r) {
+#pragma unroll
+    for (int k = 0; k < kVecs; ++k) raw[k] = next[k];
     if (r > r_first) {
       while (b < p.batch && (int64_t)p.cu_rows[b + 1] <= r) ++b;
       meet();  // the last row's counts have been read
@@ -266,25 +274,32 @@ __global__ __launch_bounds__(kThreads, 4) void shape_kernel(ShapeLogits p, Stat*
       cold = temp == 0.f;
       c = cold ? 1.f : kLog2e / temp;
       meet();  // (the counts are zero)
+      if (kBias != kNone) {
+        bias0 = max(of(8), 0);
+        const int64_t bias1 = min((int64_t)of(9), p.n_bias);
+        for (int64_t e = bias0 + tid; e < bias1; e += kThreads) {
+          const uint32_t at = (uint32_t)p.bias_token[e] - (uint32_t)p0, entry = (uint32_t)(e - bias0) + 1u;
+          if (at < (uint32_t)kPiece) {
+            if (kBias == kPacked) atomicMax(&said_l[at], entry << 16);
+            else atomicMax(&bias_l[at], entry);
+          }
+        }
+        if (kBias == kPacked) meet();  // (the words are not compared any more)
+      }
       if (p.history) {
         const int n = min(max(of(2), 0), p.max_history), prompt = min(max(of(3), 0), n);
         const int32_t* h = p.history + (int64_t)b * p.history_stride;
         scan(h, 0, prompt, [&](uint32_t at) { atomicOr(&said_l[at], kSaid); });
         scan(h, prompt, n, [&](uint32_t at) { atomicAdd(&said_l[at], 1u); });
       }
-      if (kBias) {
-        bias0 = max(of(8), 0);
-        const int64_t bias1 = min((int64_t)of(9), p.n_bias);
-        for (int64_t e = bias0 + tid; e < bias1; e += kThreads) {
-          const uint32_t at = (uint32_t)p.bias_token[e] - (uint32_t)p0;
-          if (at < (uint32_t)kPiece) atomicMax(&bias_l[at], (uint32_t)(e - bias0) + 1u);
-        }
-      }
     } else if (p.tokens) {
       drafts(r - 1, (uint32_t)-1);
     }
     if (p.tokens) drafts(r, 1u);
     meet();
+    if (r + 1 < r_end)
+#pragma unroll
+      for (int k = 0; k < kVecs; ++k) next[k] = load(r + 1, k);
 
     Stat all{-INFINITY, 0.f, INT32_MAX, 0};
     if (kMode == kStats || kMode == kWhole) {
@@ -360,9 +375,9 @@ __global__ __launch_bounds__(kThreads, 4) void shape_kernel(ShapeLogits p, Stat*
   }
 }
 
-inline int pieces_of(int vocab, bool bias) { return (vocab + piece_of(bias) - 1) / piece_of(bias); }
+inline int pieces_of(int vocab, int bias) { return (vocab + piece_of(bias) - 1) / piece_of(bias); }
 
-template <typename In, typename Out, bool kBias>
+template <typename In, typename Out, int kBias>
 hipError_t launch_t(const ShapeLogits& p, bool probabilities, void* ws, hipStream_t stream) {
   const int pieces = pieces_of(p.vocab, kBias);
   // rows of a block: more share one count of the history, as long as the blocks fill the chip twice
@@ -382,14 +397,17 @@ hipError_t launch_t(const ShapeLogits& p, bool probabilities, void* ws, hipStrea
 
 template <typename In, typename Out>
 hipError_t launch_b(const ShapeLogits& p, bool probabilities, void* ws, hipStream_t stream) {
-  return p.bias_start ? launch_t<In, Out, true>(p, probabilities, ws, stream)
-                      : launch_t<In, Out, false>(p, probabilities, ws, stream);
+  if (!p.bias_start) return launch_t<In, Out, kNone>(p, probabilities, ws, stream);
+  // a token is counted once for each place of the history and for each row at most
+  if ((p.history ? p.max_history : 0) + (p.tokens ? p.n_rows : 0) < 1 << 15 && p.n_bias < 1 << 16)
+    return launch_t<In, Out, kPacked>(p, probabilities, ws, stream);
+  return launch_t<In, Out, kBeside>(p, probabilities, ws, stream);
 }
 
 }  // namespace
 
 size_t shape_logits_workspace(int64_t n_rows, int vocab) {
-  const int pieces = pieces_of(vocab, true);  // (the smaller pieces)
+  const int pieces = pieces_of(vocab, kBeside);  // (the smaller pieces)
   return pieces > 1 ? (size_t)n_rows * pieces * sizeof(Stat) : 0;
 }
 
