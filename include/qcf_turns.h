@@ -69,7 +69,7 @@ qcf_status qcf_norm_rope_store(void* k_cache, void* v_cache, int64_t n_slots, in
  * units as one bf16 number, after they entered the sum.  A row's bits do not depend on the other
  * rows' values.
  * Errors: as for qcf_tree_attn (all tiles of a batch, of 128 query vectors each, 32 in float32, of one
- * request and KV head, are fewer than 2^31: UNSUPPORTED).
+ * request and KV head, are fewer than 2^31, batch at most 2^30: UNSUPPORTED).
  */
 size_t qcf_chunk_attn_workspace_size(int batch, int max_q, int max_kv, int n_q_heads,
                                      int n_kv_heads, int head_dim, qcf_dtype dtype);
@@ -101,7 +101,7 @@ qcf_status qcf_chunk_attn(void* out, float* lse, const void* q, int64_t n_rows,
  * row of probabilities NaN (T = 0: a NaN z is passed over).  Everything is float32: the quotient by the repetition is the
  * product with its reciprocal, the exponential of z / T 2 to the power of z log2(e) / T, the quotient rounded once.
  *   out        [n_rows, vocab], rows out_stride elements apart, of type out_dtype; may be the logits
- *              themselves (same type and stride).  Rows at and behind cu_rows[batch] are neither read nor written
+ *              themselves (same type and stride).  Rows at and behind cu_rows[batch] are left as they are
  *   logits     [n_rows, vocab], rows logits_stride elements apart (any stride >= vocab), of type dtype.
  *              Both need only the alignment of their elements
  *   cu_rows    int32 [batch + 1], ascending from 0
@@ -117,12 +117,13 @@ qcf_status qcf_chunk_attn(void* out, float* lse, const void* q, int64_t n_rows,
  *              entries of a token the last counts
  *   allowed    uint32 [n_rows, allowed_words] or NULL: bit t % 32 of word t / 32 allows token t; 32 *
  *              allowed_words >= vocab
- *   temperature  float32 [batch] or NULL (1), not negative; not looked at where probabilities == 0
+ *   temperature  float32 [batch] or NULL (1), not negative; not looked at where probabilities == 0.  Where z / T
+ *              passes float32's range it is infinite, as any other z
  *   workspace  >= qcf_shape_logits_workspace_size(n_rows, vocab) bytes (may be 0), 256-byte
  *              aligned, no initialisation; calls that overlap in time need separate ones.  A size for
  *              more rows serves fewer.
- * Errors: null pointers, strides, vocab <= 0 or beyond 2^28 (UNSUPPORTED), parts that are not given together,
- * workspace.
+ * Errors: null pointers, strides, vocab <= 0 or beyond 2^28 (UNSUPPORTED), batch or max_history beyond 2^30
+ * (UNSUPPORTED), parts that are not given together, workspace.
  */
 size_t qcf_shape_logits_workspace_size(int64_t n_rows, int vocab);
 qcf_status qcf_shape_logits(void* out, int64_t out_stride, qcf_dtype out_dtype, const void* logits,
@@ -163,7 +164,7 @@ qcf_status qcf_shape_logits(void* out, int64_t out_stride, qcf_dtype out_dtype, 
  * n_pages), the new entry is -1 and there is no copy.  A source's page outside the pool stays what it is,
  * and nothing is taken or copied for it.
  * Errors: null pointers, page_size not a power of two (UNSUPPORTED), n_pages * page_size beyond int32,
- * batch of 2^22 and more (UNSUPPORTED), outputs that are inputs.
+ * batch of 2^22 and more (UNSUPPORTED), outputs that are inputs or one another.
  */
 qcf_status qcf_page_fork(int32_t* table_out, int64_t table_out_stride, int32_t* kv_out,
                          int32_t* held_out, const int32_t* block_table, int64_t table_stride,

@@ -73,7 +73,7 @@ qcf_status qcf_chunk_attn(void* out, float* lse, const void* q, int64_t n_rows,
   if (!(softmax_scale > 0.f) || !isfinite(softmax_scale)) return QCF_ERR_INVALID_ARG;
   if (!kv_stride_ok(kv_row_stride, n_kv_heads, head_dim, dtype)) return QCF_ERR_INVALID_ARG;
   // the kernels' 32-bit numbers: offsets inside 16 rows, (row, head) pairs, tokens a few tiles on
-  if (kv_row_stride > INT32_MAX / (16 * esize(dtype)) || max_kv > INT32_MAX - (1 << 21) || max_q > 1 << 20 ||
+  if (kv_row_stride > INT32_MAX / (16 * esize(dtype)) || max_kv > INT32_MAX - (1 << 21) || max_q > 1 << 20 || batch > 1 << 30 ||
       !qcf::chunk_attn_fits(batch, max_q, n_q_heads, n_kv_heads, dtype == QCF_BF16))
     return QCF_ERR_UNSUPPORTED;
   const bool empty = n_rows == 0 || batch == 0 || max_q == 0;
@@ -115,7 +115,8 @@ qcf_status qcf_shape_logits(void* out, int64_t out_stride, qcf_dtype out_dtype, 
   if (n_rows < 0 || n_rows > INT32_MAX || vocab <= 0 || batch < 0 || out_stride < vocab || logits_stride < vocab ||
       max_history < 0 || n_bias < 0 || n_bias > INT32_MAX)
     return QCF_ERR_INVALID_ARG;
-  if (vocab > qcf::kShapeMaxVocab) return QCF_ERR_UNSUPPORTED;
+  // (the kernels' 32-bit counters run a few blocks' width past their ends)
+  if (vocab > qcf::kShapeMaxVocab || batch > 1 << 30 || max_history > 1 << 30) return QCF_ERR_UNSUPPORTED;
   const bool empty = n_rows == 0 || batch == 0;
   if (!element_ok(out, empty, out_dtype) || !element_ok(logits, empty, dtype) || !index_ok(cu_rows, empty))
     return QCF_ERR_INVALID_ARG;
@@ -164,9 +165,12 @@ qcf_status qcf_page_fork(int32_t* table_out, int64_t table_out_stride, int32_t* 
   // outputs that other blocks still read as inputs
   const void* in[] = {block_table, kv_len, source, keep_len, free_pages, free_head};
   const void* result[] = {table_out, kv_out, held_out, free_head_out, copy_src, copy_dst, copy_rows};
-  for (const void* x : in)
-    for (const void* y : result)
-      if (x && x == y) return QCF_ERR_INVALID_ARG;
+  for (size_t i = 0; i < sizeof result / sizeof *result; ++i) {
+    for (const void* x : in)
+      if (x && x == result[i]) return QCF_ERR_INVALID_ARG;
+    for (size_t j = 0; j < i; ++j)
+      if (result[j] && result[j] == result[i]) return QCF_ERR_INVALID_ARG;
+  }
   const qcf::PageFork p{table_out, table_out_stride, kv_out, held_out, block_table, table_stride, max_pages, batch,
                         kv_len, source, keep_len, free_pages, n_free, free_head, n_pages, lp, free_head_out, copy_src,
                         copy_dst, copy_rows};
@@ -219,8 +223,9 @@ qcf_status qcf_page_release(const int32_t* table_before, int64_t before_stride,
     if (x && (x == free_head_out || x == free_pages)) return QCF_ERR_INVALID_ARG;
   const size_t need = qcf_page_release_workspace_size(batch, max_pages, n_pages);
   if (workspace_bytes < need || (need > 0 && (!workspace || !aligned256(workspace)))) return QCF_ERR_WORKSPACE;
+  // without a table no page is held, whatever the pool: the workspace is not there then
   const qcf::PageRelease p{table_before, before_stride, held_before, table_after, after_stride, held_after, max_pages,
-                           batch, free_pages, n_free, free_head, free_head_out, n_pages};
+                           batch, free_pages, n_free, free_head, free_head_out, no_table ? 0 : n_pages};
   return hip_status(qcf::launch_page_release(p, workspace, stream));
 }
 

@@ -143,8 +143,8 @@ __global__ __launch_bounds__(kThreads, 4) void shape_kernel(ShapeLogits p, Stat*
   // adds (1) or takes back (-1) the drafted tokens that row r follows
   auto drafts = [&](int64_t r, uint32_t what) {
     const uint32_t* m = p.tree_mask ? p.tree_mask + r * p.mask_words : nullptr;
-    const int end = m ? (int)min(last - first, (int64_t)p.mask_words * 32) : (int)(r - first) + 1;
-    for (int j = tid; j < end; j += kThreads) {
+    const uint32_t end = (uint32_t)max(m ? min(last - first, (int64_t)p.mask_words * 32) : r - first + 1, (int64_t)0);
+    for (uint32_t j = tid; j < end; j += kThreads) {
       const uint32_t at = (uint32_t)p.tokens[first + j] - (uint32_t)p0;
       if (at < (uint32_t)kPiece && (!m || (m[j >> 5] >> (j & 31) & 1))) atomicAdd(&said_l[at], what);
     }

@@ -135,7 +135,7 @@ def test_norm_rope_store_refuses():
 # -- logits ------------------------------------------------------------------------
 def _shape(new, hist, vocab, dtype="f32", out="f32", penalties=True, bias=0, grammar=False, tree=False, temps=None,
            pad=(0, 0), seed=0, probabilities=True, tokens=True, spare=2, offset=0, z=None, in_place=False, words=None,
-           width=None, rep=None, allow=None, ws=None, prompts=None):
+           width=None, rep=None, allow=None, ws=None, prompts=None, same=None):
     rng = np.random.default_rng(seed)
     B, n = len(new), int(sum(new))
     cu = cum(new)
@@ -154,6 +154,8 @@ def _shape(new, hist, vocab, dtype="f32", out="f32", penalties=True, bias=0, gra
     history = rng.integers(-2, min(vocab + 2, 60), (B, width))
     if width > 5:
         history[:, 3] = vocab - 1
+    if same is not None:
+        history[:] = same
     prompt = np.array([int(h * rng.random()) for h in hist]) if prompts is None else np.array(prompts)
     toks = rng.integers(-1, min(vocab + 1, 70), rows)
     if penalties:
@@ -257,6 +259,19 @@ def test_shape_logits(dtype, out, probabilities):
     _shape([1], [40], 8193, seed=9, grammar=True, allow=True, **kw)
     _shape([2, 1], [0, 0], 16384, seed=10, width=0, **kw)
     _shape([1, 1], [9, 9], 300, seed=11, prompts=[-4, 100], **kw)
+
+
+@pytest.mark.parametrize("probabilities", [True, False])
+def test_shape_logits_long_histories_and_lists(probabilities):
+    """Counts of up to 15 bits and beyond, lists of more than 16 bits of entries."""
+    say("shape logits, long histories and lists", probabilities)
+    kw = dict(probabilities=probabilities, tokens=True)
+    _shape([2, 1], [32760, 4], 9000, width=32762, same=7, bias=40, seed=21, **kw)     # 15 bits at most
+    _shape([2, 1], [32760, 40000], 9000, same=7, bias=40, seed=22, **kw)
+    _shape([1, 2], [33000, 9], 4100, dtype="bf16", bias=300, grammar=True, seed=23, **kw)
+    _shape([1, 1, 1, 1], [20] * 4, 20011, bias=70000, seed=24, **kw)
+    _shape([3], [40000], 3000, tree=True, seed=25, **kw)
+    _shape([5, 4], [40000, 70000], 70003, tree=True, bias=100, pad=(1, 0), offset=3, grammar=True, seed=26, **kw)
 
 
 def test_shape_logits_in_place_and_many_requests():
@@ -457,3 +472,5 @@ def test_page_release_large_pools():
     _release(np.zeros((0, 4), int), [], np.zeros((0, 4), int), [], np.arange(5), 3, 10)
     _release(np.zeros((3, 0), int), [1, 0, 2], np.zeros((3, 0), int), [0, 0, 0], np.arange(5), 3, 10)
     _release(np.zeros((1, 4), int), [2], np.zeros((1, 4), int), [0], np.arange(5), 3, 0)
+    _release(np.zeros((0, 4), int), [], np.zeros((0, 4), int), [], np.arange(5), 3, 1 << 20)
+    _release(np.zeros((3, 0), int), [1, 0, 2], np.zeros((3, 0), int), [0, 0, 0], np.arange(5), 7, 1 << 20)

@@ -73,7 +73,8 @@ def test_chunk_attn_refusals(L):
                 dict(batch=-1), dict(max_q=-1), dict(max_kv=-1), dict(slots=-1), dict(hq=36)):
         assert call(**bad) == INVALID, bad
     for bad in (dict(dt=5), dict(d=96), dict(hq=24), dict(ps=48), dict(ps=8), dict(ps=1), dict(stride=1 << 26),
-                dict(max_kv=2 ** 31 - 5), dict(max_q=(1 << 20) + 1), dict(batch=1 << 20, max_q=1 << 20)):
+                dict(max_kv=2 ** 31 - 5), dict(max_q=(1 << 20) + 1), dict(batch=1 << 20, max_q=1 << 20),
+                dict(batch=(1 << 30) + 1, max_q=1, hq=8)):
         assert call(**bad) == UNSUPPORTED, bad
     if need:
         for bad in (dict(ws=None), dict(ws=A + 16), dict(wsb=need - 1)):
@@ -116,6 +117,7 @@ def test_shape_logits_refusals(L):
         assert call(**bad) == INVALID, bad
     assert call(dt=3) == UNSUPPORTED and call(odt=2) == UNSUPPORTED
     assert call(vocab=(1 << 28) + 1, os=1 << 29, zs=1 << 29) == UNSUPPORTED
+    assert call(batch=(1 << 30) + 1) == UNSUPPORTED and call(width=(1 << 30) + 1, hs=1 << 31) == UNSUPPORTED
     for bad in (dict(ws=None), dict(ws=A + 16), dict(wsb=need - 1)):
         assert call(**bad) == WORKSPACE, bad
     for nothing in (dict(n=0), dict(batch=0)):
@@ -132,7 +134,8 @@ def test_page_fork_refusals(L):
     for bad in (dict(to=None), dict(kvo=None), dict(ho=None), dict(table=None), dict(kv=None), dict(src=None),
                 dict(free=None), dict(fo=None), dict(cs=None), dict(cd=None), dict(cr=None), dict(tos=9), dict(ts=9),
                 dict(batch=-1), dict(n_free=-1), dict(pages=-1), dict(ps=0), dict(pages=1 << 28), dict(to=B),
-                dict(kvo=B + 64), dict(ho=B + 64), dict(head=A + 192), dict(keep=A + 64), dict(fo=C), dict(kv=MIS + 1)):
+                dict(kvo=B + 64), dict(ho=B + 64), dict(head=A + 192), dict(keep=A + 64), dict(fo=C), dict(kv=MIS + 1),
+                dict(kvo=A), dict(cs=A + 128), dict(cr=A + 320), dict(fo=A + 64)):
         assert call(**bad) == INVALID, bad
     assert call(ps=24) == UNSUPPORTED and call(batch=1 << 22) == UNSUPPORTED
 
