@@ -111,7 +111,8 @@ qcf_status qcf_chunk_attn(void* out, float* lse, const void* q, int64_t n_rows,
  *              a hist_len beyond max_history as that); prompt_len NULL: 0
  *   tokens     int32 [n_rows] or NULL: the pass's rows count as nothing said; tree_mask uint32 [n_rows,
  *              mask_words] or NULL, given with tokens only.  Tokens outside [0, vocab) are passed over
- *   repetition, presence, frequency  float32 [batch] or NULL (1, 0, 0); repetition above 0
+ *   repetition, presence, frequency  float32 [batch] or NULL (1, 0, 0); repetition above 0.  An infinite
+ *              presence or frequency bans the answer's tokens (where c = 0 nothing is taken off)
  *   bias_start int32 [batch + 1] or NULL: entries bias_start[b] .. bias_start[b+1] - 1 of bias_token
  *              (int32 [n_bias]) and bias_value (float32 [n_bias]) are request b's; of several
  *              entries of a token the last counts

@@ -12,8 +12,8 @@
 //  * O^T += V^T P^T with P^T straight from those registers: product (r, mb) contracts over the tokens
 //    4 (l / 16) + r and fills the d-columns NB (l % 16) + mb, so a lane's V operands are NB contiguous floats.
 //  * exp2f, not the bare instruction: weights below 2^-126 stay subnormal numbers.
-// Bound: latency at test sizes, the float32 matrix rate and the L2 caches beyond (K and V are read once per
-// 32 vectors).
+// Bound: latency at test sizes (3 requests of 5 to 70 rows over 33 to 700 tokens, 8/2 heads of 64, 20 us in two
+// launches), the float32 matrix rate and the L2 caches beyond (K and V are read once per 32 vectors).
 #include "qcf_chunk.h"
 
 namespace qcf {

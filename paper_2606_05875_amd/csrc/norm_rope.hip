@@ -5,7 +5,8 @@
 // head lie in the lanes of one wave: a unit of work is a pair of 16-byte vectors of one head (the two halves'
 // partners, or, interleaved or not turned, two vectors side by side), a head's units are consecutive
 // lanes, and its sum of squares takes log2(units) exchanges between them, so a row is read and written once.
-// Bound: HBM for prompts, launch and dependent loads for single rows.
+// Bound: HBM for prompts (32896 rows of 64/8 heads of 128 in bf16 241 us, 5.6 TB/s), launch and dependent loads for
+// single rows (48 rows of 32/8 heads 4.7 us).
 #include "qcf_device.h"
 #include "qcf_turns_launch.h"
 
@@ -16,7 +17,8 @@ constexpr int kThreads = 256;
 constexpr int kAhead = 3;    // units of a thread that are asked for before the angles are formed
 constexpr int kMaxRows = 8;  // rows of a block
 
-// 2^rows_log2 rows per block (kMulti: more than one, for rows of few units)
+// 2^rows_log2 rows per block (kMulti: more than one, for rows of few units that would be more than 512 blocks: 2500 rows of
+// 8/2 heads of 64 5.1 us against 7.2 with a block each, 32896 rows 29 against 65, 1000 rows 4.4 against 4.6)
 template <typename T, int D, bool kInter, bool kMulti>
 __global__ __launch_bounds__(kThreads, 4) void norm_rope_store_kernel(NormRopeStore p, int rows_log2) {
   constexpr int VEC = Vec16<T>::N;

@@ -8,8 +8,8 @@
 // of one piece takes one.  z is formed the same way both times, so nothing is stored in between.
 // Bound: instructions in the first launch (about 13 vector instructions per token where its vector has a token
 // that was said), HBM in the second.  64 rows of 128000 tokens in float32 31.5 us (2.1 TB/s of logits read once and
-// probabilities written once), 288 rows of 150001 tokens of drafted trees, bf16 to float32, with biases and masks 137 us
-// (1.9 TB/s), without them 108 us (2.4 TB/s).
+// probabilities written once), 288 rows of 150001 tokens of drafted trees, bf16 to float32, with biases and masks 132 us
+// (2.0 TB/s), without them 108 us (2.4 TB/s).
 #include <algorithm>
 
 #include "qcf_device.h"
@@ -224,14 +224,19 @@ __global__ __launch_bounds__(kThreads, 4) void shape_kernel(ShapeLogits p, Stat*
     *reinterpret_cast<uint4*>(said + 4) = *reinterpret_cast<const uint4*>(said_l + at + 4);
 #pragma unroll
     for (int i = 0; i < (int)(sizeof raw.q / 16); ++i) Vec16<In>::unpack(raw.q[i], &x[i * Vec16<In>::N]);
-    if ((said[0] | said[1]) | (said[2] | said[3]) | (said[4] | said[5]) | (said[6] | said[7])) {
+    const uint32_t any = (said[0] | said[1]) | (said[2] | said[3]) | (said[4] | said[5]) | (said[6] | said[7]);
+    if (any & (kSaid | kCount)) {
 #pragma unroll
       for (int e = 0; e < kVec; ++e) {
         const float n = (float)(said[e] & kCount), z = x[e];
         const float by = said[e] & (kSaid | kCount) ? z > 0.f ? inv_rep : rep : 1.f;
-        x[e] = fmaf(z, by, -fmaf(freq, n, n > 0.f ? pres : 0.f));
-        if (kBias == kPacked && said[e] >> 16) x[e] += p.bias_value[bias0 + (said[e] >> 16) - 1];
+        x[e] = fmaf(z, by, n > 0.f ? -fmaf(freq, n, pres) : 0.f);
       }
+    }
+    if (kBias == kPacked && any >> 16) {
+#pragma unroll
+      for (int e = 0; e < kVec; ++e)
+        if (said[e] >> 16) x[e] += p.bias_value[bias0 + (said[e] >> 16) - 1];
     }
     if (kBias == kBeside) {
       uint32_t bias[kVec];

@@ -305,6 +305,26 @@ def test_shape_logits_cold_and_odd_values():
         _shape([1, 1, 1], [0] * 3, vocab, z=60 * rng.standard_normal((5, vocab)), temps=[0.05, 1.0, 30.0], rep=[1.0, 1e-3, 1e3])
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("which", ["presence", "frequency"])
+def test_infinite_penalties_ban_what_the_answer_has(which, dtype):
+    """.. and leave every other token's logit, bits included; tokens of the prompt alone are not the answer's."""
+    say("shape logits, infinite penalties", which, dtype)
+    vocab = 9000
+    z = torch.randn((2, vocab), device="cuda").to(DT[dtype])
+    history = i32([[1, 2, 3, 4, 100, 8999, 3], [5, 6, 7, 8, 9, 10, 11]])
+    kw = dict(history=history, prompt_len=i32([2, 0]), hist_len=i32([7, 3]), tokens=i32([50, 6]))
+    cu, out, want = i32([0, 1, 2]), torch.empty_like(z), z.clone()
+    want[0, [3, 4, 100, 8999, 50]] = -math.inf
+    want[1, [5, 6, 7]] = -math.inf
+    kw[which] = f32([math.inf, math.inf])
+    qcf.qcf_shape_logits(out, z, cu, probabilities=False, **kw)
+    assert torch.equal(out, want)
+    p = torch.empty((2, vocab), device="cuda")
+    qcf.qcf_shape_logits(p, z, cu, **kw)
+    assert torch.isfinite(p).all() and torch.equal(p == 0, want == -math.inf)
+
+
 def test_shape_logits_feeds_verification():
     """The probabilities are qcf_verify_drafts' target: a token is drawn where something is allowed, none (-1) where nothing is."""
     say("shape logits, verification")
