@@ -130,8 +130,8 @@ class TurnStep(DraftStep):
     def shape(self, logits, tokens=None, history=None, prompt_len=None, **shaping):
         """``target`` [max_rows, vocab] <- the probabilities of the model's logits [max_rows, vocab] after the planned
         rows.  ``tokens`` are the rows' tokens and ``history`` [batch, width] those of the requests' cached tokens, in
-        their order, of which the first prompt_len[b] count as the prompt; the rest as qcf.qcf_shape_logits
-        takes it (repetition, presence, frequency, bias_*, allowed, temperature)."""
+        their order, of which the first prompt_len[b] count as the prompt (so before ``commit``); the rest as
+        qcf.qcf_shape_logits takes it (repetition, presence, frequency, bias_*, allowed, temperature)."""
         self._shaping(logits.shape[1])
         qcf.qcf_shape_logits(self.target, logits, self.cu, history=history, prompt_len=prompt_len,
                              hist_len=None if history is None else self.cache.kv_len, tokens=tokens,
