@@ -8,14 +8,16 @@
 // tile's S run beside this tile's exponentials.
 //
 // Keys and values go from the pages into LDS without passing registers, two stages of each: step t asks for
-// K(t+2) and V(t+1) in between the products of S(t+1), and ends by waiting for them.  Wave w copies the tile's
+// K(t+2) and V(t+1) before anything else and ends by waiting for them (in between the products of S(t+1), as the contiguous
+// kernels do, the 16 questions below took 252 us in place of 247: pages are rarely in the L2).  Wave w copies the tile's
 // rows 16 w .. + 15, which lie in one page; the page numbers of a tile's four groups come by one load, a step
 // ahead of the copies.
 // Two blocks per CU: one's products run beside the other's exponentials, starts and ends.
 // Bound: matrix units and vector units together, where tiles are whole and long: 2048 rows over 30848 tokens, 64/8 heads
-// of 128, 2045 us, 1.04 PFLOP/s.  16 questions of 16 to 128 rows over 2000 to 12700 tokens (32/8 heads) 252 us, 0.67
-// PFLOP/s: tiles of 32 rows are rounded up, units of a few tiles start and end, some are merged.  Head size 64 does half
-// the products per exponential: prompts of 700 to 4000 rows with windows of 1024, 236 us, 0.51 PFLOP/s.
+// of 128, 2045 us, 1.04 PFLOP/s.  16 questions of 16 to 128 rows over 2000 to 12700 tokens (32/8 heads) 245 us, 0.69
+// PFLOP/s: tiles of 32 rows are rounded up, units of a few tiles start and end, some are merged, and a fifth is waiting for
+// pages (202 us with all tokens in the same few).  Head size 64 does half
+// the products per exponential: prompts of 700 to 4000 rows with windows of 1024, 231 us, 0.52 PFLOP/s.
 #include "qcf_chunk.h"
 #include "qcf_paged.h"
 
@@ -191,12 +193,10 @@ __global__ __launch_bounds__(kW * 64, 2) void chunk_attn_kernel(ChunkAttn p, Chu
     typedef float f32x2_t __attribute__((ext_vector_type(2)));
     typedef __bf16 bf16x2_t __attribute__((ext_vector_type(2)));
     // P of the tile; with kNext S of the next one beside it: one product per fenced group with its K fragment
-    // read four groups ahead, a group's arguments, exponentials and sums in three groups in turn, and the copies of
-    // K(t+2) and V(t+1) in between
-    auto weights = [&](auto next_s, const uint8_t* kn, f32x16 (&sn)[2], f32x16 (&s)[2], bf16x8 (&pb)[2][2], int t,
-                       uint64_t ak, uint64_t av) {
+    // read four groups ahead, a group's arguments, exponentials and sums in three groups in turn
+    auto weights = [&](auto next_s, const uint8_t* kn, f32x16 (&sn)[2], f32x16 (&s)[2], bf16x8 (&pb)[2][2]) {
       constexpr bool kNext = decltype(next_s)::value;
-      constexpr int NM = 2 * NS, EG = 32 / NM, PF = 4, DSTEP = NM / (2 * GC);
+      constexpr int NM = 2 * NS, EG = 32 / NM, PF = 4;
       const float nm = -finite(m), sc = big ? 1.f : scale2;
       float psum = 0.f, x[32], pw[32];
       bf16x8 kf[NM];
@@ -225,13 +225,6 @@ __global__ __launch_bounds__(kW * 64, 2) void chunk_attn_kernel(ChunkAttn p, Chu
         __builtin_amdgcn_sched_barrier(0);
         if (kNext) {
           if (i + PF < NM) kf[i + PF] = k_frag(kn, i + PF);
-          if (i % DSTEP == 0) {
-            if (i / DSTEP < GC) {
-              copy_k(t + 2, ak, i / DSTEP);  // (behind the last tile from the pool's first rows, for nobody)
-            } else {
-              copy_v(t + 1, av, i / DSTEP - GC);
-            }
-          }
           sn[i / NS] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[i], qreg[i % NS], i % NS == 0 ? f32x16{} : sn[i / NS], 0, 0, 0);
         }
         if (i + 1 < NM) arg(i + 1);
@@ -323,9 +316,13 @@ __global__ __launch_bounds__(kW * 64, 2) void chunk_attn_kernel(ChunkAttn p, Chu
       next = look(t + 3);
       bf16x8 pb[2][2];
       const uint64_t ak = base_of(t + 2, page2), av = base_of(t + 1, page1);
+#pragma unroll
+      for (int i = 0; i < GC; ++i) copy_k(t + 2, ak, i);
+#pragma unroll
+      for (int i = 0; i < GC; ++i) copy_v(t + 1, av, i);
       maximum(s, true);
       __builtin_amdgcn_s_setprio(1);
-      weights(std::true_type{}, k_ring + ((t + 1) & 1) * TB, sn, s, pb, t, ak, av);
+      weights(std::true_type{}, k_ring + ((t + 1) & 1) * TB, sn, s, pb);
       __builtin_amdgcn_s_setprio(0);
       products_o(v_ring + (t & 1) * TB, pb);
       meet();
@@ -367,7 +364,7 @@ __global__ __launch_bounds__(kW * 64, 2) void chunk_attn_kernel(ChunkAttn p, Chu
         }
         maximum(s, sees != 0);
         bf16x8 pb[2][2];
-        weights(std::false_type{}, k_ring, s, s, pb, t, ak, av);
+        weights(std::false_type{}, k_ring, s, s, pb);
         if (loose) {
           add_loose(t, loose, sees, s);
           take_out(t, loose);
