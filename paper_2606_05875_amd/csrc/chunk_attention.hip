@@ -17,7 +17,7 @@
 // of 128, 2045 us, 1.04 PFLOP/s.  16 questions of 16 to 128 rows over 2000 to 12700 tokens (32/8 heads) 245 us, 0.69
 // PFLOP/s: tiles of 32 rows are rounded up, units of a few tiles start and end, some are merged, and a fifth is waiting for
 // pages (202 us with all tokens in the same few).  Head size 64 does half
-// the products per exponential: prompts of 700 to 4000 rows with windows of 1024, 231 us, 0.52 PFLOP/s.
+// the products per exponential: prompts of 700 to 4000 rows with windows of 1024, 226 us, 0.53 PFLOP/s.
 #include "qcf_chunk.h"
 #include "qcf_paged.h"
 
