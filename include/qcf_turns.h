@@ -60,7 +60,8 @@ qcf_status qcf_norm_rope_store(void* k_cache, void* v_cache, int64_t n_slots, in
  *   page_size  at least 16 (UNSUPPORTED below)
  *   window     >= 0; 0: all tokens
  *   max_q      >= every cu_q[b+1] - cu_q[b] (further rows are left alone), at most 2^20 (UNSUPPORTED)
- *   workspace  >= qcf_chunk_attn_workspace_size(...) bytes (may be 0), 256-byte aligned: partial results
+ *   workspace  >= qcf_chunk_attn_workspace_size(...) bytes, 256-byte aligned, wherever there are rows (max_kv = 0
+ *              among them: rows that see no token): partial results
  *              of long tiles that are cut over blocks, merged in order by a second kernel
  *              (deterministic).  It needs no initialisation and keeps nothing; calls that
  *              overlap in time need separate ones.  The size for (batch, max_q, max_kv) covers

@@ -50,7 +50,8 @@ qcf_status qcf_norm_rope_store(void* k_cache, void* v_cache, int64_t n_slots, in
 size_t qcf_chunk_attn_workspace_size(int batch, int max_q, int max_kv, int n_q_heads,
                                      int n_kv_heads, int head_dim, qcf_dtype dtype) {
   if (!dtype_ok(dtype) || check_heads(n_q_heads, n_kv_heads, head_dim) != QCF_OK) return 0;
-  if (batch <= 0 || max_q <= 0 || max_kv <= 0) return 0;
+  // (rows that see no token go through the same kernels: max_kv does not matter)
+  if (batch <= 0 || max_q <= 0 || max_kv < 0) return 0;
   return qcf::chunk_attn_workspace(max_q, n_q_heads, n_kv_heads, head_dim, dtype == QCF_BF16);
 }
 

@@ -115,6 +115,25 @@ def test_missing_pages_and_short_bounds(dtype, ps, window):
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("d,window", [(64, 0), (128, 20)])
+def test_no_tokens_at_all(dtype, d, window):
+    """max_kv = 0, or an empty pool: every row gives zeros and a log-sum-exp of -infinity; a workspace of the asked size is
+    enough, and nothing is written behind it."""
+    say("chunk attention without tokens", dtype, d, window)
+    x = Chunk([300, 0, 40, 7], [60, 9, 0, 200], 8, 2, d, dtype, 16, window, seed=14)
+    rows = int(x.cu[-1])
+    need = qcf.qcf_chunk_attn_workspace_size(4, 200, 0, 8, 2, d, DT[dtype])
+    ws = torch.full((need + 512,), 0x5A, dtype=torch.uint8, device="cuda")
+    for how in (dict(max_kv=0, ws=ws[:need]), dict(max_kv=0), dict(max_kv=0, table=x.table[:, :0])):
+        o, e = x.call(**how)
+        assert (o[:rows] == 0).all() and (e[:rows] == -math.inf).all() and (o[rows:] == 5.0).all() and (e[rows:] == 5.0).all()
+    x.k, x.v = x.k[:0], x.v[:0]
+    o, e = x.call()
+    assert (o[:rows] == 0).all() and (e[:rows] == -math.inf).all()
+    assert (ws[need:] == 0x5A).all()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
 def test_logits_of_any_size(dtype):
     """One row and head with logits beyond 2^28: the others' bits are those of a call without it; rows that see only
     logits of -infinity or NaN are NaN."""

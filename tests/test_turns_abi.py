@@ -83,6 +83,33 @@ def test_chunk_attn_refusals(L):
         assert call(**nothing, out=None, q=None, ws=None, wsb=0) == OK
 
 
+def test_chunk_attn_without_tokens_needs_its_workspace(L):
+    """Rows that see no token (max_kv = 0, no table, no pool) go through the same kernels, which use the workspace."""
+    for dt in (F32, BF16):
+        for d in (64, 128):
+            need = L.qcf_chunk_attn_workspace_size(4, 8, 0, 32, 8, d, dt)
+            assert 0 < need <= L.qcf_chunk_attn_workspace_size(4, 8, 1, 32, 8, d, dt)
+
+            def call(**k):
+                g = k.get
+                return L.qcf_chunk_attn(A, None, B, 32, A, g("kc"), g("kc"), g("slots", 1 << 20), 8 * d, g("table"), g("cols", 70000),
+                                        g("cols", 70000), 16, A, 0, dt, 4, 8, g("max_kv", 0), 32, 8, d, 0.1, g("ws"),
+                                        g("wsb", 0), None)
+            pool = dict(kc=C, table=A)
+            for nothing in ({}, pool, dict(cols=0, max_kv=100), dict(slots=15, max_kv=100), dict(pool, slots=0, cols=0)):
+                for bad in (dict(), dict(wsb=need), dict(ws=A + 16, wsb=need), dict(ws=A, wsb=need - 1)):
+                    assert call(**nothing, **bad) == WORKSPACE, (nothing, bad)
+    for x in ((0, 8, 0), (4, 0, 0), (-1, 8, 0), (4, -1, 0)):
+        assert L.qcf_chunk_attn_workspace_size(*x, 32, 8, 128, BF16) == 0
+
+
+def test_chunk_attn_workspace_grows_from_no_tokens_on(L):
+    for dt in (F32, BF16):
+        for batch, max_q in ((1, 1), (16, 9), (300, 4000)):
+            sizes = [L.qcf_chunk_attn_workspace_size(batch, max_q, kv, 32, 8, 64, dt) for kv in (0, 1, 63, 64, 4096, 33000)]
+            assert sizes == sorted(sizes) and sizes[0] > 0
+
+
 def test_chunk_attn_workspace_is_monotone(L):
     """The size for (batch, max_q, max_kv) covers every smaller call."""
     for dt in (F32, BF16):
