@@ -97,10 +97,12 @@ qcf_status qcf_chunk_attn(void* out, float* lse, const void* q, int64_t n_rows,
  * the pass's new rows those that row r follows: tokens[cu_rows[b] + j] with bit j of row r's tree mask
  * (qcf_page_plan), itself included, or without a mask with j up to its own index; the
  * request's first tokens 0 .. prompt_len[b] - 1 were said as well, outside the answer.
- * With T = 0 the probability is 1 for the largest z (the lowest such token) and 0 elsewhere.  A row without a z
+ * With T = 0 the probability is 1 for the largest z (the lowest such token) and 0 elsewhere; however small T is above 0,
+ * largest z that are equal share it.  A row without a z
  * above -infinity gives zeros (qcf_verify_drafts: token -1); a NaN z or one of +infinity makes a
  * row of probabilities NaN (T = 0: a NaN z is passed over).  Everything is float32: the quotient by the repetition is the
  * product with its reciprocal, the exponential of z / T 2 to the power of z log2(e) / T, the quotient rounded once.
+ * Probabilities, and exponentials on the way to them, below 2^-126 become zero.
  *   out        [n_rows, vocab], rows out_stride elements apart, of type out_dtype; may be the logits
  *              themselves (same type and stride).  Rows at and behind cu_rows[batch] are left as they are
  *   logits     [n_rows, vocab], rows logits_stride elements apart (any stride >= vocab), of type dtype.
@@ -119,8 +121,8 @@ qcf_status qcf_chunk_attn(void* out, float* lse, const void* q, int64_t n_rows,
  *              entries of a token the last counts
  *   allowed    uint32 [n_rows, allowed_words] or NULL: bit t % 32 of word t / 32 allows token t; 32 *
  *              allowed_words >= vocab
- *   temperature  float32 [batch] or NULL (1), not negative; not looked at where probabilities == 0.  Where z / T
- *              passes float32's range it is infinite, as any other z
+ *   temperature  float32 [batch] or NULL (1), not negative; not looked at where probabilities == 0.  z / T may
+ *              pass float32's range: it is formed of differences to the row's largest z
  *   workspace  >= qcf_shape_logits_workspace_size(n_rows, vocab) bytes (may be 0), 256-byte
  *              aligned, no initialisation; calls that overlap in time need separate ones.  A size for
  *              more rows serves fewer.

@@ -10,7 +10,10 @@
 // that was said), HBM in the second.  64 rows of 128000 tokens in float32 31.5 us (2.1 TB/s of logits read once and
 // probabilities written once), 288 rows of 150001 tokens of drafted trees, bf16 to float32, with biases and masks 132 us
 // (2.0 TB/s), without them 108 us (2.4 TB/s).
+#include <float.h>
+
 #include <algorithm>
+#include <type_traits>
 
 #include "qcf_device.h"
 #include "qcf_turns_launch.h"
@@ -34,24 +37,37 @@ constexpr uint32_t said_bit(int bias) { return bias == kPacked ? 1u << 15 : 1u <
 enum Mode { kLogits, kStats, kWrite, kWhole };
 
 // Of a part of a row.  With c = log2(e) / T in float32, exp(z / T) is exp2(z c) but for c's rounding, and exp2(z c - m) with
-// one fused multiply-add keeps that product exact, so that a token near the maximum is hardly off at all.
+// one fused multiply-add keeps that product exact, so that a token near the maximum is hardly off at all.  The rounding of
+// m, up to 2^-24 of it, is the same for all of a part and falls out of the quotient; beyond 2^22 (small temperatures) it
+// would be too much to be an exponent, and such a part's z are taken less the largest first (where z c may pass float32).
 struct Stat {
-  float m, s;  // the maximum times c, sum of exp2(z c - m); T = 0: the maximum
+  float m, s;  // the maximum times c, sum of exp2(z c - m), of a big one exp2((z - max) c); T = 0: the maximum
   int at;      // lowest token with the maximum (T = 0)
-  int pad;
+  float z;     // the maximum
 };
 
+// a value that is the same in every lane, in scalar registers
+__device__ __forceinline__ int uni(int x) { return __builtin_amdgcn_readfirstlane(x); }
+__device__ __forceinline__ float uni(float x) { return __int_as_float(uni(__float_as_int(x))); }
+
 __device__ __forceinline__ float finite(float m) { return m == -INFINITY ? 0.f : m; }
+__device__ __forceinline__ bool is_big(float m) { return fabsf(finite(m)) > 0x1p22f; }
+
+// What a part's sum counts for in one with the maximum r.m (r.z).  Where one of them may be big (they need not both be) the
+// difference of what the sums are taken of is formed in float64, which holds the products.
+template <bool kBig>
+__device__ __forceinline__ float share_of(float m, float z, const Stat& r, float c) {
+  if (!kBig) return __builtin_amdgcn_exp2f(m - finite(r.m));
+  const double a = is_big(m) ? (double)z * c : m, ref = is_big(r.m) ? (double)r.z * c : finite(r.m);
+  return __builtin_amdgcn_exp2f((float)(a - ref));
+}
 
 // two parts of a row, the first's tokens before the second's
-__device__ __forceinline__ Stat both(const Stat& a, const Stat& b, bool cold) {
-  Stat r{fmaxf(a.m, b.m), 0.f, INT32_MAX, 0};
-  if (cold) {
-    r.at = min(a.m == r.m ? a.at : INT32_MAX, b.m == r.m ? b.at : INT32_MAX);
-  } else {
-    const float ref = finite(r.m);
-    r.s = a.s * __builtin_amdgcn_exp2f(a.m - ref) + b.s * __builtin_amdgcn_exp2f(b.m - ref);
-  }
+template <bool kBig>
+__device__ __forceinline__ Stat both(const Stat& a, const Stat& b, bool cold, float c) {
+  Stat r{fmaxf(a.m, b.m), 0.f, INT32_MAX, fmaxf(a.z, b.z)};
+  if (cold) r.at = min(a.m == r.m ? a.at : INT32_MAX, b.m == r.m ? b.at : INT32_MAX);
+  else r.s = a.s * share_of<kBig>(a.m, a.z, r, c) + b.s * share_of<kBig>(b.m, b.z, r, c);
   return r;
 }
 
@@ -282,6 +298,7 @@ __global__ __launch_bounds__(kThreads, 4) void shape_kernel(ShapeLogits p, Stat*
       const float temp = kMode == kLogits ? 1.f : __int_as_float(of(7));
       cold = temp == 0.f;
       c = cold ? 1.f : kLog2e / temp;
+      if (c == INFINITY) c = FLT_MAX;  // (a T below 2^-127 counts as that)
       meet();  // (the counts are zero)
       if (kBias != kNone) {
         bias0 = max(of(8), 0);
@@ -310,7 +327,7 @@ __global__ __launch_bounds__(kThreads, 4) void shape_kernel(ShapeLogits p, Stat*
 #pragma unroll
       for (int k = 0; k < kVecs; ++k) next[k] = load(r + 1, k);
 
-    Stat all{-INFINITY, 0.f, INT32_MAX, 0};
+    Stat all{-INFINITY, 0.f, INT32_MAX, -INFINITY};
     if (kMode == kStats || kMode == kWhole) {
       // the waves', each with its own maximum, then the block's in the waves' order
       float x[kVecs][kVec], m = -INFINITY;
@@ -320,8 +337,9 @@ __global__ __launch_bounds__(kThreads, 4) void shape_kernel(ShapeLogits p, Stat*
 #pragma unroll
         for (int e = 0; e < kVec; ++e) m = fmaxf(m, x[k][e]);
       }
-      m = wave_max(m);
-      Stat wave{cold ? m : m * c, 0.f, INT32_MAX, 0};
+      m = uni(wave_max(m));
+      // (-infinity is kept for a part without a z above it)
+      Stat wave{cold || m == -INFINITY ? m : fmaxf(m * c, -FLT_MAX), 0.f, INT32_MAX, m};
       if (cold) {
         const int id = self();
 #pragma unroll
@@ -331,20 +349,29 @@ __global__ __launch_bounds__(kThreads, 4) void shape_kernel(ShapeLogits p, Stat*
             if (x[k][e] == m && m > -INFINITY) wave.at = p0 + (id + k * kThreads) * kVec + e;
         wave.at = wave_min_i(wave.at);
       } else {
+        const auto sum = [&](auto exponent) {
+#pragma unroll
+          for (int k = 0; k < kVecs; ++k) {
+            float s = 0.f;
+#pragma unroll
+            for (int e = 0; e < kVec; ++e) s += __builtin_amdgcn_exp2f(exponent(x[k][e]));
+            wave.s += s;
+          }
+        };
         const float ref = finite(wave.m);
-#pragma unroll
-        for (int k = 0; k < kVecs; ++k) {
-          float s = 0.f;
-#pragma unroll
-          for (int e = 0; e < kVec; ++e) s += __builtin_amdgcn_exp2f(fmaf(x[k][e], c, -ref));
-          wave.s += s;
-        }
+        if (is_big(wave.m)) sum([&](float z) { return (z - m) * c; });
+        else sum([&](float z) { return fmaf(z, c, -ref); });
         wave.s = wave_sum(wave.s);
       }
       if (lane == 0) red_l[w] = wave;
       meet();
+      const auto join = [&](auto big) {
 #pragma unroll 1
-      for (int i = 0; i < kWaves; ++i) all = both(all, red_l[i], cold);
+        for (int i = 0; i < kWaves; ++i) all = both<decltype(big)::value>(all, red_l[i], cold, c);
+      };
+      // (two loops: the test within one 137 us for the trees above in place of 132)
+      if (__ballot(is_big(red_l[lane % kWaves].m))) join(std::true_type{});
+      else join(std::false_type{});
       if (kMode == kStats && tid == 0) stats[r * pieces + piece] = all;
     } else if (kMode == kWrite) {
       // the row's: pieces in their order, 64 at a time
@@ -353,15 +380,24 @@ __global__ __launch_bounds__(kThreads, 4) void shape_kernel(ShapeLogits p, Stat*
       for (int i0 = 0; i0 < pieces; i0 += 64) {
         Stat one = st[min(i0 + lane, pieces - 1)];
         const bool there = i0 + lane < pieces;
-        const float m = wave_max(there ? one.m : -INFINITY);
-        Stat some{m, 0.f, INT32_MAX, 0};
-        if (cold) some.at = wave_min_i(there && one.m == m ? one.at : INT32_MAX);
-        else some.s = wave_sum(there ? one.s * __builtin_amdgcn_exp2f(one.m - finite(m)) : 0.f);
-        all = both(all, some, cold);
+        // (a row whose maximum is big has it in a part that is)
+        const bool big = __ballot(is_big(one.m)) != 0;
+        Stat some{uni(wave_max(there ? one.m : -INFINITY)), 0.f, INT32_MAX, -INFINITY};
+        if (big) some.z = uni(wave_max(there ? one.z : -INFINITY));
+        if (cold) {
+          some.at = wave_min_i(there && one.m == some.m ? one.at : INT32_MAX);
+        } else {
+          float share = share_of<false>(one.m, one.z, some, c);
+          if (big) share = share_of<true>(one.m, one.z, some, c);
+          some.s = wave_sum(there ? one.s * share : 0.f);
+        }
+        if (i0 == 0) all = some;
+        else all = both<true>(all, some, cold, c);
       }
     }
     if (kMode != kStats) {
-      const float ref = finite(all.m), inv = all.s == 0.f ? 0.f : 1.f / all.s;
+      const bool big = uni(is_big(all.m) && !cold ? 1 : 0);
+      const float ref = uni(big ? 0.f : finite(all.m)), inv = uni(all.s == 0.f ? 0.f : 1.f / all.s), top = uni(all.z);
       Out* out = static_cast<Out*>(p.out) + r * p.out_stride;
 #pragma unroll
       for (int k = 0; k < kVecs; ++k) {
@@ -369,6 +405,10 @@ __global__ __launch_bounds__(kThreads, 4) void shape_kernel(ShapeLogits p, Stat*
         float x[kVec];
         shaped(raw[k], k, x);
         if (kMode != kLogits) {
+          if (big) {
+#pragma unroll
+            for (int e = 0; e < kVec; ++e) x[e] -= top;
+          }
 #pragma unroll
           for (int e = 0; e < kVec; ++e) x[e] = cold ? (t0 + e == all.at ? 1.f : 0.f) : __builtin_amdgcn_exp2f(fmaf(x[e], c, -ref)) * inv;
         }

@@ -305,6 +305,100 @@ def test_shape_logits_cold_and_odd_values():
         _shape([1, 1, 1], [0] * 3, vocab, z=60 * rng.standard_normal((5, vocab)), temps=[0.05, 1.0, 30.0], rep=[1.0, 1e-3, 1e3])
 
 
+def _warmth(z, t):
+    """(float64 probabilities of rows z at temperature t, relative bounds of the kernel's).  log2(e) / T is off by 2 * 2^-24 of
+    itself (the constant, the quotient), the difference to the maximum and its product by one each: 4 * 2^-24 of the gap
+    z / T below the maximum's, of the token's own and, in the sum, of their mean, which is below log(vocab) < 11; the
+    exponential, additions, quotient and rounding as above."""
+    t = float(np.float32(t))
+    with np.errstate(all="ignore"):
+        top = z.max(1, keepdims=True)
+        x = (z - top) / t if math.isfinite(t) else np.where(np.isfinite(z), 0.0, -math.inf)
+        p = np.exp(x)
+    p /= p.sum(1, keepdims=True)
+    return p, p * (4 * np.where(np.isfinite(x), -x, 0) + 44 + 70 + 64) * E
+
+
+@pytest.mark.parametrize("vocab", [37, 500, 8192, 40000])
+@pytest.mark.parametrize("temp", [1e-8, 1e-9, 1e-12, 1e-30, 1e-37])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_small_temperatures(vocab, temp, dtype):
+    """z / T far beyond 2^28 and beyond float32's range: the largest logits share the probability, and logits a few steps of
+    float32 below them get what their difference gives."""
+    say("shape logits, small temperatures", vocab, temp, dtype)
+    rng = np.random.default_rng(vocab)
+    rows, z = 40, rng.uniform(5, 40, (40, vocab))
+    z[::4] *= -1                                                         # the largest is negative
+    z[1::4] -= 60
+    z[2] *= 1e5
+    z = np.asarray(z, np.float32)
+    z[5] = 0
+    z[6, :] = -1
+    z[6, vocab - 1] = 0
+    for r in (3, 7, 11):                                                  # ties, in one piece and in several
+        z[r, [0, vocab // 3, vocab - 1]] = 50
+    for r in (9, 12):                                                     # steps of float32 below the largest
+        z[r, 1], z[r, 2], z[r, vocab - 2] = 70, np.nextafter(np.float32(70), np.float32(0)), 70 - 2.0 ** -15
+    x = torch.from_numpy(z).to(DT[dtype]).cuda()
+    out = torch.empty((rows, vocab), device="cuda")
+    qcf.qcf_shape_logits(out, x, i32(np.arange(rows + 1)), temperature=f32([temp] * rows))
+    p, rel = _warmth(host(x), temp)
+    for r in range(rows):
+        within(host(out)[r], p[r], rel[r] + 2.0 ** -125, f"row {r}")
+
+
+def test_small_temperatures_between_pieces():
+    """Parts of a row on both sides of 2^28, and logits whose difference alone decides between pieces."""
+    say("shape logits, small temperatures between pieces")
+    vocab, t = 30000, 2.0 ** -26
+    rng = np.random.default_rng(4)
+    rows = 30
+    z = np.asarray(rng.uniform(0, 2.7, (rows, vocab)), np.float32)        # z log2(e) / T passes 2^28 at 2.77
+    near = np.float32(2.0 ** 28 * t / math.log2(math.e))
+    for r in range(rows):
+        for at in rng.choice(vocab, 6, replace=False):
+            z[r, at] = near + np.float32(rng.integers(-12, 13) * 2.0 ** -22)
+    z[3] *= -1
+    out = torch.empty((rows, vocab), device="cuda")
+    qcf.qcf_shape_logits(out, torch.from_numpy(z).cuda(), i32(np.arange(rows + 1)), temperature=f32([t] * rows))
+    p, rel = _warmth(z.astype(np.float64), t)
+    for r in range(rows):
+        within(host(out)[r], p[r], rel[r] + 2.0 ** -125, f"row {r}")
+
+
+@pytest.mark.parametrize("vocab", [37, 40000])
+def test_temperatures_at_the_ends_of_float32(vocab):
+    """The smallest temperatures, whose reciprocal is no float32, leave the largest logit; logits of infinity are what they are at
+    any temperature."""
+    say("shape logits, the smallest temperatures", vocab)
+    rng = np.random.default_rng(5)
+    z = np.round(8 * rng.standard_normal((6, vocab))).astype(np.float32)
+    z[1] = 0
+    z[2] = -np.abs(z[2])
+    z[3, 3], z[4], z[5, 1] = math.inf, -math.inf, -math.inf
+    for t in (1e-39, 1e-45, 1e-9):
+        out = torch.empty((6, vocab), device="cuda")
+        qcf.qcf_shape_logits(out, torch.from_numpy(z).cuda(), i32(np.arange(7)), temperature=f32([t] * 6))
+        got = host(out)
+        top = z == z.max(1, keepdims=True)
+        want = top / top.sum(1, keepdims=True)
+        for r in (0, 1, 2, 5):
+            within(got[r], want[r], want[r] * 64 * E, f"row {r}")
+        assert np.isnan(got[3]).all() and (got[4] == 0).all()
+
+
+def test_small_temperatures_feed_verification():
+    """A verifier draws the largest logit's token where the temperature is tiny."""
+    say("shape logits, small temperatures, verification")
+    vocab, B = 20000, 12
+    logits = torch.randn(B, vocab, device="cuda") * 18
+    cu, out = i32(np.arange(B + 1)), torch.empty_like(logits)
+    qcf.qcf_shape_logits(out, logits, cu, temperature=f32([1e-9] * B))
+    n_out, path, toks = i32([0] * B), i32([[0]] * B), i32([[0]] * B)
+    qcf.qcf_verify_drafts(n_out, path, toks, out, i32([1] * B), cu, f32([0.5] * B), f32(np.linspace(0, 0.99, B)))
+    assert toks.view(-1).tolist() == logits.argmax(1).tolist()
+
+
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("which", ["presence", "frequency"])
 def test_infinite_penalties_ban_what_the_answer_has(which, dtype):
