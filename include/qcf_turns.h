@@ -122,7 +122,8 @@ qcf_status qcf_chunk_attn(void* out, float* lse, const void* q, int64_t n_rows,
  *   allowed    uint32 [n_rows, allowed_words] or NULL: bit t % 32 of word t / 32 allows token t; 32 *
  *              allowed_words >= vocab
  *   temperature  float32 [batch] or NULL (1), not negative; not looked at where probabilities == 0.  z / T may
- *              pass float32's range: it is formed of differences to the row's largest z
+ *              pass float32's range: it is formed of differences to the row's largest z.  An infinite one makes all
+ *              finite z equal
  *   workspace  >= qcf_shape_logits_workspace_size(n_rows, vocab) bytes (may be 0), 256-byte
  *              aligned, no initialisation; calls that overlap in time need separate ones.  A size for
  *              more rows serves fewer.

@@ -299,6 +299,7 @@ __global__ __launch_bounds__(kThreads, 4) void shape_kernel(ShapeLogits p, Stat*
       cold = temp == 0.f;
       c = cold ? 1.f : kLog2e / temp;
       if (c == INFINITY) c = FLT_MAX;  // (a T below 2^-127 counts as that)
+      if (c == 0.f) c = 0x1p-149f;     // (infinite: -infinity times c has to stay that, and no finite z counts)
       meet();  // (the counts are zero)
       if (kBias != kNone) {
         bias0 = max(of(8), 0);

@@ -387,6 +387,30 @@ def test_temperatures_at_the_ends_of_float32(vocab):
         assert np.isnan(got[3]).all() and (got[4] == 0).all()
 
 
+@pytest.mark.parametrize("vocab", [37, 8192, 40000])
+def test_large_temperatures(vocab):
+    """The largest temperatures, infinity among them, spread the probability evenly over what is allowed; what is not allowed, or
+    has a logit of -infinity, stays at zero."""
+    say("shape logits, large temperatures", vocab)
+    rng = np.random.default_rng(6)
+    z = (8 * rng.standard_normal((4, vocab))).astype(np.float32)
+    z[1, 2] = -math.inf
+    a = rng.random((4, (vocab + 31) // 32 * 32)) < 0.5
+    a[2], a[3, vocab // 2] = False, True
+    for t in (1e30, 3e38, math.inf):
+        for allowed in (None, a):
+            out = torch.empty((4, vocab), device="cuda")
+            qcf.qcf_shape_logits(out, torch.from_numpy(z).cuda(), i32(np.arange(5)), temperature=f32([t] * 4),
+                                 allowed=None if allowed is None else i32(D.pack_bits(allowed)))
+            some = np.isfinite(z) & (a[:, :vocab] if allowed is not None else True)
+            for r in range(4):
+                if not some[r].any():
+                    assert (host(out)[r] == 0).all()
+                    continue
+                p, rel = _warmth(np.where(some[r], z[r].astype(np.float64), -math.inf)[None], t)
+                within(host(out)[r], p[0], rel[0] + 2.0 ** -125, f"row {r} at {t}")
+
+
 def test_small_temperatures_feed_verification():
     """A verifier draws the largest logit's token where the temperature is tiny."""
     say("shape logits, small temperatures, verification")
