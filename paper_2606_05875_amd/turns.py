@@ -95,18 +95,18 @@ class TurnStep(DraftStep):
                                                  cache.head_dim, cache.dtype)
         self.ws_chunk = torch.empty(max(need, 256), dtype=torch.uint8, device=cache.device)
         self.target = self.ws_shape = None
+        self._shaped = {}  # target and workspace of each vocabulary
         if vocab is not None:
             self._shaping(vocab)
 
     def _shaping(self, vocab):
-        """Room for probabilities over ``vocab`` tokens; what became too small is kept, for a captured pass may
-        write to it."""
-        if self.target is None or self.target.shape[1] != vocab:
-            self._outgrown.append((self.target, self.ws_shape))
+        """Room for probabilities over ``vocab`` tokens; each vocabulary keeps its own, for a captured pass may write to it."""
+        if vocab not in self._shaped:
             dev = self.cache.device
-            self.target = torch.zeros((self.max_rows, vocab), dtype=torch.float32, device=dev)
             need = qcf.qcf_shape_logits_workspace_size(self.max_rows, vocab)
-            self.ws_shape = torch.empty(max(need, 256), dtype=torch.uint8, device=dev)
+            self._shaped[vocab] = (torch.zeros((self.max_rows, vocab), dtype=torch.float32, device=dev),
+                                   torch.empty(max(need, 256), dtype=torch.uint8, device=dev))
+        self.target, self.ws_shape = self._shaped[vocab]
 
     def store(self, layer, q, k, v):
         if self.q_norm is None:

@@ -270,6 +270,29 @@ def test_turns_in_a_graph():
             assert torch.equal(a[:rows_of], b[:rows_of])
 
 
+def test_alternating_vocabularies_keep_their_buffers():
+    """Each vocabulary has one target and workspace, however often it comes; a captured pass finds its own again."""
+    say("turns, alternating vocabularies")
+    freq = qcf.rope_frequencies(64, 1e4)
+    cache = TurnCache(1, 8, 16, 2, 64, 2, 4)
+    step = TurnStep(cache, 6, 3, 4, freq, vocab=500)
+    step.plan(i32([3, 2]))
+    logits = {v: torch.randn(6, v, device="cuda") for v in (500, 20000, 9001)}
+    first = {v: step.shape(x) for v, x in logits.items()}
+    want = {v: t.clone() for v, t in first.items()}
+    at = {v: t.data_ptr() for v, t in first.items()}
+    assert first[500].shape == (6, 500) and len(set(at.values())) == 3
+    torch.cuda.synchronize()
+    held = torch.cuda.memory_allocated()
+    for _ in range(3):
+        for v in (20000, 500, 9001):
+            got = step.shape(logits[v])
+            assert got.data_ptr() == at[v] == step.target.data_ptr() and torch.equal(got[:5], want[v][:5])
+        assert all(torch.equal(first[v][:5], want[v][:5]) for v in first)
+        del got
+    assert torch.cuda.memory_allocated() == held
+
+
 def test_turn_step_refusals():
     freq = qcf.rope_frequencies(64, 1e4)
     cache = TurnCache(2, 8, 8, 2, 64, 2, 4)
