@@ -91,9 +91,12 @@ class TurnStep(DraftStep):
         self.few = self.max_new * group <= FEW_VECTORS or cache.page_size < 16
         if cache.page_size < 16 and any(self.window):
             raise qcf.QcfError("layers with a window need pages of at least 16 rows")
-        need = qcf.qcf_chunk_attn_workspace_size(cache.batch, self.max_new, self.max_kv, n_q_heads, cache.n_kv_heads,
-                                                 cache.head_dim, cache.dtype)
-        self.ws_chunk = torch.empty(max(need, 256), dtype=torch.uint8, device=cache.device)
+        # (68 MB in bf16 at head size 128, whatever the sizes)
+        self.ws_chunk = None
+        if not self.few or any(self.window):
+            need = qcf.qcf_chunk_attn_workspace_size(cache.batch, self.max_new, self.max_kv, n_q_heads,
+                                                     cache.n_kv_heads, cache.head_dim, cache.dtype)
+            self.ws_chunk = torch.empty(max(need, 256), dtype=torch.uint8, device=cache.device)
         self.target = self.ws_shape = None
         self._shaped = {}  # target and workspace of each vocabulary
         if vocab is not None:

@@ -293,6 +293,33 @@ def test_alternating_vocabularies_keep_their_buffers():
     assert torch.cuda.memory_allocated() == held
 
 
+def test_steps_of_few_rows_hold_no_workspace_they_never_use():
+    """Layers that see all tokens of few rows take the tree call; one with a window takes the chunk call, and its rows see
+    the window's tokens."""
+    say("turns of few rows")
+    rng = np.random.default_rng(10)
+    freq = qcf.rope_frequencies(48, 1e4)
+    for ps, window, holds in ((16, 0, False), (8, 0, False), (16, (0, 40), True)):
+        model = Model(rng, "bf16", 2, 8, 2, 64, 100)
+        cache = TurnCache(2, 60, ps, 2, 64, 3, 30)
+        mirror = Mirror(2, 3, 2, 64)
+        first = TurnStep(cache, 300, 130, 8, freq, q_norm=model.qn, k_norm=model.kn, window=window)
+        assert first.ws_chunk is not None or ps < 16
+        run_pass(first, model, [100, 7, 90], mirror, rng)
+        first.commit(all_rows=True)
+        torch.cuda.synchronize()
+        before = torch.cuda.memory_allocated()
+        step = TurnStep(cache, 12, 4, 8, freq, q_norm=model.qn, k_norm=model.kn, window=window)
+        assert step.few and (step.ws_chunk is not None) == holds
+        if not holds:
+            need = qcf.qcf_chunk_attn_workspace_size(3, 4, 30 * ps, 8, 2, 64, torch.bfloat16)
+            assert torch.cuda.memory_allocated() - before < need
+        for new in ([1, 1, 1], [4, 0, 3]):
+            run_pass(step, model, new, mirror, rng)
+            step.commit(all_rows=True)
+            check_cache(cache, mirror)
+
+
 def test_turn_step_refusals():
     freq = qcf.rope_frequencies(64, 1e4)
     cache = TurnCache(2, 8, 8, 2, 64, 2, 4)
