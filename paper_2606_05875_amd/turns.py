@@ -32,7 +32,9 @@ FEW_VECTORS = 256
 
 
 class TurnCache(PagedCache):
-    """Pages of ``n_layers`` layers for up to ``batch`` requests, which may share pages."""
+    """Pages of ``n_layers`` layers for up to ``batch`` requests, which may share pages.  ``pages_missing``: pages that the
+    last change of requests, and the passes since the one before, asked for when none was free (their tokens
+    are not seen); after a change ``free_head`` counts what is free again."""
 
     def __init__(self, n_layers, n_pages, page_size, n_kv_heads, head_dim, batch, max_pages,
                  dtype=torch.bfloat16, device="cuda"):
@@ -40,7 +42,7 @@ class TurnCache(PagedCache):
         i32 = lambda *shape: torch.zeros(shape, dtype=torch.int32, device=self.device)
         self._pools = qcf.PoolSet(self.k + self.v)
         self._table, self._kv, self._held, self._head = i32(batch, max_pages), i32(batch), i32(batch), i32(1)
-        self._head_after = i32(1)
+        self._head_after, self.pages_missing = i32(1), i32(1)
         self._copy_src, self._copy_dst, self._copy_rows = i32(batch), i32(batch), i32(batch)
         self._itself = torch.arange(batch, dtype=torch.int32, device=self.device)
         need = qcf.qcf_page_release_workspace_size(batch, max_pages, n_pages)
@@ -50,7 +52,7 @@ class TurnCache(PagedCache):
         """Request b becomes a continuation of request source[b] (int32; itself, another's, or -1: it ends) at its
         first keep_len[b] tokens (all of them without keep_len).  Full pages are shared, started ones
         copied in every layer, and pages that no request holds any more become free, pages beyond the tokens
-        (rejected drafts) among them."""
+        (rejected drafts) among them; the copies' pages are taken before."""
         qcf.qcf_page_fork(self._table, self._kv, self._held, self.block_table, self.kv_len, source, self.free_pages,
                           self.page_size, self.n_pages, keep_len=keep_len, free_head=self.free_head,
                           free_head_out=self._head, copy_src=self._copy_src, copy_dst=self._copy_dst,
@@ -62,6 +64,7 @@ class TurnCache(PagedCache):
         self.kv_len.copy_(self._kv)
         self.pages_held.copy_(self._held)
         self.free_head.copy_(self._head_after)
+        torch.sub(self._head, self.n_pages, out=self.pages_missing).clamp_(min=0)
 
     def keep(self, keep_len):
         """Every request keeps its first keep_len[b] tokens (0: it ends)."""

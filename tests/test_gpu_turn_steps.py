@@ -320,6 +320,39 @@ def test_steps_of_few_rows_hold_no_workspace_they_never_use():
             check_cache(cache, mirror)
 
 
+def test_a_cache_that_runs_out_of_pages_says_so():
+    """Continuations that find no page: how many were missing is kept (free_head counts free pages alone again), and the list is
+    whole afterwards."""
+    say("turns, pages run out")
+    rng = np.random.default_rng(11)
+    freq = qcf.rope_frequencies(48, 1e4)
+    cache = TurnCache(1, 8, 16, 2, 64, 4, 6)
+    model = Model(rng, "bf16", 1, 4, 2, 64, 100, False)
+    step = TurnStep(cache, 120, 90, 4, freq)
+    mirror = Mirror(1, 4, 2, 64)
+    run_pass(step, model, [84, 7, 0, 0], mirror, rng)                   # 6 + 1 of 8 pages
+    step.commit(all_rows=True)
+    assert int(cache.pages_missing[0]) == 0
+    cache.continue_from(i32([0, 0, 0, 0]))                              # three copies, one page (and the one that 1 gives up, later)
+    assert int(cache.pages_missing[0]) == 2
+    table = cache.block_table.cpu().numpy()
+    assert (table[:, 5] >= 0).sum() == 2 and (table[2:, 5] == -1).all()
+    head, held = int(cache.free_head[0]), {int(p) for p in table.ravel() if p >= 0}
+    assert len(held) + 8 - head == 8 and not held & set(cache.free_pages.tolist()[head:])
+    cache.keep(i32([84, 80, 80, 0]))
+    assert int(cache.pages_missing[0]) == 0
+    mirror.continue_from([0, 0, 0, 0], [84, 80, 80, 0])
+    check_cache(cache, mirror)
+    # planned rows that found no page: free_head says so until requests change, then that change
+    step.plan(i32([10, 1, 1, 40]))
+    assert int(cache.free_head[0]) == cache.n_pages + 3
+    step.commit(all_rows=True)
+    cache.keep(i32([84, 80, 80, 0]))
+    assert int(cache.pages_missing[0]) == 3 and int(cache.free_head[0]) <= cache.n_pages
+    mirror.continue_from([0, 1, 2, 3], [84, 80, 80, 0])
+    check_cache(cache, mirror)
+
+
 def test_turn_step_refusals():
     freq = qcf.rope_frequencies(64, 1e4)
     cache = TurnCache(2, 8, 8, 2, 64, 2, 4)
