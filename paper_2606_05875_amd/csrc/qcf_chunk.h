@@ -174,6 +174,8 @@ __global__ __launch_bounds__(kMergeThreads) void chunk_merge_kernel(ChunkAttn p,
   const float4* part = reinterpret_cast<const float4*>(ws.o);
   float mx = -INFINITY, lt = 0.f;
   float4 a = make_float4(0.f, 0.f, 0.f, 0.f);
+  // (float32: subnormal factors are kept, as the weights are in a unit that is not cut)
+  auto factor = [](float x) { return std::is_same<T, float>::value ? exp2f(x) : __builtin_amdgcn_exp2f(x); };
   auto add = [&](auto count, int x) {
     constexpr int J = decltype(count)::value;
     float2 ml[J];
@@ -189,7 +191,7 @@ __global__ __launch_bounds__(kMergeThreads) void chunk_merge_kernel(ChunkAttn p,
     for (int j = 0; j < J; ++j) {
       if (x + j > x1) break;
       const float mn = fmaxf(mx, ml[j].x);
-      const float fa = __builtin_amdgcn_exp2f(gap(mx, mn)), fo = __builtin_amdgcn_exp2f(gap(ml[j].x, mn));
+      const float fa = factor(gap(mx, mn)), fo = factor(gap(ml[j].x, mn));
       mx = mn;
       lt = fmaf(lt, fa, ml[j].y * fo);
       a.x = fmaf(a.x, fa, o[j].x * fo);

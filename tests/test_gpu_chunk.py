@@ -133,6 +133,31 @@ def test_no_tokens_at_all(dtype, d, window):
     assert (ws[need:] == 0x5A).all()
 
 
+@pytest.mark.parametrize("d", [64, 128])
+def test_float32_weights_stay_above_zero_in_merged_parts(d):
+    """Parts of a row that weigh 2^-135 of it, in a row that is cut over blocks and in one that is not: weights are
+    subnormal numbers (14 bits), so that large values count and infinite ones are infinite."""
+    say("chunk attention small weights", d)
+    for kv in (40, 9000):
+        x = Chunk([kv], [1], 8, 2, d, "f32", 16, seed=15)
+        at = torch.from_numpy(x.slot[0][:kv // 2]).cuda()
+        low = np.float32(-135 / (x.scale * math.log2(math.e)))
+        x.k.zero_()
+        x.k[at, :, 0] = float(low)
+        x.q[:1] = 0
+        x.q[0, :, 0] = 1.0
+        x.v[:, :, 5] = 0
+        x.v[at, :, 5] = 3e34                                             # (4500 of them, weighed 1 in a part, are below 3.4e38)
+        x.v[at[0], :, 3] = math.inf
+        o = host(x.call()[0])[0]
+        weight = 2.0 ** (float(low) * x.scale * math.log2(math.e))
+        want = weight * float(np.float32(3e34)) * (kv // 2) / (kv + 1 - kv // 2)
+        assert (o[:, 3] == math.inf).all()
+        # half a step of the weight is 2^-15 of it at most, of two factors in a row 2^-14; the rest is below 2^-16
+        np.testing.assert_allclose(o[:, 5], want, rtol=2.0 ** -14 + 2.0 ** -16)
+        assert np.isfinite(np.delete(o, 3, axis=1)).all()
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 def test_logits_of_any_size(dtype):
     """One row and head with logits beyond 2^28: the others' bits are those of a call without it; rows that see only
