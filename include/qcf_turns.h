@@ -214,7 +214,7 @@ qcf_status qcf_copy_pages(void* const* pools, int n_pools, int64_t n_slots, int6
  *                pages for large tables.  No initialisation; calls that overlap in time need separate
  *                ones.  The size covers every call whose three values do not exceed those given
  * Entries outside [0, n_pages) are no pages.
- * Errors: null pointers, sizes, n_pages beyond int32, free_head_out that is free_head, 2^22 pieces of 1024
+ * Errors: null pointers, sizes, n_pages beyond int32, outputs that are inputs or one another, 2^22 pieces of 1024
  * entries and more (UNSUPPORTED), workspace.
  */
 size_t qcf_page_release_workspace_size(int batch, int max_pages, int64_t n_pages);

@@ -222,6 +222,7 @@ qcf_status qcf_page_release(const int32_t* table_before, int64_t before_stride,
   const void* in[] = {table_before, table_after, held_before, held_after, free_head};
   for (const void* x : in)
     if (x && (x == free_head_out || x == free_pages)) return QCF_ERR_INVALID_ARG;
+  if (free_pages == free_head_out) return QCF_ERR_INVALID_ARG;
   const size_t need = qcf_page_release_workspace_size(batch, max_pages, n_pages);
   if (workspace_bytes < need || (need > 0 && (!workspace || !aligned256(workspace)))) return QCF_ERR_WORKSPACE;
   // without a table no page is held, whatever the pool: the workspace is not there then

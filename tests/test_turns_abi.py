@@ -200,6 +200,12 @@ def test_page_release_refusals(L):
         assert call(**bad) == WORKSPACE, bad
 
 
+def test_page_release_outputs_are_not_one_another(L):
+    """The new head is written while other threads write the list."""
+    call = lambda free, out: L.qcf_page_release(A, 10, A + 64, A, 10, A + 128, 10, 4, free, 8, C, out, 100, None, 0, None)
+    assert call(B, B) == INVALID
+
+
 def test_the_binding_refuses_host_tensors():
     i, f = torch.zeros(4, dtype=torch.int32), torch.zeros(4, 2, 64)
     t = i.view(2, 2)
