@@ -319,10 +319,14 @@ __global__ __launch_bounds__(kThreads, 4) void shape_kernel(ShapeLogits p, Stat*
         scan(h, 0, prompt, [&](uint32_t at) { atomicOr(&said_l[at], kSaid); });
         scan(h, prompt, n, [&](uint32_t at) { atomicAdd(&said_l[at], 1u); });
       }
-    } else if (p.tokens) {
+      if (p.tokens) drafts(r, 1u);
+    } else if (p.tree_mask) {
       drafts(r - 1, (uint32_t)-1);
+      drafts(r, 1u);
+    } else if (p.tokens && tid == 0) {  // (a chain's next row follows one token more)
+      const uint32_t at = (uint32_t)p.tokens[r] - (uint32_t)p0;
+      if (at < (uint32_t)kPiece) atomicAdd(&said_l[at], 1u);
     }
-    if (p.tokens) drafts(r, 1u);
     meet();
     if (r + 1 < r_end)
 #pragma unroll

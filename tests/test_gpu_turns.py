@@ -274,6 +274,30 @@ def test_shape_logits_long_histories_and_lists(probabilities):
     _shape([5, 4], [40000, 70000], 70003, tree=True, bias=100, pad=(1, 0), offset=3, grammar=True, seed=26, **kw)
 
 
+@pytest.mark.parametrize("probabilities", [True, False])
+def test_long_chains_count_what_they_follow(probabilities):
+    """Chains without a mask give the bits of the same chains with one, in blocks of up to 16 rows that begin and end anywhere
+    in a request."""
+    say("shape logits, long chains", probabilities)
+    rng = np.random.default_rng(30)
+    new, vocab = [4000, 1, 0, 37, 2500, 16, 3, 1700], 8200
+    cu, n = cum(new), sum(new)
+    bits = np.zeros((n, 4000), bool)
+    for b, m in enumerate(new):
+        bits[cu[b]:cu[b + 1], :m] = np.tril(np.ones((m, m), bool))
+    logits = torch.randn((n, vocab), device="cuda").bfloat16()
+    some = lambda lo, hi: f32(rng.uniform(lo, hi, len(new)))
+    kw = dict(tokens=i32(rng.integers(-1, 60, n)), history=i32(rng.integers(0, 90, (len(new), 50))),
+              hist_len=i32([50, 0, 9, 20, 1, 3, 50, 7]), repetition=some(0.7, 1.6), presence=some(-1, 1), frequency=some(-0.01, 0.01),
+              probabilities=probabilities)
+    outs = []
+    for mask in (None, i32(D.pack_bits(bits))):
+        out = torch.empty((n, vocab), device="cuda")
+        qcf.qcf_shape_logits(out, logits, i32(cu), tree_mask=mask, **kw)
+        outs.append(out)
+    assert torch.equal(*outs)
+
+
 def test_shape_logits_in_place_and_many_requests():
     say("shape logits in place, many requests")
     _shape([3, 2], [30, 50], 30001, in_place=True, bias=9, grammar=True)
