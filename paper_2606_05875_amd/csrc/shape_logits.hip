@@ -159,11 +159,11 @@ __global__ __launch_bounds__(kThreads, 4) void shape_kernel(ShapeLogits p, Stat*
   float rep = 1.f, inv_rep = 1.f, pres = 0.f, freq = 0.f, c = 1.f;
   bool cold = false;
   int64_t bias0 = 0;
-  // adds (1) or takes back (-1) the drafted tokens that row r follows
-  auto drafts = [&](int64_t r, uint32_t what) {
+  // adds (1) or takes back (-1) the drafted tokens that row r follows, of the request's from the given one on
+  auto drafts = [&](int64_t r, int64_t from, uint32_t what) {
     const uint32_t* m = p.tree_mask ? p.tree_mask + r * p.mask_words : nullptr;
     const uint32_t end = (uint32_t)max(m ? min(last - first, (int64_t)p.mask_words * 32) : r - first + 1, (int64_t)0);
-    for (uint32_t j = tid; j < end; j += kThreads) {
+    for (uint32_t j = (uint32_t)from + tid; j < end; j += kThreads) {
       const uint32_t at = (uint32_t)p.tokens[first + j] - (uint32_t)p0;
       if (at < (uint32_t)kPiece && (!m || (m[j >> 5] >> (j & 31) & 1))) atomicAdd(&said_l[at], what);
     }
@@ -284,6 +284,7 @@ __global__ __launch_bounds__(kThreads, 4) void shape_kernel(ShapeLogits p, Stat*
       meet();  // the last row's counts have been read
     }
     if (b >= p.batch) return;
+    int64_t chained = 0;
     if (b != counted) {
       const int x = *(param ? param + b + second : p.cu_rows);
       const auto of = [&](int i) { return __builtin_amdgcn_readlane(param ? x : instead, i); };
@@ -319,14 +320,12 @@ __global__ __launch_bounds__(kThreads, 4) void shape_kernel(ShapeLogits p, Stat*
         scan(h, 0, prompt, [&](uint32_t at) { atomicOr(&said_l[at], kSaid); });
         scan(h, prompt, n, [&](uint32_t at) { atomicAdd(&said_l[at], 1u); });
       }
-      if (p.tokens) drafts(r, 1u);
     } else if (p.tree_mask) {
-      drafts(r - 1, (uint32_t)-1);
-      drafts(r, 1u);
-    } else if (p.tokens && tid == 0) {  // (a chain's next row follows one token more)
-      const uint32_t at = (uint32_t)p.tokens[r] - (uint32_t)p0;
-      if (at < (uint32_t)kPiece) atomicAdd(&said_l[at], 1u);
+      drafts(r - 1, 0, (uint32_t)-1);
+    } else {
+      chained = r - first;  // (a chain's next row follows one token more)
     }
+    if (p.tokens) drafts(r, chained, 1u);
     meet();
     if (r + 1 < r_end)
 #pragma unroll
