@@ -187,6 +187,17 @@ def test_logits_of_any_size(dtype):
     assert torch.isnan(o[1]).all() and torch.isnan(e[1]).all() and torch.isfinite(o[[0, 2]]).all()
 
 
+@pytest.mark.parametrize("dtype,window", [("bf16", 0), ("f32", 30), ("bf16", 70)])
+def test_more_requests_than_threads(dtype, window):
+    """700 requests, many without rows: three of them to a thread that adds up the work."""
+    say("chunk attention many requests", dtype, window)
+    rng = np.random.default_rng(16)
+    new, kv = rng.choice([0, 0, 1, 1, 2, 40], 700), rng.choice([0, 1, 15, 16, 100, 300], 700)
+    new[0], new[-1] = 0, 40
+    x = Chunk(kv.tolist(), new.tolist(), 8, 2, 64, dtype, 16, window, seed=17)
+    x.check(*x.call())
+
+
 def test_the_same_as_the_tree_call_without_a_mask():
     """Rows of a decoded token, a chain and a prompt: what qcf_tree_attn gives, within both calls' roundings."""
     say("chunk and tree attention")

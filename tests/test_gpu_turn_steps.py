@@ -211,6 +211,35 @@ def test_an_answer_from_shaped_probabilities():
         check_cache(cache, mirror)
 
 
+def test_the_first_token_after_a_question():
+    """One row of logits per request, its last: the question is cached by then, so its tokens count from the history."""
+    say("the first token after a question")
+    rng = np.random.default_rng(12)
+    layers, hq, hkv, d, B, vocab = 1, 8, 2, 64, 3, 9000
+    cache = TurnCache(layers, 40, 16, hkv, d, B, 12)
+    model = Model(rng, "bf16", layers, hq, hkv, d, vocab)
+    step = TurnStep(cache, 260, 100, hq, qcf.rope_frequencies(64, 1e4), q_norm=model.qn, k_norm=model.kn)
+    mirror = Mirror(layers, B, hkv, d)
+    history, prompt = rng.integers(0, 60, (B, 192)), [10, 0, 100]
+    for new in ([10, 90, 100], [70, 1, 66]):
+        run_pass(step, model, new, mirror, rng)
+        step.commit(all_rows=True)
+    logits, rep, freq, temp = rng.standard_normal((B, vocab)).astype(np.float32), [1.3, 0.8, 1.0], [0.2, 0.1, -0.3], [1.0, 0.5, 2.0]
+    rows, target = i32(np.arange(B + 1)), torch.empty((B, vocab), device="cuda")
+    qcf.qcf_shape_logits(target, f32(logits), rows, history=i32(history), prompt_len=i32(prompt), hist_len=cache.kv_len,
+                         repetition=f32(rep), frequency=f32(freq), temperature=f32(temp))
+    want = np.array([T.shape_logits(logits[b], history[b, :prompt[b]], history[b, prompt[b]:n], float(np.float32(rep[b])), 0.0,
+                                    float(np.float32(freq[b])), temperature=temp[b])[0] for b, n in enumerate(mirror.lengths())])
+    # (test_gpu_turns' bound: |z| below 5 + 0.3 * 170, T from 0.5, so 4 * 8 * 2^-24 * 56 / 0.5 and (2 * 61 / 0.5 + 79) * 2^-24)
+    np.testing.assert_allclose(host(target), want, rtol=2.4e-4, atol=2.0 ** -125)
+    n_out, path, toks = i32([0] * B), i32([[0]] * B), i32([[0]] * B)
+    u = np.array([0.1, 0.5, 0.9])
+    qcf.qcf_verify_drafts(n_out, path, toks, target, i32([0] * B), rows, f32([0.5] * B), f32(u))
+    for b, t in enumerate(toks.view(-1).tolist()):                      # drawn where the running sum passes u
+        c = np.cumsum(want[b])
+        assert c[t] >= u[b] - 1e-3 and (t == 0 or c[t - 1] <= u[b] + 1e-3)
+
+
 def test_turns_in_a_graph():
     """A captured turn (fork, chunk, shaped probabilities) replays beside eager ones with the same results."""
     say("turns in a graph")
