@@ -30,11 +30,13 @@ extern "C" {
  *     norm(x)[j] = x[j] / sqrt( (sum_i x[i]^2) / head_dim + eps ) * w[j]
  * over each head's head_dim elements, w the head's weight for queries or for keys.  Values are
  * stored as they are.  Everything up to the result's one rounding is float32 (the sum of squares too:
- * a head whose squares pass its range gives zeros), the angles float64.
+ * a head whose squares pass its range gives zeros, squares below 2^-126 lose bits and count as zeros below
+ * 2^-149, so that eps decides), the angles float64.
  *   q_weight, k_weight  one weight [head_dim] for all heads (weight stride 0), or a head's own
  *                 (head h's at h * weight stride, >= head_dim, a multiple of 16 bytes), of type dtype;
  *                 NULL: ones (its stride is 0 then).  16-byte aligned
- *   eps           finite and not negative (0: a head of zeros is NaN)
+ *   eps           finite and not negative (0: a head of zeros is NaN, one whose squares all count as zeros
+ *                 not finite)
  * All other arguments, and rows without a slot or a source, as for qcf_rope_store; without
  * positions rows are normed and not turned.
  * Errors: as for qcf_rope_store; eps, weights or their strides.

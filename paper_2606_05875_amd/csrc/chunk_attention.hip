@@ -3,21 +3,24 @@
 // One pass over the tokens with the softmax's running maximum m and sum l per query vector: S = K Q^T, p =
 // exp2(S - m), O = O alpha + V^T p^T, on v_mfma_f32_32x32x16_bf16.  Products are transposed, as in the other
 // attention kernels of this library: a lane holds tokens' logits of ONE query vector, so its p are the
-// second product's operand as they stand.  A wave holds 32 query vectors (consecutive rows times the heads
+// second product's operand as they stand: one bf16 number each, 2^-8 of it off at most, after they entered the sum in
+// float32 (a second number for the rest, as the tree kernel has for few vectors, would be half as many products again).
+// A wave holds 32 query vectors (consecutive rows times the heads
 // that share a KV head), the 4 waves of a block share every 64-token tile, and the products of the next
 // tile's S run beside this tile's exponentials.
 //
 // Keys and values go from the pages into LDS without passing registers, two stages of each: step t asks for
 // K(t+2) and V(t+1) before anything else and ends by waiting for them (in between the products of S(t+1), as the contiguous
-// kernels do, the 16 questions below took 252 us in place of 247: pages are rarely in the L2).  Wave w copies the tile's
+// kernels do, the 16 questions below took 2% longer: pages are rarely in the L2).  Wave w copies the tile's
 // rows 16 w .. + 15, which lie in one page; the page numbers of a tile's four groups come by one load, a step
 // ahead of the copies.
 // Two blocks per CU: one's products run beside the other's exponentials, starts and ends.
 // Bound: matrix units and vector units together, where tiles are whole and long: 2048 rows over 30848 tokens, 64/8 heads
-// of 128, 2045 us, 1.04 PFLOP/s.  16 questions of 16 to 128 rows over 2000 to 12700 tokens (32/8 heads) 245 us, 0.69
+// of 128, 2075 us, 1.03 PFLOP/s.  16 questions of 16 to 128 rows over 2000 to 12700 tokens (32/8 heads) 250 us, 0.67
 // PFLOP/s: tiles of 32 rows are rounded up, units of a few tiles start and end, some are merged, and a fifth is waiting for
-// pages (202 us with all tokens in the same few).  Head size 64 does half
-// the products per exponential: prompts of 700 to 4000 rows with windows of 1024, 226 us, 0.53 PFLOP/s.
+// pages (191 us with all tokens in the same few).  Head size 64 does half
+// the products per exponential: prompts of 700 to 4000 rows with windows of 1024, 232 us, 0.52 PFLOP/s.  64 single rows in
+// such windows (32/8 heads of 128) 77 us, 3.5 TB/s: a tile of 128 vectors holds 4.
 #include "qcf_chunk.h"
 #include "qcf_paged.h"
 

@@ -144,7 +144,7 @@ __device__ __forceinline__ ReleaseRow release_row(const PageRelease& p, int i) {
 }
 
 // Small tables: one block marks the pages of both tables in LDS (two bits per page) and writes those that are only in
-// the first.  Bound: latency (16 requests of up to 200 pages 9.2 us, of three dependent loads; one of 2 pages 6.4).
+// the first.  Bound: latency (16 requests of up to 200 pages 9 us, of three dependent loads; one of 2 pages 6.4).
 constexpr int kRelThreads = 1024;
 constexpr int kRelWords = 1 << 14;  // of 32 pages, per bit set
 

@@ -209,7 +209,7 @@ __global__ __launch_bounds__(kMergeThreads) void chunk_merge_kernel(ChunkAttn p,
 }
 
 // How a call is cut, from its bounds (lengths are on the device): tiles of 128 vectors (float32: 32), as many
-// blocks as run at once, two per CU.  (Three of head size 64, whose registers would do: 246 us against 240 for
+// blocks as run at once, two per CU.  (Three of head size 64, whose registers would do: 234 us against 233 for
 // prompts of 700 to 4000 rows with windows of 1024: the vector units are busy with two.)
 constexpr int kChunkBlocks = 512;
 inline ChunkCut chunk_cut(int max_q, int hq, int hkv, bool bf16) {
@@ -217,7 +217,7 @@ inline ChunkCut chunk_cut(int max_q, int hq, int hkv, bool bf16) {
   ChunkCut c;
   c.vt_log2 = bf16 ? 7 : 5;
   c.tiles = (int)((vectors + (1 << c.vt_log2) - 1) >> c.vt_log2);
-  c.start = 6;  // (what it costs in steps: windows of 1024 246, 226, 224, 224 us with 2, 4, 6, 9; 16 questions 249, 247, 246, 244)
+  c.start = 6;  // (what it costs in steps: windows of 1024 252, 233, 233, 232 us with 2, 4, 6, 9; 16 questions 252, 250, 250, 248)
   c.blocks = kChunkBlocks;
   return c;
 }

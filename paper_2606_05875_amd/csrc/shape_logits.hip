@@ -7,7 +7,7 @@
 // maximum and its sum of exponentials, then the row's from all of them (in the pieces' order) and the values; a row
 // of one piece takes one.  z is formed the same way both times, so nothing is stored in between.
 // Bound: instructions in the first launch (about 13 vector instructions per token where its vector has a token
-// that was said), HBM in the second.  64 rows of 128000 tokens in float32 31.5 us (2.1 TB/s of logits read once and
+// that was said), HBM in the second.  64 rows of 128000 tokens in float32 31.7 us (2.1 TB/s of logits read once and
 // probabilities written once), 288 rows of 150001 tokens of drafted trees, bf16 to float32, with biases and masks 132 us
 // (2.0 TB/s), without them 108 us (2.4 TB/s).
 #include <float.h>
@@ -25,7 +25,7 @@ constexpr int kThreads = 256;
 constexpr int kVec = 8;  // tokens of a thread at a time
 constexpr int kWaves = kThreads / 64;
 // Where the biases' entries are kept: nowhere, in the upper half of the tokens' counts, or, for long lists and histories
-// whose counts could pass 15 bits, beside them (pieces are half as long then: the trees above 176 us in place of 141)
+// whose counts could pass 15 bits, beside them (pieces are half as long then: the trees above 149 us in place of 132)
 enum Bias { kNone, kPacked, kBeside };
 // Tokens of a block's piece: 32 KB of LDS for what is looked up of them
 constexpr int piece_of(int bias) { return bias == kBeside ? 4096 : 8192; }

@@ -135,7 +135,8 @@ class TurnStep(DraftStep):
 
     def shape(self, logits, tokens=None, history=None, prompt_len=None, **shaping):
         """``target`` [max_rows, vocab] <- the probabilities of the model's logits [max_rows, vocab] after the planned
-        rows.  ``tokens`` are the rows' tokens and ``history`` [batch, width] those of the requests' cached tokens, in
+        rows: of all of them, for drafted tokens.  (After a question or a prompt, of which each request's last row
+        alone is drawn from, qcf.qcf_shape_logits takes those rows, with the question in the history.)  ``tokens`` are the rows' tokens and ``history`` [batch, width] those of the requests' cached tokens, in
         their order, of which the first prompt_len[b] count as the prompt (so before ``commit``); the rest as
         qcf.qcf_shape_logits takes it (repetition, presence, frequency, bias_*, allowed, temperature)."""
         self._shaping(logits.shape[1])
