@@ -435,6 +435,36 @@ def test_large_temperatures(vocab):
                 within(host(out)[r], p[0], rel[0] + 2.0 ** -125, f"row {r} at {t}")
 
 
+@pytest.mark.parametrize("vocab,entries", [(6000, 0), (6000, 60), (6000, 70000), (20011, 60), (20011, 70000), (600001, 60), (600001, 70000)])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_temperatures_of_shaped_logits(vocab, entries, dtype):
+    """Rows of requests with small, ordinary and large temperatures side by side, with penalties, biases and masks, in one
+    piece, several and more than 64: the probabilities of the logits that the same call gives."""
+    say("shape logits, temperatures of shaped logits", vocab, entries, dtype)
+    rng = np.random.default_rng(vocab + entries)
+    new, temps = [2, 1, 1, 1, 2, 1], [1e-9, 1.0, 2.0 ** -19, math.inf, 1e-38, 0.25]
+    B, n = len(new), sum(new)
+    some = lambda lo, hi: f32(rng.uniform(lo, hi, B))
+    a = rng.random((n, (vocab + 31) // 32 * 32)) < 0.7
+    a[2] = False
+    a[4] = True
+    kw = dict(tokens=i32(rng.integers(0, 60, n)), history=i32(rng.integers(0, vocab, (B, 300))), hist_len=i32([300, 0, 9, 20, 1, 300]),
+              repetition=some(0.7, 1.6), presence=some(-1, 1), frequency=some(-1, 1), allowed=i32(D.pack_bits(a)))
+    if entries:
+        each = rng.multinomial(entries, [1 / B] * B)
+        kw.update(bias_start=i32(cum(each)), bias_token=i32(rng.integers(0, vocab, entries)), bias_value=f32(rng.normal(0, 3, entries)))
+    x = (5 * torch.randn((n, vocab), device="cuda")).to(DT[dtype])
+    z, out = (torch.empty((n, vocab), device="cuda") for _ in range(2))
+    qcf.qcf_shape_logits(z, x, i32(cum(new)), probabilities=False, **kw)
+    qcf.qcf_shape_logits(out, x, i32(cum(new)), temperature=f32(temps), **kw)
+    z, out = host(z), host(out)
+    assert (out[2] == 0).all()
+    for r, b in enumerate(np.repeat(np.arange(B), new)):
+        if r != 2:
+            p, rel = _warmth(z[r][None], temps[b])
+            within(out[r], p[0], rel[0] + (200 * E) * p[0] + 2.0 ** -125, f"row {r}")   # (up to 147 pieces joined)
+
+
 def test_small_temperatures_feed_verification():
     """A verifier draws the largest logit's token where the temperature is tiny."""
     say("shape logits, small temperatures, verification")
