@@ -15,12 +15,12 @@
 // rows 16 w .. + 15, which lie in one page; the page numbers of a tile's four groups come by one load, a step
 // ahead of the copies.
 // Two blocks per CU: one's products run beside the other's exponentials, starts and ends.
-// Bound: matrix units and vector units together, where tiles are whole and long: 2048 rows over 30848 tokens, 64/8 heads
-// of 128, 2022 to 2082 us from card to card, 1.03 to 1.06 PFLOP/s.  16 questions of 16 to 128 rows over 2000 to 12700
-// tokens (32/8 heads) 246 to 250 us, 0.67 PFLOP/s: tiles of 32 rows are rounded up, units of a few tiles start and end, some are merged, and a fifth is waiting for
-// pages (191 us with all tokens in the same few).  Head size 64 does half
-// the products per exponential: prompts of 700 to 4000 rows with windows of 1024, 225 to 233 us, 0.52 PFLOP/s.  64 single rows in
-// such windows (32/8 heads of 128) 77 us, 3.5 TB/s: a tile of 128 vectors holds 4.
+// Bound: matrix units and vector units together, where tiles are whole and long: 2048 rows over 30848 tokens, 64/8
+// heads of 128, 2022 to 2082 us from card to card, 1.03 to 1.06 PFLOP/s.  16 questions of 16 to 128 rows over 2000 to
+// 12700 tokens (32/8 heads) 246 to 250 us, 0.67 PFLOP/s: tiles of 32 rows are rounded up, units of a few tiles start
+// and end, some are merged, and a fifth is waiting for pages (191 us with all tokens in the same few).  Head size 64
+// does half the products per exponential: prompts of 700 to 4000 rows with windows of 1024, 225 to 233 us, 0.52
+// PFLOP/s.  64 single rows in such windows (32/8 heads of 128) 77 us, 3.5 TB/s: a tile of 128 vectors holds 4.
 #include "qcf_chunk.h"
 #include "qcf_paged.h"
 
